@@ -83,6 +83,13 @@ typedef enum smat_storage {
   SMAT_SIMULATED = 1 /* the model sees the reusable buffer holding theta~ */
 } smat_storage;
 
+typedef enum smat_act {
+  SMAT_ACT_NONE = 0,
+  SMAT_ACT_GELU = 1,      /* z Phi(z), Phi the standard normal's distribution function */
+  SMAT_ACT_GELU_TANH = 2, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+  SMAT_ACT_SILU = 3       /* z / (1 + exp(-z)) */
+} smat_act;
+
 /* Per-tensor operation parameters (Sec. 4.1).
  *   s          scale (the paper's alpha), finite
  *   keep       keep probability 1 - p in [0, 1]; keep >= 1 leaves the tensor outside the mask
@@ -526,6 +533,120 @@ smat_status smat_merge_plan_destroy(smat_merge_plan* plan);
  * and size must be multiples of 16 bytes and the ranges must not overlap.  Errors:
  * SMAT_ERR_INVALID, SMAT_ERR_HIP. */
 smat_status smat_stream_copy(const void* src, void* dst, uint64_t bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------- linear layers, 8-bit activation checkpoints
+ * The layers whose weights the simulated steps transform: a product with its epilogue in one pass, its
+ * gradients, and the activations that a training step saves between them, held in 8 bits.
+ *
+ * Matrices are row-major with a row stride ld in elements (ld >= columns) and contiguous rows, at any
+ * element's alignment; dimensions are at most 2^31 - 1 and rows * ld below 2^60.  A call's matrices have one dtype (SMAT_F32 or
+ * SMAT_BF16); products and epilogues are computed in fp32 (bf16 products are exact there) and each output is
+ * rounded once.  A dimension of 0 is valid: no output, or, where the summed dimension is 0, an empty sum.
+ * Outputs must not overlap inputs or each other, except that `out` may be `mul` or `residual`
+ * itself (same pointer and row stride).
+ *
+ * Calls take device memory for partial sums from the caller: `workspace` of at least the bytes that the
+ * matching *_workspace_bytes call gives for the same arguments (0: NULL is allowed), aligned to 16 bytes.
+ * It may be reused by later work on the same stream.  The calls can be captured into a graph.
+ *
+ * A checkpoint of a matrix [rows, cols] is, with blocks = ceil(cols / 32),
+ *   codes  [rows, 32 * blocks] int8, aligned to 16 bytes, zeros in the columns past cols
+ *   exps   [rows, blocks] uint8
+ * An element is codes * 2^(exps - 127).  A block's power of two is 2^E with
+ * E = max(floor(log2 max|x|) - 6, -126); codes are x 2^-E rounded to nearest even and held to +-127.
+ * So |x - x^| <= 2^E / 2, except that x between 127.5 and 128 times 2^E reads back as 127 * 2^E.  A block that holds
+ * a NaN or an infinity has exps 255 and codes 0 and reads back as NaNs.  Values read back are
+ * exact in bf16 and fp32. */
+
+/* smat_ckpt_write -- the checkpoint of x [rows, cols].  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+smat_status smat_ckpt_write(const void* x, int64_t ldx, smat_dtype dtype, int64_t rows, int64_t cols, int8_t* codes,
+                            uint8_t* exps, hipStream_t stream);
+
+/* smat_ckpt_read -- out = act(z^), or act(z^) (.) u^ with a second checkpoint (up_codes, up_exps; NULL: none), in
+ * fp32, rounded once.  Reads a saved activation back, or recomputes a layer's output from its saved
+ * pre-activation (and a gated MLP's hidden activation from both).  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE,
+ * SMAT_ERR_HIP. */
+smat_status smat_ckpt_read(const int8_t* codes, const uint8_t* exps, const int8_t* up_codes, const uint8_t* up_exps,
+                           smat_act act, smat_dtype dtype, int64_t rows, int64_t cols, void* out, int64_t ldout,
+                           hipStream_t stream);
+
+/* Arguments of smat_linear: z = x W^T + bias, out = act(z) (.) mul + residual. */
+typedef struct smat_linear_args {
+  int32_t dtype, act;      /* smat_dtype, smat_act */
+  int64_t m, n, k;
+  const void* x;           /* [m, k] */
+  int64_t ldx;
+  const void* w;           /* [n, k] */
+  int64_t ldw;
+  const void* bias;        /* [n], or NULL */
+  const void* mul;         /* [m, n], or NULL: 1 */
+  int64_t ldmul;
+  const void* residual;    /* [m, n], or NULL: 0 */
+  int64_t ldres;
+  void* out;               /* [m, n] */
+  int64_t ldout;
+  int8_t* z_codes;         /* checkpoint of z (of its fp32 values), or NULL for both */
+  uint8_t* z_exps;
+} smat_linear_args;
+
+/* smat_linear -- the layer's forward pass, from single tokens (m = 1) up.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE,
+ * SMAT_ERR_HIP. */
+smat_status smat_linear_workspace_bytes(const smat_linear_args* args, size_t* bytes);
+smat_status smat_linear(const smat_linear_args* args, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Arguments of smat_linear_dgrad: v = dy W + dy2 W2, and with the checkpoints z^ (and u^) of the layer whose
+ * output's gradient v is,
+ *   out = v                                                       no z checkpoint (act = SMAT_ACT_NONE)
+ *   out = v (.) act'(z^)                                          z
+ *   out = v (.) u^ (.) act'(z^), out_up = v (.) act(z^)           z and up: the gradients of z and u where the
+ *                                                                 layer's output was act(z) (.) u */
+typedef struct smat_linear_dgrad_args {
+  int32_t dtype, act;
+  int64_t m, n, k, k2;
+  const void* dy;          /* [m, k] */
+  int64_t lddy;
+  const void* w;           /* [k, n] */
+  int64_t ldw;
+  const void* dy2;         /* [m, k2]; k2 = 0: no second product */
+  int64_t lddy2;
+  const void* w2;          /* [k2, n] */
+  int64_t ldw2;
+  const int8_t* z_codes;   /* checkpoint of z [m, n], or NULL for both */
+  const uint8_t* z_exps;
+  const int8_t* up_codes;  /* checkpoint of u [m, n], or NULL for both */
+  const uint8_t* up_exps;
+  void* out;               /* [m, n] */
+  int64_t ldout;
+  void* out_up;            /* [m, n] with up, else NULL */
+  int64_t ldup;
+} smat_linear_dgrad_args;
+
+/* smat_linear_dgrad -- the gradient at a layer's input, taken through the activation that produced it.
+ * Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+smat_status smat_linear_dgrad_workspace_bytes(const smat_linear_dgrad_args* args, size_t* bytes);
+smat_status smat_linear_dgrad(const smat_linear_dgrad_args* args, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
+
+/* Arguments of smat_linear_wgrad: dw = dy^T x, db = the column sums of dy. */
+typedef struct smat_linear_wgrad_args {
+  int32_t dtype, reserved; /* reserved must be 0 */
+  int64_t m, n, k;
+  const void* dy;          /* [m, n] */
+  int64_t lddy;
+  const void* x;           /* [m, k], or NULL: its checkpoint is given */
+  int64_t ldx;
+  const int8_t* x_codes;   /* checkpoint of x, or NULL for both */
+  const uint8_t* x_exps;
+  void* dw;                /* [n, k] */
+  int64_t lddw;
+  void* db;                /* [n], or NULL */
+} smat_linear_wgrad_args;
+
+/* smat_linear_wgrad -- the gradients of a layer's weight and bias; the same bits in every run.  Errors:
+ * SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+smat_status smat_linear_wgrad_workspace_bytes(const smat_linear_wgrad_args* args, size_t* bytes);
+smat_status smat_linear_wgrad(const smat_linear_wgrad_args* args, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
 
 /* smat_last_error -- message of the last failure on the calling thread ("" if none). */
 const char* smat_last_error(void);

@@ -20,6 +20,7 @@ SMAT_OK, SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_STATE, SMAT_ERR_HIP = 0, 1, 
 SMAT_F32, SMAT_BF16 = 0, 1
 SMAT_NOISE_GAUSSIAN, SMAT_NOISE_UNIFORM, SMAT_NOISE_LAPLACE = 0, 1, 2
 SMAT_EXPERT, SMAT_SIMULATED = 0, 1
+SMAT_ACT_NONE, SMAT_ACT_GELU, SMAT_ACT_GELU_TANH, SMAT_ACT_SILU = 0, 1, 2, 3
 
 STATUS_NAMES = {0: "SMAT_OK", 1: "SMAT_ERR_INVALID", 2: "SMAT_ERR_DTYPE", 3: "SMAT_ERR_STATE", 4: "SMAT_ERR_HIP"}
 
@@ -33,6 +34,8 @@ EXPORTS = (
     "smat_stream_copy", "smat_backward_multi", "smat_plan_clear_grads", "smat_simulate_multi_dev",
     "smat_backward_multi_dev", "smat_adamw_fused_multi_dev", "smat_grad_norm_multi_dev", "smat_step_state_advance",
     "smat_scale_draw", "smat_simulate_multi_static",
+    "smat_ckpt_write", "smat_ckpt_read", "smat_linear", "smat_linear_workspace_bytes", "smat_linear_dgrad",
+    "smat_linear_dgrad_workspace_bytes", "smat_linear_wgrad", "smat_linear_wgrad_workspace_bytes",
 )
 
 
@@ -80,6 +83,27 @@ class smat_merge_term(ctypes.Structure):
 class smat_merge_desc(ctypes.Structure):
     _fields_ = [("theta0", c_void_p), ("out", c_void_p), ("n", c_int64), ("tensor_id", c_uint32),
                 ("reserved", c_uint32), ("elem_offset", c_uint64)]
+
+
+class smat_linear_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("act", c_int32), ("m", c_int64), ("n", c_int64), ("k", c_int64),
+                ("x", c_void_p), ("ldx", c_int64), ("w", c_void_p), ("ldw", c_int64), ("bias", c_void_p),
+                ("mul", c_void_p), ("ldmul", c_int64), ("residual", c_void_p), ("ldres", c_int64),
+                ("out", c_void_p), ("ldout", c_int64), ("z_codes", c_void_p), ("z_exps", c_void_p)]
+
+
+class smat_linear_dgrad_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("act", c_int32), ("m", c_int64), ("n", c_int64), ("k", c_int64), ("k2", c_int64),
+                ("dy", c_void_p), ("lddy", c_int64), ("w", c_void_p), ("ldw", c_int64),
+                ("dy2", c_void_p), ("lddy2", c_int64), ("w2", c_void_p), ("ldw2", c_int64),
+                ("z_codes", c_void_p), ("z_exps", c_void_p), ("up_codes", c_void_p), ("up_exps", c_void_p),
+                ("out", c_void_p), ("ldout", c_int64), ("out_up", c_void_p), ("ldup", c_int64)]
+
+
+class smat_linear_wgrad_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("reserved", c_int32), ("m", c_int64), ("n", c_int64), ("k", c_int64),
+                ("dy", c_void_p), ("lddy", c_int64), ("x", c_void_p), ("ldx", c_int64),
+                ("x_codes", c_void_p), ("x_exps", c_void_p), ("dw", c_void_p), ("lddw", c_int64), ("db", c_void_p)]
 
 
 class SmatError(RuntimeError):
@@ -133,6 +157,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "smat_scale_draw": [c_uint64, c_uint32, c_float, POINTER(c_float)],
         "smat_simulate_multi_static": [POINTER(smat_tensor_desc), c_int32, c_int32, c_int32, POINTER(smat_op_params),
                                        c_uint64, c_uint32, P],
+        "smat_ckpt_write": [P, c_int64, c_int32, c_int64, c_int64, P, P, P],
+        "smat_ckpt_read": [P, P, P, P, c_int32, c_int32, c_int64, c_int64, P, c_int64, P],
+        "smat_linear": [POINTER(smat_linear_args), P, c_size_t, P],
+        "smat_linear_workspace_bytes": [POINTER(smat_linear_args), POINTER(c_size_t)],
+        "smat_linear_dgrad": [POINTER(smat_linear_dgrad_args), P, c_size_t, P],
+        "smat_linear_dgrad_workspace_bytes": [POINTER(smat_linear_dgrad_args), POINTER(c_size_t)],
+        "smat_linear_wgrad": [POINTER(smat_linear_wgrad_args), P, c_size_t, P],
+        "smat_linear_wgrad_workspace_bytes": [POINTER(smat_linear_wgrad_args), POINTER(c_size_t)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "smat.h"
+#include "smat_error.h"
 #include "smat_launch.h"
 
 using smat::AdamConsts;
@@ -22,10 +23,10 @@ using smat::StepState;
 using smat::TensorRec;
 
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
 
-smat_status fail(smat_status st, const char* fmt, ...) {
+smat_status smat::fail(smat_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -35,11 +36,9 @@ smat_status fail(smat_status st, const char* fmt, ...) {
   return st;
 }
 
-#define SMAT_HIP(call)                                                                   \
-  do {                                                                                   \
-    hipError_t e_ = (call);                                                              \
-    if (e_ != hipSuccess) return fail(SMAT_ERR_HIP, "%s: %s", #call, hipGetErrorString(e_)); \
-  } while (0)
+using smat::fail;
+
+namespace {
 
 constexpr uint32_t kMaxStep = 1u << 30;
 

@@ -1,0 +1,75 @@
+// Arguments and host-side launchers of the linear-layer kernels and the activation checkpoints
+// (internal to libsmat).
+//
+// Every product is out[i][j] = sum_r P(i, r) Q(j, r) with an epilogue on out.  An operand is `direct`
+// where r runs along its rows, P(i, r) = P[i ld + r], and `transposed` where its rows are r,
+// P(i, r) = P[r ld + i]:
+//   layer            P = x [m, k] direct        Q = W [n, k] direct        i = m, j = n, r = k
+//   data gradient    P = dy [m, k] direct       Q = W [k, n] transposed    i = m, j = n, r = k
+//   weight gradient  P = dy [m, n] transposed   Q = x [m, k] transposed    i = n, j = k, r = m
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace smat {
+
+constexpr int kCkptBlock = 32;  // elements along a row that share a checkpoint's power of two
+inline int64_t ckpt_blocks(int64_t cols) { return (cols + kCkptBlock - 1) / kCkptBlock; }
+
+enum LinEpilogue : int { kEpiStore = 0, kEpiLayer = 1, kEpiDgrad = 2 };
+
+struct LinProduct {
+  const void* p;
+  const void* q;
+  int64_t ldp, ldq;
+  int64_t r;
+};
+
+struct LinArgs {
+  LinProduct prod[2];  // the products that are summed; prod[1].r == 0 where there is one
+  int64_t i, j;
+  void* out;
+  int64_t ldout;
+  // layer: out = act(v + bias) (.) mul + residual, codes and exps of v + bias
+  const void* bias;
+  const void* mul;
+  const void* residual;
+  int64_t ldmul, ldres;
+  int8_t* codes;
+  uint8_t* exps;
+  // data gradient: act'(z^) from z, u^ from up; out_up = v (.) act(z^)
+  const int8_t* z_codes;
+  const uint8_t* z_exps;
+  const int8_t* up_codes;
+  const uint8_t* up_exps;
+  void* out_up;
+  int64_t ldup;
+  int32_t act;
+  // sums of `splits` ranges of r, joined by a second kernel: [splits][i][j rounded up to 8] fp32
+  int32_t splits;
+  float* partial;
+};
+
+// Element types by smat_dtype code: 0 = fp32, 1 = bf16.
+struct LinPlan {
+  int32_t splits;
+  size_t workspace;  // bytes
+};
+LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi);
+hipError_t launch_linear(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
+                         hipStream_t stream);
+
+// db[j] = sum_i dy[i][j] for dy [rows, cols].
+size_t column_sum_workspace(int64_t rows, int64_t cols);
+hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t cols, int dtype, void* db,
+                             void* workspace, hipStream_t stream);
+
+hipError_t launch_ckpt_write(const void* x, int64_t ld, int64_t rows, int64_t cols, int dtype, int8_t* codes,
+                             uint8_t* exps, hipStream_t stream);
+// out = act(z^), or act(z^) (.) u^ with up_codes.
+hipError_t launch_ckpt_read(const int8_t* codes, const uint8_t* exps, const int8_t* up_codes, const uint8_t* up_exps,
+                            int act, int64_t rows, int64_t cols, int dtype, void* out, int64_t ldout,
+                            hipStream_t stream);
+
+}  // namespace smat

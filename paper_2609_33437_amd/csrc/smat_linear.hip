@@ -1,0 +1,352 @@
+// Linear-layer products for gfx950 on the matrix cores: the layer itself, its data gradient and its
+// weight gradient, with their epilogues (see smat_linear.h for the operands).
+//
+// A block computes a tile of out.  Q's rows are the matrix instruction's rows and P's its columns, so a
+// lane ends with consecutive j of one i; Q's rows are dealt to the instructions so that two of them
+// leave a lane eight consecutive j (q_row), which is what the epilogues work on.
+#include "smat_linear_dev.h"
+#include "smat_launch.h"
+
+namespace smat {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------- operands in LDS
+// A stage of an operand holds 128 bytes of r for each of its B rows or columns, in 16-byte chunks.
+// Direct operands lie in rows of 8 chunks, transposed ones in rows of one r with B / (16 / bytes) chunks.
+// A fragment is what a matrix step over 64 bytes of r reads: for bf16 lane l holds r = 8 (l / 16) .. + 8 of
+// row l % 16 (one 32-deep instruction), for fp32 r = 4 (l / 16) .. + 4 (four 4-deep instructions, one
+// element each).
+//
+// Chunks are exchanged within their row (an exclusive or) so that the lanes that read together reach
+// different banks: by the row's number in P, and in Q, whose lanes read rows q_row, by the bits of the row
+// that differ between them.
+__device__ __forceinline__ constexpr int q_row(int r, int t) { return (r >> 2) * 8 + t * 4 + (r & 3); }
+template <bool Q>
+__device__ __forceinline__ int direct_swizzle(int row) {
+  return Q ? ((row & 3) | ((row >> 1) & 4)) : (row & 7);
+}
+// Transposed rows: lanes of one read lie in rows r = 8 g + (0..3), g < 4
+// (bf16), or r = 4 g (fp32).
+template <typename T, bool Q>
+__device__ __forceinline__ int transposed_swizzle(int r) {
+  if (sizeof(typename El<T>::Mem) == 4) return Q ? ((r >> 2) & 1) * 8 + ((r >> 3) & 1) : ((r >> 2) & 3) * 4;
+  return Q ? (r & 3) * 4 : ((r & 3) | ((r >> 1) & 4)) * 2;
+}
+
+template <typename T>
+struct Frag;
+template <>
+struct Frag<Bf16> {
+  bf16x8 v;
+};
+template <>
+struct Frag<float> {
+  f32x4 v;
+};
+__device__ __forceinline__ void mma(const Frag<Bf16>& q, const Frag<Bf16>& p, f32x4& c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.v, p.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(const Frag<float>& q, const Frag<float>& p, f32x4& c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(q.v[e], p.v[e], c, 0, 0, 0);
+}
+
+// The fragment of rows row0 .. row0 + 16 of P (of the pair's instruction t of rows row0 .. row0 + 32 of Q)
+// over chunks 4 kk .. 4 kk + 4 of r, from a stage of B rows.
+template <typename T, bool TRANS, bool Q, int B>
+__device__ __forceinline__ Frag<T> read_frag(const char* stage, int row0, int t, int kk) {
+  const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+  Frag<T> f;
+  if constexpr (!TRANS) {
+    const int row = row0 + (Q ? q_row(l, t) : l), c = (4 * kk + g) ^ direct_swizzle<Q>(row);
+    f.v = *reinterpret_cast<const decltype(f.v)*>(stage + row * 128 + c * 16);
+  } else if constexpr (sizeof(typename El<T>::Mem) == 2) {
+    // each 16 lanes read four rows of r, 8 bytes a lane, and the instruction transposes them
+    constexpr int kRow = B * 2;
+    const int col = row0 + (Q ? (l & 3) * 8 + t * 4 : (l & 3) * 4);
+    union {
+      i16x4 h[2];
+      bf16x8 v;
+    } u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = 32 * kk + 8 * g + 4 * h + (l >> 2);
+      const int c = (col >> 3) ^ transposed_swizzle<T, Q>(r);
+      const char* at = stage + r * kRow + c * 16 + (col & 4) * 2;
+      u.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) i16x4*)const_cast<char*>(at));
+    }
+    f.v = u.v;
+  } else {
+    constexpr int kRow = B * 4;
+    const int col = row0 + (Q ? q_row(l, t) : l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 16 * kk + 4 * g + e, c = (col >> 2) ^ transposed_swizzle<T, Q>(r);
+      f.v[e] = *reinterpret_cast<const float*>(stage + r * kRow + c * 16 + (col & 3) * 4);
+    }
+  }
+  return f;
+}
+
+// ---------------------------------------------------------------- the general tile
+// Any alignment, strides and sizes: chunks go through registers, loaded whole where they lie inside the
+// operand and element by element at its ends.
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const typename El<T>::Mem* p, int64_t valid) {
+  constexpr int kChunk = 16 / El<T>::kBytes;
+  if (valid >= kChunk) return *reinterpret_cast<const typename El<T>::vec_mem*>(p);
+  u32x4 x = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int e = 0; e < kChunk; ++e)
+    if (e < valid) {
+      if constexpr (El<T>::kBytes == 4)
+        x[e] = __float_as_uint(p[e]);
+      else
+        x[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
+    }
+  return x;
+}
+
+// A thread's chunks of a stage: rows row0 .. row0 + B of the operand (of `rows`), r from r0 (below `rend`).
+template <typename T, bool TRANS, bool Q, int B, int THREADS>
+struct Stage {
+  static constexpr int kChunk = 16 / El<T>::kBytes, kDeep = 128 / El<T>::kBytes, kCount = B * 8 / THREADS;
+  u32x4 x[kCount];
+  __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t row0, int64_t rows, int64_t r0,
+                                       int64_t rend) {
+    const auto* p = static_cast<const typename El<T>::Mem*>(base);
+#pragma unroll
+    for (int u = 0; u < kCount; ++u) {
+      const int id = (int)threadIdx.x + u * THREADS;
+      int64_t valid, at;
+      if constexpr (!TRANS) {
+        const int64_t row = row0 + id / 8, r = r0 + (id % 8) * kChunk;
+        valid = row < rows ? rend - r : 0;
+        at = row * ld + r;
+      } else {
+        const int64_t r = r0 + id / (B / kChunk), row = row0 + (id % (B / kChunk)) * kChunk;
+        valid = r < rend ? rows - row : 0;
+        at = r * ld + row;
+      }
+      x[u] = valid > 0 ? load_chunk<T>(p + at, valid) : u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  __device__ __forceinline__ void store(char* stage) const {
+#pragma unroll
+    for (int u = 0; u < kCount; ++u) {
+      const int id = (int)threadIdx.x + u * THREADS;
+      int at;
+      if constexpr (!TRANS) {
+        const int row = id / 8, c = (id % 8) ^ direct_swizzle<Q>(row);
+        at = row * 128 + c * 16;
+      } else {
+        const int r = id / (B / kChunk), c = (id % (B / kChunk)) ^ transposed_swizzle<T, Q>(r);
+        at = r * B * El<T>::kBytes + c * 16;
+      }
+      *reinterpret_cast<u32x4*>(stage + at) = x[u];
+    }
+  }
+};
+
+// The epilogue of a wave's accumulators, or their store as a partial sum.
+template <typename T, int EPI, int NI, int NJ>
+__device__ __forceinline__ void finish(const LinArgs& a, int64_t i0, int64_t j0, const f32x4 (&acc)[NI][NJ]) {
+  const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+#pragma unroll
+  for (int p = 0; p < NI; ++p) {
+#pragma unroll
+    for (int q = 0; q < NJ; q += 2) {
+      const int64_t i = i0 + 16 * p + l, j = j0 + 16 * q + 8 * g;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = acc[p][q][e];
+        v[4 + e] = acc[p][q + 1][e];
+      }
+      if (a.splits > 1) {
+        const int64_t ld = (a.j + 7) & ~(int64_t)7;
+        if (i < a.i && j < ld) El<float>::store8(a.partial + ((int64_t)blockIdx.y * a.i + i) * ld + j, v);
+      } else {
+        epilogue8<T, EPI, 16, 32>(a, i, j, v);
+      }
+    }
+  }
+}
+
+constexpr int kTileB = 128, kTileThreads = 256;
+
+template <typename T, bool PT, bool QT, int EPI>
+__global__ __launch_bounds__(kTileThreads, 2) void k_linear_tile(LinArgs a) {
+  constexpr int kDeep = 128 / El<T>::kBytes;
+  __shared__ alignas(16) char sp[kTileB * 128], sq[kTileB * 128];
+  const int64_t tiles_j = (a.j + kTileB - 1) / kTileB;
+  const int64_t ti = blockIdx.x / tiles_j, i0 = ti * kTileB, j0 = ((int64_t)blockIdx.x - ti * tiles_j) * kTileB;
+  const int wave = (int)threadIdx.x / 64, wi = (wave / 2) * 64, wj = (wave % 2) * 64;
+  // stages of r: those of prod[0], then those of prod[1]; this block's range of them
+  const int64_t n0 = (a.prod[0].r + kDeep - 1) / kDeep, n = n0 + (a.prod[1].r + kDeep - 1) / kDeep;
+  const int64_t first = n * blockIdx.y / a.splits, last = n * (blockIdx.y + 1) / a.splits;
+  f32x4 acc[4][4] = {};
+  Stage<T, PT, false, kTileB, kTileThreads> p;
+  Stage<T, QT, true, kTileB, kTileThreads> q;
+  const auto load = [&](int64_t s) {
+    const LinProduct& pr = s < n0 ? a.prod[0] : a.prod[1];
+    const int64_t r0 = (s < n0 ? s : s - n0) * kDeep;
+    p.load(pr.p, pr.ldp, i0, a.i, r0, pr.r);
+    q.load(pr.q, pr.ldq, j0, a.j, r0, pr.r);
+  };
+  if (first < last) load(first);
+  for (int64_t s = first; s < last; ++s) {
+    p.store(sp);
+    q.store(sq);
+    __syncthreads();
+    if (s + 1 < last) load(s + 1);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      Frag<T> fp[4], fq[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        fp[x] = read_frag<T, PT, false, kTileB>(sp, wi + 16 * x, 0, kk);
+        fq[x] = read_frag<T, QT, true, kTileB>(sq, wj + 32 * (x / 2), x % 2, kk);
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) mma(fq[y], fp[x], acc[x][y]);
+    }
+    __syncthreads();
+  }
+  finish<T, EPI>(a, i0 + wi, j0 + wj, acc);
+}
+
+// Joins the partial sums in their order and applies the epilogue: eight j a thread.
+template <typename T, int EPI>
+__global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
+  const int64_t eights = ((a.j + kCkptBlock - 1) / kCkptBlock) * 4, ld = (a.j + 7) & ~(int64_t)7;
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = t / eights, j = (t - i * eights) * 8;
+  float v[8] = {};
+  if (i < a.i && j < ld) {
+    for (int32_t s = 0; s < a.splits; ++s) {
+      float x[8];
+      El<float>::load8(a.partial + ((int64_t)s * a.i + i) * ld + j, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+  }
+  epilogue8<T, EPI, 1, 2>(a, i, j, v);
+}
+
+// ---------------------------------------------------------------- column sums
+// A block sums 64 columns over its share of the rows, four rows at a time; a second launch adds the
+// shares in their order.
+constexpr int kSumRows = 512;
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_column_sum(const typename El<T>::Mem* __restrict__ dy, int64_t ld, int64_t rows,
+                                                    int64_t cols, float* __restrict__ partial) {
+  __shared__ float s[4][64];
+  const int col = (int)threadIdx.x & 63, sub = (int)threadIdx.x >> 6;
+  const int64_t j = (int64_t)blockIdx.x * 64 + col, r0 = (int64_t)blockIdx.y * kSumRows;
+  const int64_t rend = r0 + kSumRows < rows ? r0 + kSumRows : rows;
+  float v = 0.f;
+  if (j < cols)
+    for (int64_t r = r0 + sub; r < rend; r += 4) v += El<T>::load(dy + r * ld + j);
+  s[sub][col] = v;
+  __syncthreads();
+  if (sub == 0 && j < cols) partial[(int64_t)blockIdx.y * cols + j] = (s[0][col] + s[1][col]) + (s[2][col] + s[3][col]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_column_join(const float* __restrict__ partial, int64_t cols, int32_t shares,
+                                                     typename El<T>::Mem* __restrict__ db) {
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= cols) return;
+  float v = 0.f;
+  for (int32_t s = 0; s < shares; ++s) v += partial[(int64_t)s * cols + j];
+  El<T>::store(db + j, v);
+}
+
+// ---------------------------------------------------------------- launches
+namespace {
+template <typename F>
+void with_element(int dtype, F&& fn) {
+  if (dtype == 1)
+    fn(Bf16());
+  else
+    fn(float());
+}
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int kComputeUnits = 256;
+
+// fn(element type, P transposed, Q transposed, epilogue) of an operation.
+template <typename F>
+void with_form(int dtype, LinEpilogue epi, F&& fn) {
+  with_element(dtype, [&](auto t) {
+    if (epi == kEpiLayer)
+      fn(t, std::false_type(), std::false_type(), std::integral_constant<int, kEpiLayer>());
+    else if (epi == kEpiDgrad)
+      fn(t, std::false_type(), std::true_type(), std::integral_constant<int, kEpiDgrad>());
+    else
+      fn(t, std::true_type(), std::true_type(), std::integral_constant<int, kEpiStore>());
+  });
+}
+}  // namespace
+
+LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue) {
+  const int64_t deep = dtype == 1 ? 64 : 32;
+  const int64_t stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
+  const int64_t tiles = div_up(a.i, kTileB) * div_up(a.j, kTileB);
+  // ranges of r until every compute unit has two blocks, each range at least four stages long
+  int64_t splits = tiles > 0 ? 2 * kComputeUnits / tiles : 1;
+  if (splits > stages / 4) splits = stages / 4;
+  LinPlan p;
+  p.splits = (int32_t)(splits < 1 ? 1 : splits);
+  p.workspace = p.splits > 1 ? (size_t)p.splits * (size_t)a.i * (size_t)(div_up(a.j, 8) * 8) * 4 : 0;
+  return p;
+}
+
+hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
+                         hipStream_t stream) {
+  LinArgs a = args;
+  a.splits = plan.splits;
+  a.partial = static_cast<float*>(workspace);
+  hipError_t e = hipSuccess;
+  with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
+    using T = decltype(t);
+    const dim3 grid((uint32_t)(div_up(a.i, kTileB) * div_up(a.j, kTileB)), (uint32_t)a.splits);
+    k_linear_tile<T, pt(), qt(), ep()><<<grid, dim3(kTileThreads), 0, stream>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess || a.splits <= 1) return;
+    k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
+    e = hipGetLastError();
+  });
+  return e;
+}
+
+size_t column_sum_workspace(int64_t rows, int64_t cols) { return (size_t)div_up(rows, kSumRows) * (size_t)cols * 4; }
+
+hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t cols, int dtype, void* db,
+                             void* workspace, hipStream_t stream) {
+  const int64_t shares = div_up(rows, kSumRows);
+  float* partial = static_cast<float*>(workspace);
+  hipError_t e = hipSuccess;
+  with_element(dtype, [&](auto t) {
+    using T = decltype(t);
+    using Mem = typename El<T>::Mem;
+    if (shares > 0) {
+      k_column_sum<T><<<dim3((uint32_t)div_up(cols, 64), (uint32_t)shares), dim3(256), 0, stream>>>(
+          static_cast<const Mem*>(dy), ld, rows, cols, partial);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return;
+    k_column_join<T><<<dim3((uint32_t)div_up(cols, 256)), dim3(256), 0, stream>>>(partial, cols, (int32_t)shares,
+                                                                                  static_cast<Mem*>(db));
+    e = hipGetLastError();
+  });
+  return e;
+}
+
+}  // namespace smat
