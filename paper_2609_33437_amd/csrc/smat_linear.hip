@@ -221,6 +221,214 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_linear_tile(LinArgs a) {
   finish<T, EPI>(a, i0 + wi, j0 + wj, acc);
 }
 
+// ---------------------------------------------------------------- the pipelined tile
+// bf16 operands whose rows start on 16-byte boundaries (and, where r runs along them, end on one) go
+// from global memory to LDS without passing registers.
+//
+// A tile of 256 x 256 is computed by eight waves; a stage (64 r) of each operand lies in LDS in two halves of
+// 128 rows or columns, twice, 128 KB in all.  A wave computes 64 x 32 of each of the four quadrants, one
+// quadrant a phase: it reads the half that the phase adds (at most eight fragments), starts the copy of one
+// half two stages ahead into the place that the previous phase emptied, and then issues the phase's 16 matrix
+// instructions.  Waves 4 to 7 run half a phase behind waves 0 to 3, so on each SIMD one wave's
+// matrix instructions cover the other's memory instructions.
+//
+// What orders the phases: a wave passes the barrier before its matrix instructions once its own reads of LDS have
+// returned and all but its last 12 copies (six halves) have landed.  So a half is read after a barrier
+// that every wave passed with its share of it landed, and a copy into a half starts after a barrier that every wave
+// passed with its reads of it returned.  Copies past the last stage deliver zeros to places that
+// nothing reads; they keep the count.
+constexpr int kFastB = 256, kFastThreads = 512, kFastHalf = 128, kHalfBytes = kFastHalf * 128;
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// A buffer descriptor of `bytes` bytes: offsets past them read as zeros.
+__device__ __forceinline__ i32x4 make_rsrc(const void* p, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+               __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF),
+               __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+}
+// 16 bytes a lane from `offset` of the buffer to LDS bytes lds + 16 lane.
+__device__ __forceinline__ void copy_to_lds(i32x4 rsrc, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds), "v"(offset), "s"(rsrc)
+               : "memory");
+}
+constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer
+
+// Copies of an operand's halves for one wave: rows (columns) row0 .. of the operand, `rows` of them in all.
+template <bool TRANS, bool Q>
+struct Copy {
+  const uint16_t* base;  // of the tile's first row or column
+  int64_t ld, left;      // left: rows or columns from the tile's first one
+  int64_t r;             // of the product
+  uint32_t off[2][2];    // [half][instruction]: this lane's byte offset at r0 = 0
+  uint32_t chunk[2];     // this lane's first r of the stage (direct)
+  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows) {
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    r = pr.r;
+    ld = Q ? pr.ldq : pr.ldp;
+    left = rows - row0;
+    base = static_cast<const uint16_t*>(Q ? pr.q : pr.p) + (TRANS ? row0 : row0 * ld);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (!TRANS) {
+          const int row = (wave * 2 + u) * 8 + lane / 8, c = (lane % 8) ^ direct_swizzle<Q>(row);
+          chunk[u] = (uint32_t)c * 8;
+          off[h][u] = h * kFastHalf + row < left ? (uint32_t)((h * kFastHalf + row) * ld * 2) + (uint32_t)c * 16 : kNowhere;
+        } else {
+          const int rr = (wave * 2 + u) * 4 + lane / 16, c = (lane % 16) ^ transposed_swizzle<Bf16, Q>(rr);
+          chunk[u] = (uint32_t)rr;
+          off[h][u] = (uint32_t)(rr * ld * 2) + (uint32_t)(h * kFastHalf * 2 + c * 16);
+        }
+      }
+  }
+  // half h of the stage that starts at r0, into LDS bytes `lds` ..
+  __device__ __forceinline__ void start(int h, int64_t r0, uint32_t lds) const {
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    i32x4 rsrc;
+    if constexpr (!TRANS) {
+      rsrc = make_rsrc(base + r0, 0x7FFFFFF0u);
+    } else {
+      const int64_t deep = r - r0 < 64 ? r - r0 : 64;
+      const int64_t bytes = deep > 0 ? (((deep - 1) * ld + left) * 2 + 15) & ~(int64_t)15 : 0;
+      rsrc = make_rsrc(base + r0 * ld, (uint32_t)bytes);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      uint32_t o = off[h][u];
+      if constexpr (!TRANS) o = r0 + chunk[u] < r ? o : kNowhere;
+      copy_to_lds(rsrc, o, lds + (wave * 2 + u) * 1024);
+    }
+  }
+};
+
+// Tile `b` of ti x tj in an order that keeps the tiles that run together close: consecutive blocks go to the
+// eight XCDs in turn, so each XCD takes one run of the order, in columns four tiles high.
+__device__ __forceinline__ void tile_place(uint32_t b, uint32_t ti, uint32_t tj, uint32_t& i, uint32_t& j) {
+  const uint32_t n = ti * tj, x = b & 7u, q = n >> 3, rem = n & 7u;
+  const uint32_t t = x * q + (x < rem ? x : rem) + (b >> 3);
+  constexpr uint32_t kHigh = 4;
+  const uint32_t band = t / (kHigh * tj), in = t - band * kHigh * tj, high = ti - band * kHigh < kHigh ? ti - band * kHigh : kHigh;
+  j = in / high;
+  i = band * kHigh + (in - j * high);
+}
+
+template <bool PT, bool QT, int EPI>
+__global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
+  using T = Bf16;
+  extern __shared__ char smem[];  // [stage parity][P half 0, P half 1, Q half 0, Q half 1]
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+  uint32_t ti, tj;
+  tile_place(blockIdx.x, (uint32_t)((a.i + kFastB - 1) / kFastB), (uint32_t)((a.j + kFastB - 1) / kFastB), ti, tj);
+  const int64_t i0 = (int64_t)ti * kFastB, j0 = (int64_t)tj * kFastB;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
+  const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
+  const int64_t first = n * blockIdx.y / a.splits, last = n * (blockIdx.y + 1) / a.splits;
+  Copy<PT, false> cp;
+  Copy<QT, true> cq;
+  const bool second = first >= n0;
+  cp.set(a.prod[second], i0, a.i);
+  cq.set(a.prod[second], j0, a.j);
+  int64_t at = second ? first - n0 : first, here = second ? n - n0 : n0;  // the next stage to copy, in its product
+  int64_t todo = last - first;                                            // stages still to copy
+  const auto half = [&](int which, int buf) {  // 0 Q0, 1 P0, 2 Q1, 3 P1 of the next stage to copy
+    const int64_t r0 = todo > 0 ? at * 64 : (int64_t)1 << 40;
+    const uint32_t to = lds0 + buf * 4 * kHalfBytes;
+    if (which == 0) cq.start(0, todo > 0 ? r0 : cq.r, to + 2 * kHalfBytes);
+    if (which == 1) cp.start(0, todo > 0 ? r0 : cp.r, to);
+    if (which == 2) cq.start(1, todo > 0 ? r0 : cq.r, to + 3 * kHalfBytes);
+    if (which == 3) cp.start(1, todo > 0 ? r0 : cp.r, to + kHalfBytes);
+  };
+  const auto advance = [&] {
+    --todo;
+    if (++at == here && todo > 0) {  // on to the second product
+      cp.set(a.prod[1], i0, a.i);
+      cq.set(a.prod[1], j0, a.j);
+      at = 0;
+      here = n - n0;
+    }
+  };
+  f32x4 acc[2][2][4][2] = {};
+  Frag<T> fp[4][2], fq[2][2][2];  // [tile][kk], [half][tile][kk]
+  const auto read_p = [&](int h, int buf) {
+    const char* s = smem + buf * 4 * kHalfBytes + h * kHalfBytes;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) fp[x][kk] = read_frag<T, PT, false, kFastHalf>(s, wi + 16 * x, 0, kk);
+  };
+  const auto read_q = [&](int h, int buf) {
+    const char* s = smem + buf * 4 * kHalfBytes + (2 + h) * kHalfBytes;
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) fq[h][y][kk] = read_frag<T, QT, true, kFastHalf>(s, wj, y, kk);
+  };
+  const auto multiply = [&](int hp, int hq) {
+    asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) mma(fq[hq][y][kk], fp[x][kk], acc[hp][hq][x][y]);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+  };
+  // stage in buffer `buf`: Q0 is in registers already
+  const auto stage = [&](int buf) {
+    read_p(0, buf);
+    half(0, buf);
+    multiply(0, 0);
+    read_q(1, buf);
+    half(1, buf);
+    multiply(0, 1);
+    read_p(1, buf);
+    half(2, buf);
+    multiply(1, 0);
+    read_q(0, buf ^ 1);
+    half(3, buf);
+    advance();
+    multiply(1, 1);
+  };
+  for (int buf = 0; buf < 2; ++buf) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) half(w, buf);
+    advance();
+  }
+  asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_q(0, 0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  if (wave >= 4) __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  for (int64_t s = first; s < last; s += 2) {
+    stage(0);
+    if (s + 1 < last) stage(1);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy outlives the block's LDS
+  if (wave < 4) __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int hp = 0; hp < 2; ++hp)
+#pragma unroll
+    for (int hq = 0; hq < 2; ++hq) finish<T, EPI>(a, i0 + hp * kFastHalf + wi, j0 + hq * kFastHalf + wj, acc[hp][hq]);
+}
+
 // Joins the partial sums in their order and applies the epilogue: eight j a thread.
 template <typename T, int EPI>
 __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
@@ -281,6 +489,16 @@ void with_element(int dtype, F&& fn) {
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int kComputeUnits = 256;
 
+// Whether the pipelined kernel can take an operand: 16-byte rows, and offsets of a tile below 2^31.
+bool operand_fits(const void* p, int64_t ld, int64_t r, bool trans) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && (trans || r % 8 == 0) && ld < ((int64_t)1 << 21);
+}
+bool fast_fits(const LinArgs& a, bool pt, bool qt) {
+  for (const LinProduct& pr : a.prod)
+    if (pr.r > 0 && !(operand_fits(pr.p, pr.ldp, pr.r, pt) && operand_fits(pr.q, pr.ldq, pr.r, qt))) return false;
+  return a.prod[0].r > 0;
+}
+
 // fn(element type, P transposed, Q transposed, epilogue) of an operation.
 template <typename F>
 void with_form(int dtype, LinEpilogue epi, F&& fn) {
@@ -316,8 +534,23 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
   hipError_t e = hipSuccess;
   with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
     using T = decltype(t);
-    const dim3 grid((uint32_t)(div_up(a.i, kTileB) * div_up(a.j, kTileB)), (uint32_t)a.splits);
-    k_linear_tile<T, pt(), qt(), ep()><<<grid, dim3(kTileThreads), 0, stream>>>(a);
+    if constexpr (std::is_same<T, Bf16>::value) {
+      if (fast_fits(a, pt(), qt())) {
+        const dim3 grid((uint32_t)(div_up(a.i, kFastB) * div_up(a.j, kFastB)), (uint32_t)a.splits);
+        auto* kernel = k_linear_fast<pt(), qt(), ep()>;
+        static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                              hipFuncAttributeMaxDynamicSharedMemorySize, 8 * kHalfBytes);
+        e = allowed;
+        if (e != hipSuccess) return;
+        kernel<<<grid, dim3(kFastThreads), 8 * kHalfBytes, stream>>>(a);
+      } else {
+        const dim3 grid((uint32_t)(div_up(a.i, kTileB) * div_up(a.j, kTileB)), (uint32_t)a.splits);
+        k_linear_tile<T, pt(), qt(), ep()><<<grid, dim3(kTileThreads), 0, stream>>>(a);
+      }
+    } else {
+      const dim3 grid((uint32_t)(div_up(a.i, kTileB) * div_up(a.j, kTileB)), (uint32_t)a.splits);
+      k_linear_tile<T, pt(), qt(), ep()><<<grid, dim3(kTileThreads), 0, stream>>>(a);
+    }
     e = hipGetLastError();
     if (e != hipSuccess || a.splits <= 1) return;
     k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
