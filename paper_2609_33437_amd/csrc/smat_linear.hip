@@ -151,29 +151,71 @@ struct Stage {
   }
 };
 
-// The epilogue of a wave's accumulators, or their store as a partial sum.
-template <typename T, int EPI, int NI, int NJ>
-__device__ __forceinline__ void finish(const LinArgs& a, int64_t i0, int64_t j0, const f32x4 (&acc)[NI][NJ]) {
-  const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+// The epilogue of a wave's accumulators, or their store as a partial sum: four eights of values a lane at a
+// time, chosen by a branch on a uniform number.  Unrolled over all 16 eights an epilogue with an activation is 100 KB
+// of instructions that every tile reads anew; one eight at a time, its branches, its loads of other matrices and its
+// stores wait for each other (12 us a tile of 256 x 256, against 6.5 us for four).
+// Instruction tile p of the accumulators lies ROWS(p) rows below i0, pair q COLS(q) columns right of j0.
+template <typename T, int EPI, bool WHOLE, int NI, int NJ, typename R, typename C>
+__device__ __forceinline__ void finish_eights(const LinArgs& a, int64_t i0, int64_t j0, const f32x4 (&acc)[NI][NJ],
+                                              R rows, C cols) {
+  constexpr int kEights = NI * NJ / 2, kAhead = WHOLE ? 4 : 1;
+  const bool partial = a.splits > 1;
+  const int64_t ld = (a.j + 7) & ~(int64_t)7;
+#pragma unroll 1
+  for (int first = 0; first < kEights; first += kAhead) {
+    const int which = __builtin_amdgcn_readfirstlane(first);
+    float v[kAhead][8];
+    Side<T, EPI> side[kAhead];
+    ColumnSide<T, EPI> column;
+    const int64_t j = j0 + cols(which / NI);
+    if (!partial) {
+      column_load<T, EPI>(a, j, column);
 #pragma unroll
-  for (int p = 0; p < NI; ++p) {
+      for (int n = 0; n < kAhead; ++n) side_load<T, EPI, WHOLE>(a, i0 + rows(which % NI + n), j, side[n]);
+    }
 #pragma unroll
-    for (int q = 0; q < NJ; q += 2) {
-      const int64_t i = i0 + 16 * p + l, j = j0 + 16 * q + 8 * g;
-      float v[8];
+    for (int c = 0; c < kEights; c += kAhead) {
+      if (which == c) {
+        asm volatile("" ::: "memory");  // a branch, not a select for each value
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = acc[p][q][e];
-        v[4 + e] = acc[p][q + 1][e];
+        for (int n = 0; n < kAhead; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[n][e] = acc[(c + n) % NI][c / NI * 2][e];
+            v[n][4 + e] = acc[(c + n) % NI][c / NI * 2 + 1][e];
+          }
       }
-      if (a.splits > 1) {
-        const int64_t ld = (a.j + 7) & ~(int64_t)7;
-        if (i < a.i && j < ld) El<float>::store8(a.partial + ((int64_t)blockIdx.y * a.i + i) * ld + j, v);
+    }
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      const int64_t i = i0 + rows(which % NI + n);
+      if (partial) {
+        if (WHOLE || (i < a.i && j < ld))
+          El<float>::store8(a.partial + ((int64_t)blockIdx.y * a.i + i) * ld + j, v[n]);
       } else {
-        epilogue8<T, EPI, 16, 32>(a, i, j, v);
+        epilogue8<T, EPI, 16, 32, WHOLE>(a, i, j, v[n], column, side[n]);
       }
     }
   }
+}
+
+// ROWS and COLS of the last tile and pair bound the wave's part of the tile.
+template <typename T, int EPI, int NI, int NJ, typename R, typename C>
+__device__ __forceinline__ void finish(const LinArgs& a, int64_t i0, int64_t j0, const f32x4 (&acc)[NI][NJ], R rows,
+                                       C cols) {
+  static_assert(NI % 4 == 0, "four eights of one pair at a time");
+  const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+  if (i0 + rows(NI - 1) + 16 <= a.i && j0 + cols(NJ / 2 - 1) + 32 <= a.j)
+    finish_eights<T, EPI, true>(a, i0 + l, j0 + 8 * g, acc, rows, cols);
+  else
+    finish_eights<T, EPI, false>(a, i0 + l, j0 + 8 * g, acc, rows, cols);
+}
+
+// The first of range s's stages where n < 2^27 stages are dealt to `splits` ranges.
+__device__ __forceinline__ int64_t split_start(int64_t n, uint32_t s, int32_t splits) {
+  const uint32_t each = (uint32_t)n / (uint32_t)splits, more = (uint32_t)n - each * (uint32_t)splits;
+  return (int64_t)(each * s + (s < more ? s : more));
 }
 
 constexpr int kTileB = 128, kTileThreads = 256;
@@ -187,7 +229,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_linear_tile(LinArgs a) {
   const int wave = (int)threadIdx.x / 64, wi = (wave / 2) * 64, wj = (wave % 2) * 64;
   // stages of r: those of prod[0], then those of prod[1]; this block's range of them
   const int64_t n0 = (a.prod[0].r + kDeep - 1) / kDeep, n = n0 + (a.prod[1].r + kDeep - 1) / kDeep;
-  const int64_t first = n * blockIdx.y / a.splits, last = n * (blockIdx.y + 1) / a.splits;
+  const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
   f32x4 acc[4][4] = {};
   Stage<T, PT, false, kTileB, kTileThreads> p;
   Stage<T, QT, true, kTileB, kTileThreads> q;
@@ -218,7 +260,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_linear_tile(LinArgs a) {
     }
     __syncthreads();
   }
-  finish<T, EPI>(a, i0 + wi, j0 + wj, acc);
+  finish<T, EPI>(
+      a, i0 + wi, j0 + wj, acc, [](int p) { return 16 * p; }, [](int q) { return 32 * q; });
 }
 
 // ---------------------------------------------------------------- the pipelined tile
@@ -226,14 +269,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_linear_tile(LinArgs a) {
 // from global memory to LDS without passing registers.
 //
 // A tile of 256 x 256 is computed by eight waves; a stage (64 r) of each operand lies in LDS in two halves of
-// 128 rows or columns, twice, 128 KB in all.  A wave computes 64 x 32 of each of the four quadrants, one
-// quadrant a phase: it reads the half that the phase adds (at most eight fragments), starts the copy of one
-// half two stages ahead into the place that the previous phase emptied, and then issues the phase's 16 matrix
-// instructions.  Waves 4 to 7 run half a phase behind waves 0 to 3, so on each SIMD one wave's
-// matrix instructions cover the other's memory instructions.
+// 128 rows or columns, twice, 128 KB in all.  A wave computes 64 x 32 of each of the four quadrants in two phases
+// a stage: the first reads P's first half and both halves of Q (16 fragments) and multiplies them, the second
+// reads P's second half.  Between its reads and its 32 matrix instructions a phase starts the copies
+// into the halves that the previous phase emptied.  Waves 4 to 7 run half a phase behind waves 0 to 3, so on
+// each SIMD one wave's matrix instructions cover the other's memory instructions.  (With one quadrant a phase the
+// barriers left the matrix cores idle for a quarter of the time.)
 //
 // What orders the phases: a wave passes the barrier before its matrix instructions once its own reads of LDS have
-// returned and all but its last 12 copies (six halves) have landed.  So a half is read after a barrier
+// returned and all but its last 8 copies (four halves) have landed.  So a half is read after a barrier
 // that every wave passed with its share of it landed, and a copy into a half starts after a barrier that every wave
 // passed with its reads of it returned.  Copies past the last stage deliver zeros to places that
 // nothing reads; they keep the count.
@@ -328,7 +372,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   const int64_t i0 = (int64_t)ti * kFastB, j0 = (int64_t)tj * kFastB;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
-  const int64_t first = n * blockIdx.y / a.splits, last = n * (blockIdx.y + 1) / a.splits;
+  const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
   Copy<PT, false> cp;
   Copy<QT, true> cq;
   const bool second = first >= n0;
@@ -336,13 +380,11 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   cq.set(a.prod[second], j0, a.j);
   int64_t at = second ? first - n0 : first, here = second ? n - n0 : n0;  // the next stage to copy, in its product
   int64_t todo = last - first;                                            // stages still to copy
-  const auto half = [&](int which, int buf) {  // 0 Q0, 1 P0, 2 Q1, 3 P1 of the next stage to copy
-    const int64_t r0 = todo > 0 ? at * 64 : (int64_t)1 << 40;
-    const uint32_t to = lds0 + buf * 4 * kHalfBytes;
-    if (which == 0) cq.start(0, todo > 0 ? r0 : cq.r, to + 2 * kHalfBytes);
-    if (which == 1) cp.start(0, todo > 0 ? r0 : cp.r, to);
-    if (which == 2) cq.start(1, todo > 0 ? r0 : cq.r, to + 3 * kHalfBytes);
-    if (which == 3) cp.start(1, todo > 0 ? r0 : cp.r, to + kHalfBytes);
+  const auto copy_p = [&](int h, int buf) {  // half h of the next stage to copy
+    cp.start(h, todo > 0 ? at * 64 : cp.r, lds0 + (buf * 4 + h) * kHalfBytes);
+  };
+  const auto copy_q = [&](int h, int buf) {
+    cq.start(h, todo > 0 ? at * 64 : cq.r, lds0 + (buf * 4 + 2 + h) * kHalfBytes);
   };
   const auto advance = [&] {
     --todo;
@@ -353,7 +395,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
       here = n - n0;
     }
   };
-  f32x4 acc[2][2][4][2] = {};
+  f32x4 acc[8][4] = {};  // [half of P, tile][half of Q, tile]
   Frag<T> fp[4][2], fq[2][2][2];  // [tile][kk], [half][tile][kk]
   const auto read_p = [&](int h, int buf) {
     const char* s = smem + buf * 4 * kHalfBytes + h * kHalfBytes;
@@ -369,8 +411,8 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) fq[h][y][kk] = read_frag<T, QT, true, kFastHalf>(s, wj, y, kk);
   };
-  const auto multiply = [&](int hp, int hq) {
-    asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
+  const auto multiply = [&](int hp) {
+    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
@@ -380,39 +422,36 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) mma(fq[hq][y][kk], fp[x][kk], acc[hp][hq][x][y]);
+        for (int y = 0; y < 4; ++y) mma(fq[y / 2][y % 2][kk], fp[x][kk], acc[4 * hp + x][y]);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
   };
-  // stage in buffer `buf`: Q0 is in registers already
+  // The stage in buffer `buf`.  The copies run ahead of it: P's second half by one stage, the others by two.
   const auto stage = [&](int buf) {
     read_p(0, buf);
-    half(0, buf);
-    multiply(0, 0);
+    read_q(0, buf);
     read_q(1, buf);
-    half(1, buf);
-    multiply(0, 1);
+    copy_p(1, buf ^ 1);
+    advance();
+    multiply(0);
     read_p(1, buf);
-    half(2, buf);
-    multiply(1, 0);
-    read_q(0, buf ^ 1);
-    half(3, buf);
-    advance();
-    multiply(1, 1);
+    copy_q(0, buf);
+    copy_q(1, buf);
+    copy_p(0, buf);
+    multiply(1);
   };
-  for (int buf = 0; buf < 2; ++buf) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) half(w, buf);
-    advance();
-  }
-  asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  read_q(0, 0);
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  copy_q(0, 0);
+  copy_q(1, 0);
+  copy_p(0, 0);
+  copy_p(1, 0);
+  advance();
+  copy_q(0, 1);
+  copy_q(1, 1);
+  copy_p(0, 1);
+  asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   if (wave >= 4) __builtin_amdgcn_s_barrier();
@@ -423,10 +462,9 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy outlives the block's LDS
   if (wave < 4) __builtin_amdgcn_s_barrier();
-#pragma unroll
-  for (int hp = 0; hp < 2; ++hp)
-#pragma unroll
-    for (int hq = 0; hq < 2; ++hq) finish<T, EPI>(a, i0 + hp * kFastHalf + wi, j0 + hq * kFastHalf + wj, acc[hp][hq]);
+  finish<T, EPI>(
+      a, i0 + wi, j0 + wj, acc, [](int p) { return p / 4 * kFastHalf + p % 4 * 16; },
+      [](int q) { return q * kFastHalf; });
 }
 
 // Joins the partial sums in their order and applies the epilogue: eight j a thread.
@@ -444,7 +482,11 @@ __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
       for (int e = 0; e < 8; ++e) v[e] += x[e];
     }
   }
-  epilogue8<T, EPI, 1, 2>(a, i, j, v);
+  Side<T, EPI> s;
+  ColumnSide<T, EPI> c;
+  column_load<T, EPI>(a, j, c);
+  side_load<T, EPI>(a, i, j, s);
+  epilogue8<T, EPI, 1, 2>(a, i, j, v, c, s);
 }
 
 // ---------------------------------------------------------------- column sums

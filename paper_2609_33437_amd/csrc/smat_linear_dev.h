@@ -108,7 +108,7 @@ __device__ __forceinline__ void logistic_both(float x, float& g, float& h) {
   g = act_rcp<T>(1.f + e);
   h = e * g;
 }
-// The standard normal's distribution function at z, and exp(-z^2 / 2).
+// The standard normal's distribution function at z, and exp(-z^2 / 2).  (The coefficients carry the half.)
 template <typename T>
 __device__ __forceinline__ float normal_cdf(float z, float& gauss) {
   if constexpr (sizeof(typename El<T>::Mem) == 4) {
@@ -118,11 +118,11 @@ __device__ __forceinline__ float normal_cdf(float z, float& gauss) {
     gauss = act_exp<T>(-0.5f * z * z);
     const float x = fabsf(z) * 0.70710678118654752440f;
     const float t = act_rcp<T>(__builtin_fmaf(0.3275911f, x, 1.f));
-    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-    p = __builtin_fmaf(p, t, 1.421413741f);
-    p = __builtin_fmaf(p, t, -0.284496736f);
-    p = __builtin_fmaf(p, t, 0.254829592f);
-    const float half_erfc = 0.5f * p * t * gauss;  // of |z| / sqrt(2)
+    float p = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+    p = __builtin_fmaf(p, t, 0.5f * 1.421413741f);
+    p = __builtin_fmaf(p, t, 0.5f * -0.284496736f);
+    p = __builtin_fmaf(p, t, 0.5f * 0.254829592f);
+    const float half_erfc = p * t * gauss;  // of |z| / sqrt(2)
     return z < 0.f ? half_erfc : 1.f - half_erfc;
   }
 }
@@ -211,26 +211,119 @@ __device__ __forceinline__ uint32_t block_max(const float v[8]) {
 }
 
 // ---------------------------------------------------------------- epilogues
-// The epilogue on out[i][j0 .. j0 + 8), j0 a multiple of 8; the four lanes of a checkpoint block differ
-// in lane bits A and B.  Every lane of the wave calls it (i or j0 may lie outside).
-template <typename T, int EPI, int A, int B>
-__device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j0, float v[8]) {
-  using Mem = typename El<T>::Mem;
-  const bool row = i < a.i;
-  const int64_t valid = row ? a.j - j0 : 0;
-  if constexpr (EPI == kEpiLayer) {
-    if (a.bias && valid > 0) {
-      float b[8];
-      load_row8<T>(static_cast<const Mem*>(a.bias) + j0, valid, b);
+// What an epilogue reads beside its eight values, as it lies in memory.  Loads of whole eights can be
+// issued ahead of their use (side_load); at a row's end the epilogue loads what there is itself.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<Bf16> {
+  u32x4 x;
+  __device__ __forceinline__ void load(const uint16_t* p) { x = *reinterpret_cast<const El<Bf16>::vec_mem*>(p); }
+  __device__ __forceinline__ void get(float v[8]) const {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += b[e];
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __uint_as_float(x[e] << 16);
+      v[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
+    }
+  }
+};
+template <>
+struct Raw8<float> {
+  f32x4 x[2];
+  __device__ __forceinline__ void load(const float* p) {
+    x[0] = *reinterpret_cast<const f32x4_mem*>(p);
+    x[1] = *reinterpret_cast<const f32x4_mem*>(p + 4);
+  }
+  __device__ __forceinline__ void get(float v[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x[e / 4][e % 4];
+  }
+};
+template <typename T, int EPI>
+struct Side {};
+// The same of a column: it serves every row.
+template <typename T, int EPI>
+struct ColumnSide {};
+template <typename T>
+struct ColumnSide<T, kEpiLayer> {
+  Raw8<T> bias;
+};
+template <typename T>
+struct Side<T, kEpiLayer> {
+  Raw8<T> mul, residual;
+};
+template <typename T>
+struct Side<T, kEpiDgrad> {
+  u32x2 z, up;
+  uint32_t z_byte, up_byte;
+};
+
+__device__ __forceinline__ int64_t row_blocks(const LinArgs& a) { return (a.j + kCkptBlock - 1) / kCkptBlock; }
+
+// The loads of out[i][j0 .. j0 + 8); nothing where it is not whole (a checkpoint's rows are: they are padded).
+// WHOLE: the caller knows that all eight lie inside, here and below.
+template <typename T, int EPI, bool WHOLE = false>
+__device__ __forceinline__ void side_load(const LinArgs& a, int64_t i, int64_t j0, Side<T, EPI>& s) {
+  using Mem = typename El<T>::Mem;
+  if constexpr (EPI == kEpiLayer) {
+    if (WHOLE || (i < a.i && j0 + 8 <= a.j)) {
+      if (a.mul) s.mul.load(static_cast<const Mem*>(a.mul) + i * a.ldmul + j0);
+      if (a.residual) s.residual.load(static_cast<const Mem*>(a.residual) + i * a.ldres + j0);
+    }
+  }
+  if constexpr (EPI == kEpiDgrad) {
+    if (a.z_codes && (WHOLE || (i < a.i && j0 < a.j))) {
+      const int64_t nb = row_blocks(a), at = i * nb * kCkptBlock + j0, block = i * nb + j0 / kCkptBlock;
+      s.z = *reinterpret_cast<const u32x2*>(a.z_codes + at);
+      s.z_byte = a.z_exps[block];
+      if (a.up_codes) {
+        s.up = *reinterpret_cast<const u32x2*>(a.up_codes + at);
+        s.up_byte = a.up_exps[block];
+      }
+    }
+  }
+}
+
+template <typename T, int EPI>
+__device__ __forceinline__ void column_load(const LinArgs& a, int64_t j0, ColumnSide<T, EPI>& s) {
+  if constexpr (EPI == kEpiLayer) {
+    if (a.bias && j0 + 8 <= a.j) s.bias.load(static_cast<const typename El<T>::Mem*>(a.bias) + j0);
+  }
+}
+
+// One side matrix's values: loaded ahead, or at a row's end element by element.
+template <typename T>
+__device__ __forceinline__ void side_values(const Raw8<T>& raw, const void* row, int64_t j0, int64_t valid, float u[8]) {
+  raw.get(u);
+  if (valid < 8) {
+    const auto* p = static_cast<const typename El<T>::Mem*>(row) + j0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = e < valid ? El<T>::load(p + e) : 0.f;
+  }
+}
+
+// The epilogue on out[i][j0 .. j0 + 8), j0 a multiple of 8, with what column_load and side_load loaded for it;
+// the four lanes of a checkpoint block differ in lane bits A and B.  Every lane of the wave calls it (i or j0 may
+// lie outside).
+template <typename T, int EPI, int A, int B, bool WHOLE = false>
+__device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j0, float v[8], const ColumnSide<T, EPI>& c,
+                                          const Side<T, EPI>& s) {
+  using Mem = typename El<T>::Mem;
+  const bool row = WHOLE || i < a.i;
+  const int64_t valid = WHOLE ? 8 : row ? a.j - j0 : 0;
+  if constexpr (EPI == kEpiLayer) {
+    float u[8];
+    if (a.bias && valid > 0) {
+      side_values<T>(c.bias, a.bias, j0, valid, u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += u[e];
     }
     if (a.codes) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = e < valid ? v[e] : 0.f;
       const uint32_t byte = ckpt_byte(block_max<A, B>(v));
-      const int64_t nb = (a.j + kCkptBlock - 1) / kCkptBlock;
-      if (row && j0 < nb * kCkptBlock) {
+      const int64_t nb = row_blocks(a);
+      if (WHOLE || (row && j0 < nb * kCkptBlock)) {
         *reinterpret_cast<u32x2*>(a.codes + i * nb * kCkptBlock + j0) = ckpt_pack8(v, byte);
         if (j0 % kCkptBlock == 0) a.exps[i * nb + j0 / kCkptBlock] = (uint8_t)byte;
       }
@@ -241,14 +334,12 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
       for (int e = 0; e < 8; ++e) v[e] = act_value<T>(v[e], a.act);
     }
     if (a.mul) {
-      float u[8];
-      load_row8<T>(static_cast<const Mem*>(a.mul) + i * a.ldmul + j0, valid, u);
+      side_values<T>(s.mul, static_cast<const Mem*>(a.mul) + i * a.ldmul, j0, valid, u);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= u[e];
     }
     if (a.residual) {
-      float u[8];
-      load_row8<T>(static_cast<const Mem*>(a.residual) + i * a.ldres + j0, valid, u);
+      side_values<T>(s.residual, static_cast<const Mem*>(a.residual) + i * a.ldres, j0, valid, u);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += u[e];
     }
@@ -256,13 +347,11 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
   if (valid <= 0) return;
   if constexpr (EPI == kEpiDgrad) {
     if (a.z_codes) {
-      const int64_t nb = (a.j + kCkptBlock - 1) / kCkptBlock;
-      const int64_t at = i * nb * kCkptBlock + j0, block = i * nb + j0 / kCkptBlock;
-      float z[8], u[8];
-      ckpt_unpack8(*reinterpret_cast<const u32x2*>(a.z_codes + at), a.z_exps[block], z);
+      float z[8];
+      ckpt_unpack8(s.z, s.z_byte, z);
       if (a.up_codes) {
-        float w[8];
-        ckpt_unpack8(*reinterpret_cast<const u32x2*>(a.up_codes + at), a.up_exps[block], u);
+        float u[8], w[8];
+        ckpt_unpack8(s.up, s.up_byte, u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float value, slope;
