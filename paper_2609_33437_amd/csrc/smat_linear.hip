@@ -29,10 +29,11 @@ __device__ __forceinline__ int direct_swizzle(int row) {
 }
 // Transposed rows: lanes of one read lie in rows r = 8 g + (0..3), g < 4
 // (bf16), or r = 4 g (fp32).
-template <typename T, bool Q>
+template <typename T, bool Q, int B>
 __device__ __forceinline__ int transposed_swizzle(int r) {
-  if (sizeof(typename El<T>::Mem) == 4) return Q ? ((r >> 2) & 1) * 8 + ((r >> 3) & 1) : ((r >> 2) & 3) * 4;
-  return Q ? (r & 3) * 4 : ((r & 3) | ((r >> 1) & 4)) * 2;
+  constexpr int kChunks = B * El<T>::kBytes / 16;
+  if (El<T>::kBytes == 4) return (Q ? ((r >> 2) & 1) * 8 + ((r >> 3) & 1) : ((r >> 2) & 3) * 4) & (kChunks - 1);
+  return (Q ? (r & 3) * 4 : ((r & 3) | ((r >> 1) & 4)) * 2) & (kChunks - 1);
 }
 
 template <typename T>
@@ -73,7 +74,7 @@ __device__ __forceinline__ Frag<T> read_frag(const char* stage, int row0, int t,
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int r = 32 * kk + 8 * g + 4 * h + (l >> 2);
-      const int c = (col >> 3) ^ transposed_swizzle<T, Q>(r);
+      const int c = (col >> 3) ^ transposed_swizzle<T, Q, B>(r);
       const char* at = stage + r * kRow + c * 16 + (col & 4) * 2;
       u.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (__attribute__((address_space(3))) i16x4*)const_cast<char*>(at));
@@ -84,7 +85,7 @@ __device__ __forceinline__ Frag<T> read_frag(const char* stage, int row0, int t,
     const int col = row0 + (Q ? q_row(l, t) : l);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int r = 16 * kk + 4 * g + e, c = (col >> 2) ^ transposed_swizzle<T, Q>(r);
+      const int r = 16 * kk + 4 * g + e, c = (col >> 2) ^ transposed_swizzle<T, Q, B>(r);
       f.v[e] = *reinterpret_cast<const float*>(stage + r * kRow + c * 16 + (col & 3) * 4);
     }
   }
@@ -143,7 +144,7 @@ struct Stage {
         const int row = id / 8, c = (id % 8) ^ direct_swizzle<Q>(row);
         at = row * 128 + c * 16;
       } else {
-        const int r = id / (B / kChunk), c = (id % (B / kChunk)) ^ transposed_swizzle<T, Q>(r);
+        const int r = id / (B / kChunk), c = (id % (B / kChunk)) ^ transposed_swizzle<T, Q, B>(r);
         at = r * B * El<T>::kBytes + c * 16;
       }
       *reinterpret_cast<u32x4*>(stage + at) = x[u];
@@ -302,52 +303,73 @@ __device__ __forceinline__ void copy_to_lds(i32x4 rsrc, uint32_t offset, uint32_
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer
 
-// Copies of an operand's halves for one wave: rows (columns) row0 .. of the operand, `rows` of them in all.
-template <bool TRANS, bool Q>
+// Copies of NI KB of a stage by one of the waves that share it: rows (columns) row0 .. row0 + B of the operand, `rows`
+// of them in all.
+template <bool TRANS, bool Q, int B, int NI>
 struct Copy {
-  const uint16_t* base;  // of the tile's first row or column
-  int64_t ld, left;      // left: rows or columns from the tile's first one
+  const uint16_t* base;  // of the first row or column
+  int64_t ld, left;      // left: rows or columns from the first one
   int64_t r;             // of the product
-  uint32_t off[2][2];    // [half][instruction]: this lane's byte offset at r0 = 0
-  uint32_t chunk[2];     // this lane's first r of the stage (direct)
-  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows) {
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  uint32_t off[NI];      // this lane's byte offset at r0 = 0
+  uint32_t chunk[NI];    // this lane's first r of the stage (direct)
+  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows, int wave) {
+    const int lane = (int)threadIdx.x & 63;
     r = pr.r;
     ld = Q ? pr.ldq : pr.ldp;
     left = rows - row0;
     base = static_cast<const uint16_t*>(Q ? pr.q : pr.p) + (TRANS ? row0 : row0 * ld);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if constexpr (!TRANS) {
-          const int row = (wave * 2 + u) * 8 + lane / 8, c = (lane % 8) ^ direct_swizzle<Q>(row);
-          chunk[u] = (uint32_t)c * 8;
-          off[h][u] = h * kFastHalf + row < left ? (uint32_t)((h * kFastHalf + row) * ld * 2) + (uint32_t)c * 16 : kNowhere;
-        } else {
-          const int rr = (wave * 2 + u) * 4 + lane / 16, c = (lane % 16) ^ transposed_swizzle<Bf16, Q>(rr);
-          chunk[u] = (uint32_t)rr;
-          off[h][u] = (uint32_t)(rr * ld * 2) + (uint32_t)(h * kFastHalf * 2 + c * 16);
-        }
+    for (int u = 0; u < NI; ++u) {
+      if constexpr (!TRANS) {
+        const int row = (wave * NI + u) * 8 + lane / 8, c = (lane % 8) ^ direct_swizzle<Q>(row);
+        chunk[u] = (uint32_t)c * 8;
+        off[u] = row < left ? (uint32_t)(row * ld * 2) + (uint32_t)c * 16 : kNowhere;
+      } else {
+        constexpr int kChunks = B / 8;
+        const int rr = (wave * NI + u) * (64 / kChunks) + lane / kChunks;
+        const int c = (lane % kChunks) ^ transposed_swizzle<Bf16, Q, B>(rr);
+        off[u] = (uint32_t)(rr * ld * 2) + (uint32_t)(c * 16);
       }
+    }
   }
-  // half h of the stage that starts at r0, into LDS bytes `lds` ..
-  __device__ __forceinline__ void start(int h, int64_t r0, uint32_t lds) const {
-    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  // the stage that starts at r0, into LDS bytes `lds` .. of this wave's first KB
+  __device__ __forceinline__ void start(int64_t r0, uint32_t lds) const {
     i32x4 rsrc;
     if constexpr (!TRANS) {
       rsrc = make_rsrc(base + r0, 0x7FFFFFF0u);
     } else {
       const int64_t deep = r - r0 < 64 ? r - r0 : 64;
-      const int64_t bytes = deep > 0 ? (((deep - 1) * ld + left) * 2 + 15) & ~(int64_t)15 : 0;
-      rsrc = make_rsrc(base + r0 * ld, (uint32_t)bytes);
+      const int64_t bytes = deep > 0 && left > 0 ? (((deep - 1) * ld + left) * 2 + 15) & ~(int64_t)15 : 0;
+      rsrc = make_rsrc(base + r0 * ld, (uint32_t)(bytes < 0x7FFFFFF0 ? bytes : 0x7FFFFFF0));
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      uint32_t o = off[h][u];
+    for (int u = 0; u < NI; ++u) {
+      uint32_t o = off[u];
       if constexpr (!TRANS) o = r0 + chunk[u] < r ? o : kNowhere;
-      copy_to_lds(rsrc, o, lds + (wave * 2 + u) * 1024);
+      copy_to_lds(rsrc, o, lds + u * 1024);
     }
+  }
+};
+
+// The stages of r that a wave copies, in the order of the sum: those of prod[0], then those of prod[1].
+struct Stages {
+  int64_t at, here, todo, n0, n;  // next stage in its product, stages of that product, stages left, stages of prod[0], of both
+  __device__ __forceinline__ void set(const LinArgs& a, int64_t first, int64_t last, int64_t n0_, int64_t n_) {
+    n0 = n0_;
+    n = n_;
+    at = first >= n0 ? first - n0 : first;
+    here = first >= n0 ? n - n0 : n0;
+    todo = last - first;
+  }
+  // the next stage's first r; a place past the end once there is none
+  __device__ __forceinline__ int64_t r0(int64_t r) const { return todo > 0 ? at * 64 : r; }
+  // whether the next stage is the first of prod[1]
+  __device__ __forceinline__ bool advance() {
+    --todo;
+    if (++at != here || todo <= 0) return false;
+    at = 0;
+    here = n - n0;
+    return true;
   }
 };
 
@@ -373,27 +395,27 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
   const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
-  Copy<PT, false> cp;
-  Copy<QT, true> cq;
-  const bool second = first >= n0;
-  cp.set(a.prod[second], i0, a.i);
-  cq.set(a.prod[second], j0, a.j);
-  int64_t at = second ? first - n0 : first, here = second ? n - n0 : n0;  // the next stage to copy, in its product
-  int64_t todo = last - first;                                            // stages still to copy
+  Copy<PT, false, kFastHalf, 2> cp[2];
+  Copy<QT, true, kFastHalf, 2> cq[2];
+  const auto set = [&](const LinProduct& pr) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      cp[h].set(pr, i0 + h * kFastHalf, a.i, wave);
+      cq[h].set(pr, j0 + h * kFastHalf, a.j, wave);
+    }
+  };
+  set(a.prod[first >= n0]);
+  Stages todo;
+  todo.set(a, first, last, n0, n);
+  const uint32_t mine = lds0 + (uint32_t)wave * 2048;
   const auto copy_p = [&](int h, int buf) {  // half h of the next stage to copy
-    cp.start(h, todo > 0 ? at * 64 : cp.r, lds0 + (buf * 4 + h) * kHalfBytes);
+    cp[h].start(todo.r0(cp[h].r), mine + (buf * 4 + h) * kHalfBytes);
   };
   const auto copy_q = [&](int h, int buf) {
-    cq.start(h, todo > 0 ? at * 64 : cq.r, lds0 + (buf * 4 + 2 + h) * kHalfBytes);
+    cq[h].start(todo.r0(cq[h].r), mine + (buf * 4 + 2 + h) * kHalfBytes);
   };
   const auto advance = [&] {
-    --todo;
-    if (++at == here && todo > 0) {  // on to the second product
-      cp.set(a.prod[1], i0, a.i);
-      cq.set(a.prod[1], j0, a.j);
-      at = 0;
-      here = n - n0;
-    }
+    if (todo.advance()) set(a.prod[1]);
   };
   f32x4 acc[8][4] = {};  // [half of P, tile][half of Q, tile]
   Frag<T> fp[4][2], fq[2][2][2];  // [tile][kk], [half][tile][kk]
@@ -465,6 +487,160 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   finish<T, EPI>(
       a, i0 + wi, j0 + wj, acc, [](int p) { return p / 4 * kFastHalf + p % 4 * 16; },
       [](int q) { return q * kFastHalf; });
+}
+
+// ---------------------------------------------------------------- smaller tiles
+// The same copies and fragments for products that would leave the 256 x 256 tile's compute units idle.  A block holds
+// G groups of WI x WJ waves.  A group computes the whole tile, TI x TJ a wave, over its own share of the
+// stages of r; where G > 1 the groups' sums are added through LDS.  So a product with few tiles and a long r
+// still keeps several waves' copies in flight on each compute unit, and no launch joins them.
+//
+// A group's stages lie in NBUF buffers.  While a wave multiplies the fragments of one stage it reads those of the
+// next from LDS; a buffer is filled again once every wave of the group has read it.
+constexpr uint32_t kMaxCopies = 63;  // what a wait can leave in flight
+
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N <= (int)kMaxCopies, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+template <int TI_, int TJ_, int WI_, int WJ_, int G_, int NBUF_>
+struct GroupShape {
+  static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, G = G_, NBUF = NBUF_;
+  static constexpr int kI = TI * WI, kJ = TJ * WJ, kThreads = 64 * WI * WJ * G;
+  static constexpr int kStage = (kI + kJ) * 128;             // bytes
+  static constexpr int kSumLd = kJ + 4;                      // floats a row of a group's sums (rows 16 bytes apart in banks)
+  static constexpr int kSums = G > 1 ? G * kI * kSumLd * 4 : 0;
+  static constexpr int kLds = G * NBUF * kStage > kSums ? G * NBUF * kStage : kSums;
+  static constexpr int kResident = 160 * 1024 / kLds;        // blocks that fit a compute unit's LDS
+  static constexpr int kSimdWaves = kResident * WI * WJ * G / 4;
+};
+
+template <bool PT, bool QT, int EPI, typename S>
+__global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(LinArgs a) {
+  using T = Bf16;
+  constexpr int kWaves = S::WI * S::WJ, kNp = S::kI / 8 / kWaves, kNq = S::kJ / 8 / kWaves, kXi = S::TI / 16, kXj = S::TJ / 16;
+  static_assert(kNp * 8 * kWaves == S::kI && kNq * 8 * kWaves == S::kJ, "whole KB a wave");
+  extern __shared__ char smem[];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), group = wave / kWaves, w = wave % kWaves;
+  uint32_t ti, tj;
+  tile_place(blockIdx.x, (uint32_t)((a.i + S::kI - 1) / S::kI), (uint32_t)((a.j + S::kJ - 1) / S::kJ), ti, tj);
+  const int64_t i0 = (int64_t)ti * S::kI, j0 = (int64_t)tj * S::kJ;
+  const int wi = w / S::WJ * S::TI, wj = w % S::WJ * S::TJ;
+  const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
+  const uint32_t share = blockIdx.y * S::G + (uint32_t)group;
+  const int64_t first = split_start(n, share, a.splits * S::G), last = split_start(n, share + 1, a.splits * S::G);
+  // every group of a block takes part in the same number of steps, so that barriers meet (shares differ by one stage)
+  const int64_t steps = (n + a.splits * S::G - 1) / (a.splits * S::G);
+  Copy<PT, false, S::kI, kNp> cp;
+  Copy<QT, true, S::kJ, kNq> cq;
+  const auto set = [&](const LinProduct& pr) {
+    cp.set(pr, i0, a.i, w);
+    cq.set(pr, j0, a.j, w);
+  };
+  set(a.prod[first >= n0 && a.prod[1].r > 0]);
+  Stages todo;
+  todo.set(a, first, last, n0, n);
+  char* const mine = smem + group * S::NBUF * S::kStage;
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_char*)mine;
+  const auto copy = [&](int buf) {
+    cp.start(todo.r0(cp.r), lds + (uint32_t)(buf * S::kStage + w * kNp * 1024));
+    cq.start(todo.r0(cq.r), lds + (uint32_t)(buf * S::kStage + S::kI * 128 + w * kNq * 1024));
+    if (todo.advance()) set(a.prod[1]);
+  };
+  f32x4 acc[kXi][kXj] = {};
+  Frag<T> fp[2][kXi][2], fq[2][kXj][2];  // [parity][tile][kk]
+  const auto read = [&](int set_, int buf) {
+    const char* s = mine + buf * S::kStage;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+      for (int x = 0; x < kXi; ++x) fp[set_][x][kk] = read_frag<T, PT, false, S::kI>(s, wi + 16 * x, 0, kk);
+#pragma unroll
+      for (int y = 0; y < kXj; ++y)
+        fq[set_][y][kk] = read_frag<T, QT, true, S::kJ>(s + S::kI * 128, wj + 32 * (y / 2), y % 2, kk);
+    }
+  };
+  const auto meet = [&] {
+    if (kWaves > 1) {
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::: "memory");
+    }
+  };
+  int buf = 0;
+  // the fragments `set_` of this step have been asked for: wait for them and for the next stage, fill their
+  // buffer again, ask for the next fragments, multiply
+  const auto step = [&](int set_) {
+    wait_copies<(S::NBUF - 2) * (kNp + kNq)>();
+    meet();
+    copy(buf);
+    buf = buf + 1 == S::NBUF ? 0 : buf + 1;
+    read(set_ ^ 1, buf);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int x = 0; x < kXi; ++x)
+#pragma unroll
+        for (int y = 0; y < kXj; ++y) mma(fq[set_][y][kk], fp[set_][x][kk], acc[x][y]);
+  };
+#pragma unroll
+  for (int b = 0; b < S::NBUF; ++b) copy(b);
+  wait_copies<(S::NBUF - 1) * (kNp + kNq)>();
+  meet();
+  read(0, 0);
+  for (int64_t s = 0; s < steps; s += 2) {
+    step(0);
+    if (s + 1 < steps) step(1);
+  }
+  wait_copies<0>();  // no copy outlives the block's LDS, or lands on the sums
+  if constexpr (S::G == 1) {
+    finish<T, EPI>(
+        a, i0 + wi, j0 + wj, acc, [](int p) { return 16 * p; }, [](int q) { return 32 * q; });
+  } else {
+    // the groups' sums side by side, added in the groups' order
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(smem);
+    const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+#pragma unroll
+    for (int x = 0; x < kXi; ++x)
+#pragma unroll
+      for (int y = 0; y < kXj; ++y) {
+        const int i = wi + 16 * x + l, j = wj + 32 * (y / 2) + 8 * g + 4 * (y % 2);
+        *reinterpret_cast<f32x4*>(sums + (group * S::kI + i) * S::kSumLd + j) = acc[x][y];
+      }
+    __syncthreads();
+    constexpr int kEights = S::kI * S::kJ / 8;
+    static_assert(kEights % 64 == 0, "whole waves");
+#pragma unroll 1
+    for (int t = (int)threadIdx.x; t < kEights; t += S::kThreads) {
+      const int i = t / (S::kJ / 8), j = t % (S::kJ / 8) * 8;
+      const int64_t gi = i0 + i, gj = j0 + j;
+      Side<T, EPI> side;
+      ColumnSide<T, EPI> column;
+      if (a.splits == 1) {
+        column_load<T, EPI>(a, gj, column);
+        side_load<T, EPI>(a, gi, gj, side);
+      }
+      float v[8] = {};
+#pragma unroll
+      for (int k = 0; k < S::G; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(sums + (k * S::kI + i) * S::kSumLd + j + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * h + e] += x[e];
+        }
+      if (a.splits > 1) {
+        const int64_t ld = (a.j + 7) & ~(int64_t)7;
+        if (gi < a.i && gj < ld) El<float>::store8(a.partial + ((int64_t)blockIdx.y * a.i + gi) * ld + gj, v);
+      } else {
+        epilogue8<T, EPI, 1, 2>(a, gi, gj, v, column, side);
+      }
+    }
+  }
 }
 
 // Joins the partial sums in their order and applies the epilogue: eight j a thread.
@@ -555,18 +731,60 @@ void with_form(int dtype, LinEpilogue epi, F&& fn) {
 }
 }  // namespace
 
-LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue) {
+namespace {
+// The tiles a product can be computed with.
+enum TileForm : int32_t { kGeneral = 0, kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4 };
+using MiddleShape = GroupShape<64, 64, 2, 2, 1, 2>;  // 128 x 128, two blocks a compute unit
+using SmallShape = GroupShape<64, 64, 1, 1, 4, 2>;   // 64 x 64, r in four
+using TinyShape = GroupShape<32, 32, 1, 1, 8, 2>;    // 32 x 32, r in eight
+
+// What the choice of a tile goes by: the tile, blocks that run together on a compute unit, stages of r that a block
+// takes together (its groups), and microseconds of a stage with every unit busy and of the rest of a block.
+struct FormCost {
+  int32_t form, i, j, resident, groups;
+  double stage, rest;
+};
+}  // namespace
+
+LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int64_t deep = dtype == 1 ? 64 : 32;
   const int64_t stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
-  const int64_t tiles = div_up(a.i, kTileB) * div_up(a.j, kTileB);
-  // ranges of r until every compute unit has two blocks, each range at least four stages long
-  int64_t splits = tiles > 0 ? 2 * kComputeUnits / tiles : 1;
-  if (splits > stages / 4) splits = stages / 4;
-  LinPlan p;
-  p.splits = (int32_t)(splits < 1 ? 1 : splits);
-  p.workspace = p.splits > 1 ? (size_t)p.splits * (size_t)a.i * (size_t)(div_up(a.j, 8) * 8) * 4 : 0;
-  return p;
+  const bool pt = epi == kEpiStore, qt = epi != kEpiLayer;
+  static const FormCost general[] = {{kGeneral, kTileB, kTileB, 2, 1, 1.6, 8.0}};
+  static const FormCost pipelined[] = {{kFast, kFastB, kFastB, 1, 1, 1.40, 11.0},
+                                       {kMiddle, MiddleShape::kI, MiddleShape::kJ, 2, 1, 1.1, 8.0},
+                                       {kSmall, SmallShape::kI, SmallShape::kJ, 1, 4, 0.9, 6.0},
+                                       {kTiny, TinyShape::kI, TinyShape::kJ, 1, 8, 0.7, 5.0}};
+  const bool fits = dtype == 1 && fast_fits(a, pt, qt);
+  LinPlan best{};
+  double least = 1e30;
+  for (int c = 0; c < (fits ? 4 : 1); ++c) {
+    const FormCost& f = fits ? pipelined[c] : general[c];
+    const int64_t tiles = div_up(a.i, f.i) * div_up(a.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
+    for (int64_t splits = 1; splits <= 16 && (splits == 1 || splits * f.groups * 2 <= stages); ++splits) {
+      const double rounds = (double)div_up(tiles * splits, slots);
+      double us = rounds * (f.rest + (double)div_up(stages, splits * f.groups) * f.stage);
+      // the partial sums are written and read, and another launch joins them
+      if (splits > 1) us += 5.0 + (double)splits * (double)a.i * (double)a.j * 8.0 / 4e6;
+      if (us < least) {
+        least = us;
+        best.form = f.form;
+        best.splits = (int32_t)splits;
+      }
+    }
+  }
+  best.workspace = best.splits > 1 ? (size_t)best.splits * (size_t)a.i * (size_t)(div_up(a.j, 8) * 8) * 4 : 0;
+  return best;
 }
+
+namespace {
+template <typename S, bool PT, bool QT, int EPI>
+hipError_t launch_group(const LinArgs& a, hipStream_t stream) {
+  const dim3 grid((uint32_t)(div_up(a.i, S::kI) * div_up(a.j, S::kJ)), (uint32_t)a.splits);
+  k_linear_group<PT, QT, EPI, S><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
+  return hipGetLastError();
+}
+}  // namespace
 
 hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
                          hipStream_t stream) {
@@ -577,23 +795,23 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
   with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
     using T = decltype(t);
     if constexpr (std::is_same<T, Bf16>::value) {
-      if (fast_fits(a, pt(), qt())) {
+      if (plan.form == kFast) {
         const dim3 grid((uint32_t)(div_up(a.i, kFastB) * div_up(a.j, kFastB)), (uint32_t)a.splits);
-        auto* kernel = k_linear_fast<pt(), qt(), ep()>;
-        static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                                              hipFuncAttributeMaxDynamicSharedMemorySize, 8 * kHalfBytes);
-        e = allowed;
-        if (e != hipSuccess) return;
-        kernel<<<grid, dim3(kFastThreads), 8 * kHalfBytes, stream>>>(a);
-      } else {
-        const dim3 grid((uint32_t)(div_up(a.i, kTileB) * div_up(a.j, kTileB)), (uint32_t)a.splits);
-        k_linear_tile<T, pt(), qt(), ep()><<<grid, dim3(kTileThreads), 0, stream>>>(a);
+        k_linear_fast<pt(), qt(), ep()><<<grid, dim3(kFastThreads), 8 * kHalfBytes, stream>>>(a);
+        e = hipGetLastError();
+      } else if (plan.form == kMiddle) {
+        e = launch_group<MiddleShape, pt(), qt(), ep()>(a, stream);
+      } else if (plan.form == kSmall) {
+        e = launch_group<SmallShape, pt(), qt(), ep()>(a, stream);
+      } else if (plan.form == kTiny) {
+        e = launch_group<TinyShape, pt(), qt(), ep()>(a, stream);
       }
-    } else {
+    }
+    if (plan.form == kGeneral) {
       const dim3 grid((uint32_t)(div_up(a.i, kTileB) * div_up(a.j, kTileB)), (uint32_t)a.splits);
       k_linear_tile<T, pt(), qt(), ep()><<<grid, dim3(kTileThreads), 0, stream>>>(a);
+      e = hipGetLastError();
     }
-    e = hipGetLastError();
     if (e != hipSuccess || a.splits <= 1) return;
     k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
     e = hipGetLastError();
