@@ -54,6 +54,7 @@ struct LinArgs {
 // Element types by smat_dtype code: 0 = fp32, 1 = bf16.
 struct LinPlan {
   int32_t form;      // which tile (smat_linear.hip)
+  int32_t direct;    // operands go to LDS without passing registers
   int32_t splits;
   size_t workspace;  // bytes
 };

@@ -92,65 +92,30 @@ __device__ __forceinline__ Frag<T> read_frag(const char* stage, int row0, int t,
   return f;
 }
 
-// ---------------------------------------------------------------- the general tile
-// Any alignment, strides and sizes: chunks go through registers, loaded whole where they lie inside the
-// operand and element by element at its ends.
+// ---------------------------------------------------------------- operands of any alignment
+// 16 bytes at any element's address where `valid` elements or more of them exist, else what there is, zeros after it.
 template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const typename El<T>::Mem* p, int64_t valid) {
+__device__ __forceinline__ u32x4 load_chunk(const typename El<T>::Mem* p, int32_t valid) {
   constexpr int kChunk = 16 / El<T>::kBytes;
+  typedef uint32_t word_mem __attribute__((aligned(2)));
   if (valid >= kChunk) return *reinterpret_cast<const typename El<T>::vec_mem*>(p);
   u32x4 x = {0u, 0u, 0u, 0u};
+  if (valid <= 0) return x;
+  const int32_t words = valid * El<T>::kBytes / 4;  // whole ones; bf16 may have half a word more
+  const auto* w = reinterpret_cast<const word_mem*>(p);
 #pragma unroll
-  for (int e = 0; e < kChunk; ++e)
-    if (e < valid) {
-      if constexpr (El<T>::kBytes == 4)
-        x[e] = __float_as_uint(p[e]);
-      else
-        x[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
+  for (int e = 0; e < 3; ++e)
+    if (e < words) x[e] = w[e];
+  if constexpr (El<T>::kBytes == 2) {
+    if (valid & 1) {
+      const uint32_t half = p[valid - 1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e == words) x[e] = half;
     }
+  }
   return x;
 }
-
-// A thread's chunks of a stage: rows row0 .. row0 + B of the operand (of `rows`), r from r0 (below `rend`).
-template <typename T, bool TRANS, bool Q, int B, int THREADS>
-struct Stage {
-  static constexpr int kChunk = 16 / El<T>::kBytes, kDeep = 128 / El<T>::kBytes, kCount = B * 8 / THREADS;
-  u32x4 x[kCount];
-  __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t row0, int64_t rows, int64_t r0,
-                                       int64_t rend) {
-    const auto* p = static_cast<const typename El<T>::Mem*>(base);
-#pragma unroll
-    for (int u = 0; u < kCount; ++u) {
-      const int id = (int)threadIdx.x + u * THREADS;
-      int64_t valid, at;
-      if constexpr (!TRANS) {
-        const int64_t row = row0 + id / 8, r = r0 + (id % 8) * kChunk;
-        valid = row < rows ? rend - r : 0;
-        at = row * ld + r;
-      } else {
-        const int64_t r = r0 + id / (B / kChunk), row = row0 + (id % (B / kChunk)) * kChunk;
-        valid = r < rend ? rows - row : 0;
-        at = r * ld + row;
-      }
-      x[u] = valid > 0 ? load_chunk<T>(p + at, valid) : u32x4{0u, 0u, 0u, 0u};
-    }
-  }
-  __device__ __forceinline__ void store(char* stage) const {
-#pragma unroll
-    for (int u = 0; u < kCount; ++u) {
-      const int id = (int)threadIdx.x + u * THREADS;
-      int at;
-      if constexpr (!TRANS) {
-        const int row = id / 8, c = (id % 8) ^ direct_swizzle<Q>(row);
-        at = row * 128 + c * 16;
-      } else {
-        const int r = id / (B / kChunk), c = (id % (B / kChunk)) ^ transposed_swizzle<T, Q, B>(r);
-        at = r * B * El<T>::kBytes + c * 16;
-      }
-      *reinterpret_cast<u32x4*>(stage + at) = x[u];
-    }
-  }
-};
 
 // The epilogue of a wave's accumulators, or their store as a partial sum: four eights of values a lane at a
 // time, chosen by a branch on a uniform number.  Unrolled over all 16 eights an epilogue with an activation is 100 KB
@@ -219,52 +184,6 @@ __device__ __forceinline__ int64_t split_start(int64_t n, uint32_t s, int32_t sp
   return (int64_t)(each * s + (s < more ? s : more));
 }
 
-constexpr int kTileB = 128, kTileThreads = 256;
-
-template <typename T, bool PT, bool QT, int EPI>
-__global__ __launch_bounds__(kTileThreads, 2) void k_linear_tile(LinArgs a) {
-  constexpr int kDeep = 128 / El<T>::kBytes;
-  __shared__ alignas(16) char sp[kTileB * 128], sq[kTileB * 128];
-  const int64_t tiles_j = (a.j + kTileB - 1) / kTileB;
-  const int64_t ti = blockIdx.x / tiles_j, i0 = ti * kTileB, j0 = ((int64_t)blockIdx.x - ti * tiles_j) * kTileB;
-  const int wave = (int)threadIdx.x / 64, wi = (wave / 2) * 64, wj = (wave % 2) * 64;
-  // stages of r: those of prod[0], then those of prod[1]; this block's range of them
-  const int64_t n0 = (a.prod[0].r + kDeep - 1) / kDeep, n = n0 + (a.prod[1].r + kDeep - 1) / kDeep;
-  const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
-  f32x4 acc[4][4] = {};
-  Stage<T, PT, false, kTileB, kTileThreads> p;
-  Stage<T, QT, true, kTileB, kTileThreads> q;
-  const auto load = [&](int64_t s) {
-    const LinProduct& pr = s < n0 ? a.prod[0] : a.prod[1];
-    const int64_t r0 = (s < n0 ? s : s - n0) * kDeep;
-    p.load(pr.p, pr.ldp, i0, a.i, r0, pr.r);
-    q.load(pr.q, pr.ldq, j0, a.j, r0, pr.r);
-  };
-  if (first < last) load(first);
-  for (int64_t s = first; s < last; ++s) {
-    p.store(sp);
-    q.store(sq);
-    __syncthreads();
-    if (s + 1 < last) load(s + 1);
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      Frag<T> fp[4], fq[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        fp[x] = read_frag<T, PT, false, kTileB>(sp, wi + 16 * x, 0, kk);
-        fq[x] = read_frag<T, QT, true, kTileB>(sq, wj + 32 * (x / 2), x % 2, kk);
-      }
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) mma(fq[y], fp[x], acc[x][y]);
-    }
-    __syncthreads();
-  }
-  finish<T, EPI>(
-      a, i0 + wi, j0 + wj, acc, [](int p) { return 16 * p; }, [](int q) { return 32 * q; });
-}
-
 // ---------------------------------------------------------------- the pipelined tile
 // bf16 operands whose rows start on 16-byte boundaries (and, where r runs along them, end on one) go
 // from global memory to LDS without passing registers.
@@ -305,9 +224,10 @@ constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer
 
 // Copies of NI KB of a stage by one of the waves that share it: rows (columns) row0 .. row0 + B of the operand, `rows`
 // of them in all.
-template <bool TRANS, bool Q, int B, int NI>
+template <typename T, bool TRANS, bool Q, int B, int NI>
 struct Copy {
-  const uint16_t* base;  // of the first row or column
+  static constexpr int kBytes = El<T>::kBytes, kChunk = 16 / kBytes, kDeep = 128 / kBytes;
+  const typename El<T>::Mem* base;  // of the first row or column
   int64_t ld, left;      // left: rows or columns from the first one
   int64_t r;             // of the product
   uint32_t off[NI];      // this lane's byte offset at r0 = 0
@@ -317,18 +237,18 @@ struct Copy {
     r = pr.r;
     ld = Q ? pr.ldq : pr.ldp;
     left = rows - row0;
-    base = static_cast<const uint16_t*>(Q ? pr.q : pr.p) + (TRANS ? row0 : row0 * ld);
+    base = static_cast<const typename El<T>::Mem*>(Q ? pr.q : pr.p) + (TRANS ? row0 : row0 * ld);
 #pragma unroll
     for (int u = 0; u < NI; ++u) {
       if constexpr (!TRANS) {
         const int row = (wave * NI + u) * 8 + lane / 8, c = (lane % 8) ^ direct_swizzle<Q>(row);
-        chunk[u] = (uint32_t)c * 8;
-        off[u] = row < left ? (uint32_t)(row * ld * 2) + (uint32_t)c * 16 : kNowhere;
+        chunk[u] = (uint32_t)(c * kChunk);
+        off[u] = row < left ? (uint32_t)(row * ld * kBytes) + (uint32_t)c * 16 : kNowhere;
       } else {
-        constexpr int kChunks = B / 8;
+        constexpr int kChunks = B / kChunk;
         const int rr = (wave * NI + u) * (64 / kChunks) + lane / kChunks;
-        const int c = (lane % kChunks) ^ transposed_swizzle<Bf16, Q, B>(rr);
-        off[u] = (uint32_t)(rr * ld * 2) + (uint32_t)(c * 16);
+        const int c = (lane % kChunks) ^ transposed_swizzle<T, Q, B>(rr);
+        off[u] = (uint32_t)(rr * ld * kBytes) + (uint32_t)(c * 16);
       }
     }
   }
@@ -338,8 +258,8 @@ struct Copy {
     if constexpr (!TRANS) {
       rsrc = make_rsrc(base + r0, 0x7FFFFFF0u);
     } else {
-      const int64_t deep = r - r0 < 64 ? r - r0 : 64;
-      const int64_t bytes = deep > 0 && left > 0 ? (((deep - 1) * ld + left) * 2 + 15) & ~(int64_t)15 : 0;
+      const int64_t deep = r - r0 < kDeep ? r - r0 : kDeep;
+      const int64_t bytes = deep > 0 && left > 0 ? (((deep - 1) * ld + left) * kBytes + 15) & ~(int64_t)15 : 0;
       rsrc = make_rsrc(base + r0 * ld, (uint32_t)(bytes < 0x7FFFFFF0 ? bytes : 0x7FFFFFF0));
     }
 #pragma unroll
@@ -351,7 +271,57 @@ struct Copy {
   }
 };
 
+// The same stages by way of registers, for operands of any alignment and stride.
+template <typename T, bool TRANS, bool Q, int B, int NI>
+struct Staged {
+  static constexpr int kBytes = El<T>::kBytes, kChunk = 16 / kBytes, kDeep = 128 / kBytes;
+  static constexpr int kAcross = TRANS ? B / kChunk : 8;  // chunks a row of the stage
+  static constexpr int kRows = 64 / kAcross;              // rows of the stage a KB
+  const typename El<T>::Mem* base;                        // of the first row or column
+  int64_t ld, r;
+  int32_t left;   // rows or columns from the first one, as far as the stage reaches
+  int32_t row, c;  // this lane's row of the stage in the first KB, and its chunk
+  int64_t off;    // its elements from base at r0 = 0
+  u32x4 x[NI];
+  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows, int wave) {
+    const int lane = (int)threadIdx.x & 63;
+    r = pr.r;
+    ld = Q ? pr.ldq : pr.ldp;
+    left = (int32_t)(rows - row0 < B ? rows - row0 : B);
+    base = static_cast<const typename El<T>::Mem*>(Q ? pr.q : pr.p) + (TRANS ? row0 : row0 * ld);
+    row = wave * NI * kRows + lane / kAcross;
+    c = lane % kAcross;
+    off = row * ld + c * kChunk;
+  }
+  __device__ __forceinline__ void load(int64_t r0) {
+    const int32_t deep = (int32_t)(r - r0 < kDeep ? r - r0 : kDeep);  // r of this stage, <= 0 past the last
+    const int32_t short_ld = (int32_t)(ld < kChunk ? ld : kChunk);
+    const auto* p = base + (TRANS ? r0 * ld : r0);
+#pragma unroll
+    for (int u = 0; u < NI; ++u) {
+      const int32_t at = row + u * kRows;
+      int32_t valid;
+      if constexpr (TRANS)
+        // a chunk may run past its row into the next ones, whose values only reach columns outside, but not
+        // past the last row of the stage
+        valid = at < deep && c * kChunk < left ? (deep - 1 - at) * short_ld + left - c * kChunk : 0;
+      else
+        valid = at < left ? deep - c * kChunk : 0;
+      x[u] = load_chunk<T>(p + u * kRows * ld + off, valid);
+    }
+  }
+  __device__ __forceinline__ void store(char* stage) const {
+#pragma unroll
+    for (int u = 0; u < NI; ++u) {
+      const int at = row + u * kRows;
+      const int swizzled = TRANS ? c ^ transposed_swizzle<T, Q, B>(at) : c ^ direct_swizzle<Q>(at);
+      *reinterpret_cast<u32x4*>(stage + at * (kAcross * 16) + swizzled * 16) = x[u];
+    }
+  }
+};
+
 // The stages of r that a wave copies, in the order of the sum: those of prod[0], then those of prod[1].
+template <int DEEP>
 struct Stages {
   int64_t at, here, todo, n0, n;  // next stage in its product, stages of that product, stages left, stages of prod[0], of both
   __device__ __forceinline__ void set(const LinArgs& a, int64_t first, int64_t last, int64_t n0_, int64_t n_) {
@@ -362,7 +332,7 @@ struct Stages {
     todo = last - first;
   }
   // the next stage's first r; a place past the end once there is none
-  __device__ __forceinline__ int64_t r0(int64_t r) const { return todo > 0 ? at * 64 : r; }
+  __device__ __forceinline__ int64_t r0(int64_t r) const { return todo > 0 ? at * DEEP : r; }
   // whether the next stage is the first of prod[1]
   __device__ __forceinline__ bool advance() {
     --todo;
@@ -395,8 +365,8 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
   const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
-  Copy<PT, false, kFastHalf, 2> cp[2];
-  Copy<QT, true, kFastHalf, 2> cq[2];
+  Copy<T, PT, false, kFastHalf, 2> cp[2];
+  Copy<T, QT, true, kFastHalf, 2> cq[2];
   const auto set = [&](const LinProduct& pr) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -405,7 +375,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
     }
   };
   set(a.prod[first >= n0]);
-  Stages todo;
+  Stages<64> todo;
   todo.set(a, first, last, n0, n);
   const uint32_t mine = lds0 + (uint32_t)wave * 2048;
   const auto copy_p = [&](int h, int buf) {  // half h of the next stage to copy
@@ -517,37 +487,53 @@ struct GroupShape {
   static constexpr int kSimdWaves = kResident * WI * WJ * G / 4;
 };
 
-template <bool PT, bool QT, int EPI, typename S>
+// DIRECT: stages go from global memory to LDS (Copy), else through registers (Staged; two buffers).
+template <typename T, bool PT, bool QT, int EPI, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(LinArgs a) {
-  using T = Bf16;
   constexpr int kWaves = S::WI * S::WJ, kNp = S::kI / 8 / kWaves, kNq = S::kJ / 8 / kWaves, kXi = S::TI / 16, kXj = S::TJ / 16;
+  constexpr int kDeep = 128 / El<T>::kBytes;
   static_assert(kNp * 8 * kWaves == S::kI && kNq * 8 * kWaves == S::kJ, "whole KB a wave");
+  static_assert(S::NBUF == 2 || DIRECT, "a stage in registers, one being read, one being written");
   extern __shared__ char smem[];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), group = wave / kWaves, w = wave % kWaves;
   uint32_t ti, tj;
   tile_place(blockIdx.x, (uint32_t)((a.i + S::kI - 1) / S::kI), (uint32_t)((a.j + S::kJ - 1) / S::kJ), ti, tj);
   const int64_t i0 = (int64_t)ti * S::kI, j0 = (int64_t)tj * S::kJ;
   const int wi = w / S::WJ * S::TI, wj = w % S::WJ * S::TJ;
-  const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
+  const int64_t n0 = (a.prod[0].r + kDeep - 1) / kDeep, n = n0 + (a.prod[1].r + kDeep - 1) / kDeep;
   const uint32_t share = blockIdx.y * S::G + (uint32_t)group;
   const int64_t first = split_start(n, share, a.splits * S::G), last = split_start(n, share + 1, a.splits * S::G);
-  // every group of a block takes part in the same number of steps, so that barriers meet (shares differ by one stage)
+  // every group of a block takes the same number of steps, so that barriers meet (shares differ by one stage)
   const int64_t steps = (n + a.splits * S::G - 1) / (a.splits * S::G);
-  Copy<PT, false, S::kI, kNp> cp;
-  Copy<QT, true, S::kJ, kNq> cq;
+  using OperandP = typename std::conditional<DIRECT, Copy<T, PT, false, S::kI, kNp>, Staged<T, PT, false, S::kI, kNp>>::type;
+  using OperandQ = typename std::conditional<DIRECT, Copy<T, QT, true, S::kJ, kNq>, Staged<T, QT, true, S::kJ, kNq>>::type;
+  OperandP op;
+  OperandQ oq;
   const auto set = [&](const LinProduct& pr) {
-    cp.set(pr, i0, a.i, w);
-    cq.set(pr, j0, a.j, w);
+    op.set(pr, i0, a.i, w);
+    oq.set(pr, j0, a.j, w);
   };
   set(a.prod[first >= n0 && a.prod[1].r > 0]);
-  Stages todo;
+  Stages<kDeep> todo;
   todo.set(a, first, last, n0, n);
   char* const mine = smem + group * S::NBUF * S::kStage;
-  const uint32_t lds = (uint32_t)(uintptr_t)(lds_char*)mine;
-  const auto copy = [&](int buf) {
-    cp.start(todo.r0(cp.r), lds + (uint32_t)(buf * S::kStage + w * kNp * 1024));
-    cq.start(todo.r0(cq.r), lds + (uint32_t)(buf * S::kStage + S::kI * 128 + w * kNq * 1024));
+  // the next stage on its way: into buffer `buf`, or into registers
+  const auto fetch = [&](int buf) {
+    if constexpr (DIRECT) {
+      const uint32_t lds = (uint32_t)(uintptr_t)(lds_char*)mine + (uint32_t)(buf * S::kStage);
+      op.start(todo.r0(op.r), lds + (uint32_t)(w * kNp * 1024));
+      oq.start(todo.r0(oq.r), lds + (uint32_t)(S::kI * 128 + w * kNq * 1024));
+    } else {
+      op.load(todo.r0(op.r));
+      oq.load(todo.r0(oq.r));
+    }
     if (todo.advance()) set(a.prod[1]);
+  };
+  const auto place = [&](int buf) {
+    if constexpr (!DIRECT) {
+      op.store(mine + buf * S::kStage);
+      oq.store(mine + buf * S::kStage + S::kI * 128);
+    }
   };
   f32x4 acc[kXi][kXj] = {};
   Frag<T> fp[2][kXi][2], fq[2][kXj][2];  // [parity][tile][kk]
@@ -570,15 +556,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
       asm volatile("" ::: "memory");
     }
   };
-  int buf = 0;
-  // the fragments `set_` of this step have been asked for: wait for them and for the next stage, fill their
-  // buffer again, ask for the next fragments, multiply
-  const auto step = [&](int set_) {
-    wait_copies<(S::NBUF - 2) * (kNp + kNq)>();
-    meet();
-    copy(buf);
-    buf = buf + 1 == S::NBUF ? 0 : buf + 1;
-    read(set_ ^ 1, buf);
+  const auto multiply = [&](int set_) {
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -586,9 +564,36 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
 #pragma unroll
         for (int y = 0; y < kXj; ++y) mma(fq[set_][y][kk], fp[set_][x][kk], acc[x][y]);
   };
+  int buf = 0;
+  // The fragments `set_` of this step have been asked for.  DIRECT: wait for them and for the next stage, fill their
+  // buffer again, ask for the next fragments, multiply.  Else: put the next stage into the other buffer (whose
+  // fragments every wave had before the last barrier), start loading the one after, wait, and the same.
+  const auto step = [&](int set_) {
+    if constexpr (DIRECT) {
+      wait_copies<(S::NBUF - 2) * (kNp + kNq)>();
+      meet();
+      fetch(buf);
+      buf = buf + 1 == S::NBUF ? 0 : buf + 1;
+    } else {
+      buf ^= 1;
+      place(buf);
+      fetch(buf);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      meet();
+    }
+    read(set_ ^ 1, buf);
+    multiply(set_);
+  };
+  if constexpr (DIRECT) {
 #pragma unroll
-  for (int b = 0; b < S::NBUF; ++b) copy(b);
-  wait_copies<(S::NBUF - 1) * (kNp + kNq)>();
+    for (int b = 0; b < S::NBUF; ++b) fetch(b);
+    wait_copies<(S::NBUF - 1) * (kNp + kNq)>();
+  } else {
+    fetch(0);
+    place(0);
+    fetch(1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
   meet();
   read(0, 0);
   for (int64_t s = 0; s < steps; s += 2) {
@@ -707,13 +712,15 @@ void with_element(int dtype, F&& fn) {
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int kComputeUnits = 256;
 
-// Whether the pipelined kernel can take an operand: 16-byte rows, and offsets of a tile below 2^31.
-bool operand_fits(const void* p, int64_t ld, int64_t r, bool trans) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && (trans || r % 8 == 0) && ld < ((int64_t)1 << 21);
+// Whether an operand's stages can be copied to LDS directly: 16-byte rows, and offsets of a tile below 2^31.
+bool operand_fits(const void* p, int64_t ld, int64_t r, bool trans, int bytes) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * bytes % 16 == 0 && (trans || r * bytes % 16 == 0) &&
+         ld < ((int64_t)1 << 20);
 }
-bool fast_fits(const LinArgs& a, bool pt, bool qt) {
+bool fast_fits(const LinArgs& a, bool pt, bool qt, int bytes) {
   for (const LinProduct& pr : a.prod)
-    if (pr.r > 0 && !(operand_fits(pr.p, pr.ldp, pr.r, pt) && operand_fits(pr.q, pr.ldq, pr.r, qt))) return false;
+    if (pr.r > 0 && !(operand_fits(pr.p, pr.ldp, pr.r, pt, bytes) && operand_fits(pr.q, pr.ldq, pr.r, qt, bytes)))
+      return false;
   return a.prod[0].r > 0;
 }
 
@@ -733,7 +740,7 @@ void with_form(int dtype, LinEpilogue epi, F&& fn) {
 
 namespace {
 // The tiles a product can be computed with.
-enum TileForm : int32_t { kGeneral = 0, kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4 };
+enum TileForm : int32_t { kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4 };
 using MiddleShape = GroupShape<64, 64, 2, 2, 1, 2>;  // 128 x 128, two blocks a compute unit
 using SmallShape = GroupShape<64, 64, 1, 1, 4, 2>;   // 64 x 64, r in four
 using TinyShape = GroupShape<32, 32, 1, 1, 8, 2>;    // 32 x 32, r in eight
@@ -750,16 +757,15 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int64_t deep = dtype == 1 ? 64 : 32;
   const int64_t stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
   const bool pt = epi == kEpiStore, qt = epi != kEpiLayer;
-  static const FormCost general[] = {{kGeneral, kTileB, kTileB, 2, 1, 1.6, 8.0}};
-  static const FormCost pipelined[] = {{kFast, kFastB, kFastB, 1, 1, 1.40, 11.0},
-                                       {kMiddle, MiddleShape::kI, MiddleShape::kJ, 2, 1, 1.1, 8.0},
-                                       {kSmall, SmallShape::kI, SmallShape::kJ, 1, 4, 0.9, 6.0},
-                                       {kTiny, TinyShape::kI, TinyShape::kJ, 1, 8, 0.7, 5.0}};
-  const bool fits = dtype == 1 && fast_fits(a, pt, qt);
   LinPlan best{};
+  static const FormCost bf16[] = {{kFast, kFastB, kFastB, 1, 1, 1.40, 11.0},
+                                  {kMiddle, MiddleShape::kI, MiddleShape::kJ, 2, 1, 1.1, 8.0},
+                                  {kSmall, SmallShape::kI, SmallShape::kJ, 1, 4, 0.9, 6.0},
+                                  {kTiny, TinyShape::kI, TinyShape::kJ, 1, 8, 0.7, 5.0}};
+  best.direct = fast_fits(a, pt, qt, dtype == 1 ? 2 : 4);
   double least = 1e30;
-  for (int c = 0; c < (fits ? 4 : 1); ++c) {
-    const FormCost& f = fits ? pipelined[c] : general[c];
+  for (const FormCost& f : bf16) {
+    if (f.form == kFast && !(best.direct && dtype == 1)) continue;
     const int64_t tiles = div_up(a.i, f.i) * div_up(a.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
     for (int64_t splits = 1; splits <= 16 && (splits == 1 || splits * f.groups * 2 <= stages); ++splits) {
       const double rounds = (double)div_up(tiles * splits, slots);
@@ -778,10 +784,13 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
 }
 
 namespace {
-template <typename S, bool PT, bool QT, int EPI>
-hipError_t launch_group(const LinArgs& a, hipStream_t stream) {
+template <typename S, typename T, bool PT, bool QT, int EPI>
+hipError_t launch_group(const LinArgs& a, bool direct, hipStream_t stream) {
   const dim3 grid((uint32_t)(div_up(a.i, S::kI) * div_up(a.j, S::kJ)), (uint32_t)a.splits);
-  k_linear_group<PT, QT, EPI, S><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
+  if (direct)
+    k_linear_group<T, PT, QT, EPI, S, true><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
+  else
+    k_linear_group<T, PT, QT, EPI, S, false><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
   return hipGetLastError();
 }
 }  // namespace
@@ -799,19 +808,11 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
         const dim3 grid((uint32_t)(div_up(a.i, kFastB) * div_up(a.j, kFastB)), (uint32_t)a.splits);
         k_linear_fast<pt(), qt(), ep()><<<grid, dim3(kFastThreads), 8 * kHalfBytes, stream>>>(a);
         e = hipGetLastError();
-      } else if (plan.form == kMiddle) {
-        e = launch_group<MiddleShape, pt(), qt(), ep()>(a, stream);
-      } else if (plan.form == kSmall) {
-        e = launch_group<SmallShape, pt(), qt(), ep()>(a, stream);
-      } else if (plan.form == kTiny) {
-        e = launch_group<TinyShape, pt(), qt(), ep()>(a, stream);
       }
     }
-    if (plan.form == kGeneral) {
-      const dim3 grid((uint32_t)(div_up(a.i, kTileB) * div_up(a.j, kTileB)), (uint32_t)a.splits);
-      k_linear_tile<T, pt(), qt(), ep()><<<grid, dim3(kTileThreads), 0, stream>>>(a);
-      e = hipGetLastError();
-    }
+    if (plan.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
+    if (plan.form == kSmall) e = launch_group<SmallShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
+    if (plan.form == kTiny) e = launch_group<TinyShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
     if (e != hipSuccess || a.splits <= 1) return;
     k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
     e = hipGetLastError();
