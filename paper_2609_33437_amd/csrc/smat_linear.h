@@ -56,6 +56,8 @@ struct LinPlan {
   int32_t form;      // which tile (smat_linear.hip)
   int32_t direct;    // operands go to LDS without passing registers
   int32_t splits;
+  int32_t pack;      // bits: operands copied to 16-byte rows first (P, Q of prod[0], then of prod[1])
+  size_t packed[4];  // where in the workspace
   size_t workspace;  // bytes
 };
 LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi);

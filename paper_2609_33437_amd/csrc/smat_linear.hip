@@ -670,6 +670,47 @@ __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
   epilogue8<T, EPI, 1, 2>(a, i, j, v, c, s);
 }
 
+// ---------------------------------------------------------------- copies on 16-byte rows
+// bf16 operands off 16-byte rows, copied to rows of whole 16 bytes with zeros at their ends: every chunk is read once
+// at its element's address and written once.  A block takes kPackChunks of one operand.
+constexpr int kPackChunks = 1024;
+struct PackJob {
+  const uint16_t* from;
+  uint16_t* to;
+  int64_t ld, run, across, chunks;  // chunks a row, and in all
+  int64_t rows_on, chunks_on;       // from a thread's chunk to its next, 256 further
+  uint32_t end;                     // the first block after this operand's
+};
+struct PackJobs {
+  PackJob job[4];
+  int32_t count;
+  uint32_t blocks;
+};
+
+__global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
+  int k = 0;
+  while (k + 1 < jobs.count && blockIdx.x >= jobs.job[k].end) ++k;
+  const PackJob& j = jobs.job[k];
+  const int64_t first = (int64_t)(blockIdx.x - (k ? jobs.job[k - 1].end : 0u)) * kPackChunks + threadIdx.x;
+  const int64_t row0 = first / j.across;
+  int64_t row = row0, c = first - row0 * j.across;
+  u32x4 x[kPackChunks / 256];
+#pragma unroll
+  for (int u = 0; u < kPackChunks / 256; ++u) {
+    const int64_t left = j.run - c * 8;
+    if (first + u * 256 < j.chunks) x[u] = load_chunk<Bf16>(j.from + row * j.ld + c * 8, (int32_t)(left < 8 ? left : 8));
+    row += j.rows_on;
+    c += j.chunks_on;
+    if (c >= j.across) {
+      c -= j.across;
+      ++row;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kPackChunks / 256; ++u)
+    if (first + u * 256 < j.chunks) *reinterpret_cast<u32x4*>(j.to + (first + u * 256) * 8) = x[u];
+}
+
 // ---------------------------------------------------------------- column sums
 // A block sums 64 columns over its share of the rows, four rows at a time; a second launch adds the
 // shares in their order.
@@ -717,12 +758,6 @@ bool operand_fits(const void* p, int64_t ld, int64_t r, bool trans, int bytes) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * bytes % 16 == 0 && (trans || r * bytes % 16 == 0) &&
          ld < ((int64_t)1 << 20);
 }
-bool fast_fits(const LinArgs& a, bool pt, bool qt, int bytes) {
-  for (const LinProduct& pr : a.prod)
-    if (pr.r > 0 && !(operand_fits(pr.p, pr.ldp, pr.r, pt, bytes) && operand_fits(pr.q, pr.ldq, pr.r, qt, bytes)))
-      return false;
-  return a.prod[0].r > 0;
-}
 
 // fn(element type, P transposed, Q transposed, epilogue) of an operation.
 template <typename F>
@@ -746,40 +781,102 @@ using SmallShape = GroupShape<64, 64, 1, 1, 4, 2>;   // 64 x 64, r in four
 using TinyShape = GroupShape<32, 32, 1, 1, 8, 2>;    // 32 x 32, r in eight
 
 // What the choice of a tile goes by: the tile, blocks that run together on a compute unit, stages of r that a block
-// takes together (its groups), and microseconds of a stage with every unit busy and of the rest of a block.
+// takes together (its groups), and measured microseconds: of a stage with as many blocks on each unit, of one with one
+// block a unit, and of a block's start and end.
 struct FormCost {
   int32_t form, i, j, resident, groups;
-  double stage, rest;
+  double stage, alone, rest;
 };
-}  // namespace
+constexpr FormCost fast_cost(double stage, double rest) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, rest}; }
+template <typename S>
+constexpr FormCost cost(int32_t form, double stage, double alone, double rest) {
+  return {form, S::kI, S::kJ, S::kResident, S::G, stage, alone, rest};
+}
+// bf16 with stages copied to LDS directly; by way of registers (64 x 64 tiles, one wave a SIMD, took twice as
+// long then and are left out); fp32, whose matrix instructions take 16 times as long.
+const FormCost kDirectCosts[] = {fast_cost(1.40, 11.0), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0),
+                                 cost<SmallShape>(kSmall, 0.92, 0.92, 5.2), cost<TinyShape>(kTiny, 0.46, 0.46, 4.4)};
+const FormCost kStagedCosts[] = {cost<MiddleShape>(kMiddle, 1.15, 1.0, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)};
+const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<SmallShape>(kSmall, 2.35, 2.35, 4.5),
+                               cost<TinyShape>(kTiny, 1.1, 1.1, 4.5)};
 
-LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
-  const int64_t deep = dtype == 1 ? 64 : 32;
-  const int64_t stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
-  const bool pt = epi == kEpiStore, qt = epi != kEpiLayer;
-  LinPlan best{};
-  static const FormCost bf16[] = {{kFast, kFastB, kFastB, 1, 1, 1.40, 11.0},
-                                  {kMiddle, MiddleShape::kI, MiddleShape::kJ, 2, 1, 1.1, 8.0},
-                                  {kSmall, SmallShape::kI, SmallShape::kJ, 1, 4, 0.9, 6.0},
-                                  {kTiny, TinyShape::kI, TinyShape::kJ, 1, 8, 0.7, 5.0}};
-  best.direct = fast_fits(a, pt, qt, dtype == 1 ? 2 : 4);
+// The least-time tile and number of ranges of r by those costs.
+template <size_t N>
+double choose(const FormCost (&costs)[N], const LinArgs& a, int64_t stages, LinPlan& plan) {
   double least = 1e30;
-  for (const FormCost& f : bf16) {
-    if (f.form == kFast && !(best.direct && dtype == 1)) continue;
+  for (const FormCost& f : costs) {
     const int64_t tiles = div_up(a.i, f.i) * div_up(a.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
     for (int64_t splits = 1; splits <= 16 && (splits == 1 || splits * f.groups * 2 <= stages); ++splits) {
-      const double rounds = (double)div_up(tiles * splits, slots);
-      double us = rounds * (f.rest + (double)div_up(stages, splits * f.groups) * f.stage);
+      const int64_t blocks = tiles * splits, rounds = blocks / slots, left = blocks % slots;
+      const double steps = (double)div_up(stages, splits * f.groups), full = f.rest + steps * f.stage;
+      double us = (double)rounds * full;
+      if (left) us += left > kComputeUnits || rounds ? full : f.rest + steps * f.alone;
       // the partial sums are written and read, and another launch joins them
-      if (splits > 1) us += 5.0 + (double)splits * (double)a.i * (double)a.j * 8.0 / 4e6;
+      if (splits > 1) us += 2.5 + (double)splits * (double)a.i * (double)a.j * 8.0 / 8e6;
       if (us < least) {
         least = us;
-        best.form = f.form;
-        best.splits = (int32_t)splits;
+        plan.form = f.form;
+        plan.splits = (int32_t)splits;
       }
     }
   }
-  best.workspace = best.splits > 1 ? (size_t)best.splits * (size_t)a.i * (size_t)(div_up(a.j, 8) * 8) * 4 : 0;
+  return least;
+}
+
+// An operand as it lies in memory: `rows` runs of `run` elements.
+struct Operand {
+  const void* p;
+  int64_t ld, rows, run;
+  bool fits;
+};
+// Operands 2 s and 2 s + 1 are P and Q of product s.
+void operands(const LinArgs& a, LinEpilogue epi, int bytes, Operand (&o)[4]) {
+  const bool pt = epi == kEpiStore, qt = epi != kEpiLayer;
+  for (int s = 0; s < 2; ++s) {
+    const LinProduct& pr = a.prod[s];
+    o[2 * s] = {pr.p, pr.ldp, pt ? pr.r : a.i, pt ? a.i : pr.r, pr.r == 0 || operand_fits(pr.p, pr.ldp, pr.r, pt, bytes)};
+    o[2 * s + 1] = {pr.q, pr.ldq, qt ? pr.r : a.j, qt ? a.j : pr.r, pr.r == 0 || operand_fits(pr.q, pr.ldq, pr.r, qt, bytes)};
+  }
+}
+int64_t packed_ld(int64_t run, int bytes) { return div_up(run * bytes, 16) * 16 / bytes; }
+}  // namespace
+
+LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
+  const int bytes = dtype == 1 ? 2 : 4;
+  const int64_t deep = 128 / bytes, stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
+  LinPlan best{};
+  Operand o[4];
+  operands(a, epi, bytes, o);
+  int32_t off = 0;  // operands whose rows do not start and end on 16 bytes
+  double moved = 0.0;
+  for (int k = 0; k < 4; ++k)
+    if (!o[k].fits) {
+      off |= 1 << k;
+      moved += 2.0 * (double)o[k].rows * (double)o[k].run * bytes;
+    }
+  if (dtype == 1) {
+    const double direct = choose(kDirectCosts, a, stages, best);
+    best.direct = 1;
+    if (off) {
+      // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
+      LinPlan staged{};
+      const double through = choose(kStagedCosts, a, stages, staged);
+      if (through <= direct + 4.0 + moved / 4.5e6)
+        best = staged;
+      else
+        best.pack = off;
+    }
+  } else {
+    choose(kFp32Costs, a, stages, best);
+    best.direct = off == 0;
+  }
+  const size_t sums = best.splits > 1 ? (size_t)best.splits * (size_t)a.i * (size_t)(div_up(a.j, 8) * 8) * 4 : 0;
+  best.workspace = sums;
+  for (int k = 0; k < 4; ++k)
+    if (best.pack >> k & 1) {
+      best.packed[k] = best.workspace;
+      best.workspace += (size_t)o[k].rows * (size_t)packed_ld(o[k].run, bytes) * bytes;
+    }
   return best;
 }
 
@@ -789,7 +886,7 @@ hipError_t launch_group(const LinArgs& a, bool direct, hipStream_t stream) {
   const dim3 grid((uint32_t)(div_up(a.i, S::kI) * div_up(a.j, S::kJ)), (uint32_t)a.splits);
   if (direct)
     k_linear_group<T, PT, QT, EPI, S, true><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
-  else
+  else if constexpr (sizeof(typename El<T>::Mem) == 4 || !std::is_same<S, SmallShape>::value)
     k_linear_group<T, PT, QT, EPI, S, false><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
   return hipGetLastError();
 }
@@ -801,6 +898,25 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
   a.splits = plan.splits;
   a.partial = static_cast<float*>(workspace);
   hipError_t e = hipSuccess;
+  if (plan.pack) {
+    PackJobs jobs{};
+    Operand o[4];
+    operands(a, epi, 2, o);
+    for (int k = 0; k < 4; ++k)
+      if (plan.pack >> k & 1) {
+        uint16_t* to = reinterpret_cast<uint16_t*>(static_cast<char*>(workspace) + plan.packed[k]);
+        const int64_t ld = packed_ld(o[k].run, 2);
+        PackJob& j = jobs.job[jobs.count++];
+        j = {static_cast<const uint16_t*>(o[k].p), to, o[k].ld, o[k].run, ld / 8, o[k].rows * (ld / 8), 256 / (ld / 8), 256 % (ld / 8)};
+        jobs.blocks += (uint32_t)div_up(j.chunks, kPackChunks);
+        j.end = jobs.blocks;
+        LinProduct& pr = a.prod[k / 2];
+        (k % 2 ? pr.q : pr.p) = to;
+        (k % 2 ? pr.ldq : pr.ldp) = ld;
+      }
+    k_pack<<<dim3(jobs.blocks), dim3(256), 0, stream>>>(jobs);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
     using T = decltype(t);
     if constexpr (std::is_same<T, Bf16>::value) {

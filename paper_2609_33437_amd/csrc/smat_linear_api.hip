@@ -237,6 +237,7 @@ smat_status wgrad_call(const smat_linear_wgrad_args* g, WgradCall* c, const char
   a.ldout = g->lddw;
   c->empty = g->n == 0 || g->k == 0;
   if (!c->empty) {
+    if (ckpt) a.prod[0].ldq = smat::ckpt_blocks(g->k) * smat::kCkptBlock;  // as it is read back into the workspace
     c->plan = smat::linear_plan(a, g->dtype, smat::kEpiStore);
     c->sums = round16(c->plan.workspace);
     if (ckpt) c->x = (size_t)g->m * (size_t)(smat::ckpt_blocks(g->k) * smat::kCkptBlock) * dtype_bytes(g->dtype);
@@ -342,11 +343,9 @@ extern "C" smat_status smat_linear_wgrad(const smat_linear_wgrad_args* args, voi
   if (c.empty) return SMAT_OK;
   if (c.x) {
     void* x = ws + c.sums + c.db;
-    const int64_t ld = smat::ckpt_blocks(args->k) * smat::kCkptBlock;
     SMAT_HIP(smat::launch_ckpt_read(args->x_codes, args->x_exps, nullptr, nullptr, SMAT_ACT_NONE, args->m, args->k,
-                                    args->dtype, x, ld, stream));
+                                    args->dtype, x, c.a.prod[0].ldq, stream));
     c.a.prod[0].q = x;
-    c.a.prod[0].ldq = ld;
   }
   SMAT_HIP(smat::launch_linear(c.a, args->dtype, smat::kEpiStore, c.plan, workspace, stream));
   return SMAT_OK;
