@@ -65,9 +65,8 @@ hipError_t launch_linear(const LinArgs& a, int dtype, LinEpilogue epi, const Lin
                          hipStream_t stream);
 
 // db[j] = sum_i dy[i][j] for dy [rows, cols].
-size_t column_sum_workspace(int64_t rows, int64_t cols);
 hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t cols, int dtype, void* db,
-                             void* workspace, hipStream_t stream);
+                             hipStream_t stream);
 
 hipError_t launch_ckpt_write(const void* x, int64_t ld, int64_t rows, int64_t cols, int dtype, int8_t* codes,
                              uint8_t* exps, hipStream_t stream);

@@ -648,6 +648,125 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   }
 }
 
+// ---------------------------------------------------------------- few rows
+// A layer over a few rows (the next tokens of a few sequences) is bound by reading W once.  A wave reads 1 KB of a row
+// of W an instruction, whatever its alignment (a matrix fragment's 64 bytes of 16 rows streamed a fifth slower, and at
+// half the rate off 16-byte rows), multiplies it with the same 1 KB of each row of x on the vector units, and adds its
+// lanes' sums at the end.  A block's eight waves take JB rows of W, four a wave, and share out r where that leaves
+// waves over.
+constexpr int kRowsWaves = 8, kRowsEach = 4, kMaxRows = 8;
+
+template <typename T>
+__device__ __forceinline__ float dot_chunk(const u32x4& w, const u32x4& x, float sum) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (El<T>::kBytes == 4) {
+      sum = __builtin_fmaf(__uint_as_float(w[e]), __uint_as_float(x[e]), sum);
+    } else {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      const uint32_t we = w[e], xe = x[e];  // a bit cast of a vector's element itself takes the first one
+      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, we), __builtin_bit_cast(bf16x2, xe), sum, false);
+    }
+  }
+  return sum;
+}
+
+template <typename T, int M, int JB>
+__global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
+  using Mem = typename El<T>::Mem;
+  constexpr int kChunk = 16 / El<T>::kBytes, kGroups = kRowsWaves * kRowsEach / JB, kValues = kRowsEach * M;
+  constexpr int kStep = 64 * kChunk, kAhead = M <= 2 ? 4 : 2;
+  __shared__ float sums[kGroups][M][JB + 4];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+  const int group = wave % kGroups, jrow = wave / kGroups * kRowsEach;
+  const int64_t j0 = (int64_t)blockIdx.x * JB, r = a.prod[0].r;
+  // this thread's part of the epilogue, its loads under way from the start
+  constexpr int kFinish = M * JB / 8;
+  const int fi = (int)threadIdx.x / (JB / 8), fj = (int)threadIdx.x % (JB / 8) * 8;
+  Side<T, kEpiLayer> side;
+  ColumnSide<T, kEpiLayer> column;
+  if (threadIdx.x < kFinish) {
+    column_load<T, kEpiLayer>(a, j0 + fj, column);
+    side_load<T, kEpiLayer>(a, fi, j0 + fj, side);
+  }
+  // rows past the last of W and x repeat it; what they give is not kept
+  const Mem *w[kRowsEach], *x[M];
+#pragma unroll
+  for (int y = 0; y < kRowsEach; ++y) {
+    const int64_t row = j0 + jrow + y;
+    w[y] = static_cast<const Mem*>(a.prod[0].q) + (row < a.j ? row : a.j - 1) * a.prod[0].ldq;
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m) x[m] = static_cast<const Mem*>(a.prod[0].p) + (m < a.i ? m : a.i - 1) * a.prod[0].ldp;
+  float sum[kValues] = {};
+  const auto run = [&](auto count, int64_t k0) {
+    constexpr int kCount = decltype(count)::value;
+    u32x4 cw[kCount][kRowsEach], cx[kCount][M];
+#pragma unroll
+    for (int u = 0; u < kCount; ++u) {
+      const int64_t at = k0 + (int64_t)u * kGroups * kStep + lane * kChunk;
+#pragma unroll
+      for (int y = 0; y < kRowsEach; ++y) cw[u][y] = *reinterpret_cast<const typename El<T>::vec_mem*>(w[y] + at);
+#pragma unroll
+      for (int m = 0; m < M; ++m) cx[u][m] = *reinterpret_cast<const typename El<T>::vec_mem*>(x[m] + at);
+    }
+#pragma unroll
+    for (int u = 0; u < kCount; ++u)
+#pragma unroll
+      for (int y = 0; y < kRowsEach; ++y)
+#pragma unroll
+        for (int m = 0; m < M; ++m) sum[y * M + m] = dot_chunk<T>(cw[u][y], cx[u][m], sum[y * M + m]);
+  };
+  int64_t k = (int64_t)group * kStep;
+  constexpr int64_t kRound = (int64_t)kGroups * kStep;
+  for (; k + (kAhead - 1) * kRound + kStep <= r; k += kAhead * kRound) run(std::integral_constant<int, kAhead>(), k);
+  for (; k + kStep <= r; k += kRound) run(std::integral_constant<int, 1>(), k);
+  if (k < r) {  // what is left, less than 1 KB
+    const int64_t at = k + lane * kChunk, left = r - at;
+    const int32_t valid = (int32_t)(left < 0 ? 0 : left < kChunk ? left : kChunk);
+    u32x4 cx[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) cx[m] = load_chunk<T>(x[m] + at, valid);
+#pragma unroll
+    for (int y = 0; y < kRowsEach; ++y) {
+      const u32x4 cw = load_chunk<T>(w[y] + at, valid);
+#pragma unroll
+      for (int m = 0; m < M; ++m) sum[y * M + m] = dot_chunk<T>(cw, cx[m], sum[y * M + m]);
+    }
+  }
+  // the lanes' sums: while there are several values a lane exchanges half of them for its partner's other half, so
+  // the values are dealt to the lanes as they are added; then the one left is added over the remaining lane bits
+  int count = kValues;
+#pragma unroll
+  for (int bit = 32; bit > 0; bit >>= 1) {
+    if (count > 1) {
+      count /= 2;
+#pragma unroll
+      for (int v = 0; v < kValues / 2; ++v) {
+        if (v < count) {
+          const float low = sum[v], high = sum[v + count];
+          sum[v] = ((lane & bit) ? high : low) + __shfl_xor((lane & bit) ? low : high, bit);
+        }
+      }
+    } else {
+      sum[0] += __shfl_xor(sum[0], bit);
+    }
+  }
+  constexpr int kLanes = 64 / kValues;  // lanes with the same value
+  if (lane % kLanes == 0) {
+    const int v = lane / kLanes;
+    sums[group][v % M][jrow + v / M] = sum[0];
+  }
+  __syncthreads();
+  if (threadIdx.x >= kFinish) return;
+  float v[8] = {};
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += sums[g][fi][fj + e];
+  epilogue8<T, kEpiLayer, 1, 2>(a, fi, j0 + fj, v, column, side);
+}
+
 // Joins the partial sums in their order and applies the epilogue: eight j a thread.
 template <typename T, int EPI>
 __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
@@ -712,33 +831,46 @@ __global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
 }
 
 // ---------------------------------------------------------------- column sums
-// A block sums 64 columns over its share of the rows, four rows at a time; a second launch adds the
-// shares in their order.
-constexpr int kSumRows = 512;
+// A block sums 64 columns over all rows: eight lanes hold a row's 64 columns, 128 rows at a time, and their sums are
+// added through LDS in the rows' order.  One launch: a second one that joins shares of the rows takes as long as
+// the sums of 2,000 rows.
+constexpr int kSumCols = 64, kSumThreads = 1024, kSumRows = kSumThreads / 8;
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_column_sum(const typename El<T>::Mem* __restrict__ dy, int64_t ld, int64_t rows,
-                                                    int64_t cols, float* __restrict__ partial) {
-  __shared__ float s[4][64];
-  const int col = (int)threadIdx.x & 63, sub = (int)threadIdx.x >> 6;
-  const int64_t j = (int64_t)blockIdx.x * 64 + col, r0 = (int64_t)blockIdx.y * kSumRows;
-  const int64_t rend = r0 + kSumRows < rows ? r0 + kSumRows : rows;
-  float v = 0.f;
-  if (j < cols)
-    for (int64_t r = r0 + sub; r < rend; r += 4) v += El<T>::load(dy + r * ld + j);
-  s[sub][col] = v;
+__global__ __launch_bounds__(kSumThreads) void k_column_sum(const typename El<T>::Mem* __restrict__ dy, int64_t ld,
+                                                            int64_t rows, int64_t cols,
+                                                            typename El<T>::Mem* __restrict__ db) {
+  __shared__ float s[kSumRows][kSumCols + 1];
+  const int sub = (int)threadIdx.x / 8, c = (int)threadIdx.x % 8 * 8;
+  const int64_t j0 = (int64_t)blockIdx.x * kSumCols + c, valid = cols - j0;
+  float v[8] = {};
+  if (valid > 0) {
+#pragma unroll 4
+    for (int64_t r = sub; r < rows; r += kSumRows) {
+      float x[8];
+      load_row8<T>(dy + r * ld + j0, valid, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[sub][c + e] = v[e];
   __syncthreads();
-  if (sub == 0 && j < cols) partial[(int64_t)blockIdx.y * cols + j] = (s[0][col] + s[1][col]) + (s[2][col] + s[3][col]);
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void k_column_join(const float* __restrict__ partial, int64_t cols, int32_t shares,
-                                                     typename El<T>::Mem* __restrict__ db) {
-  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (j >= cols) return;
-  float v = 0.f;
-  for (int32_t s = 0; s < shares; ++s) v += partial[(int64_t)s * cols + j];
-  El<T>::store(db + j, v);
+  // 16 threads a column add eight rows each, then one thread their sums
+  const int col = (int)threadIdx.x % kSumCols, part = (int)threadIdx.x / kSumCols;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < kSumRows / 16; ++k) sum += s[part * (kSumRows / 16) + k][col];
+  __syncthreads();
+  s[part][col] = sum;
+  __syncthreads();
+  const int64_t j = (int64_t)blockIdx.x * kSumCols + col;
+  if (part == 0 && j < cols) {
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += s[k][col];
+    El<T>::store(db + j, sum);
+  }
 }
 
 // ---------------------------------------------------------------- launches
@@ -775,7 +907,7 @@ void with_form(int dtype, LinEpilogue epi, F&& fn) {
 
 namespace {
 // The tiles a product can be computed with.
-enum TileForm : int32_t { kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4 };
+enum TileForm : int32_t { kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4, kRows = 5 };
 using MiddleShape = GroupShape<64, 64, 2, 2, 1, 2>;  // 128 x 128, two blocks a compute unit
 using SmallShape = GroupShape<64, 64, 1, 1, 4, 2>;   // 64 x 64, r in four
 using TinyShape = GroupShape<32, 32, 1, 1, 8, 2>;    // 32 x 32, r in eight
@@ -787,15 +919,21 @@ struct FormCost {
   int32_t form, i, j, resident, groups;
   double stage, alone, rest;
 };
-constexpr FormCost fast_cost(double stage, double rest) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, rest}; }
 template <typename S>
 constexpr FormCost cost(int32_t form, double stage, double alone, double rest) {
   return {form, S::kI, S::kJ, S::kResident, S::G, stage, alone, rest};
 }
-// bf16 with stages copied to LDS directly; by way of registers (64 x 64 tiles, one wave a SIMD, took twice as
-// long then and are left out); fp32, whose matrix instructions take 16 times as long.
-const FormCost kDirectCosts[] = {fast_cost(1.40, 11.0), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0),
-                                 cost<SmallShape>(kSmall, 0.92, 0.92, 5.2), cost<TinyShape>(kTiny, 0.46, 0.46, 4.4)};
+// bf16 with stages copied to LDS directly (the 256 x 256 tile's stage by how many operands are transposed); by way
+// of registers (64 x 64 tiles, one wave a SIMD, took twice as long then and are left out); fp32, whose matrix
+// instructions take 16 times as long.
+constexpr FormCost direct_fast(double stage) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, 10.0}; }
+const FormCost kDirectCosts[3][4] = {
+    {direct_fast(1.38), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
+     cost<TinyShape>(kTiny, 0.46, 0.46, 4.4)},
+    {direct_fast(1.48), cost<MiddleShape>(kMiddle, 0.94, 0.66, 6.0), cost<SmallShape>(kSmall, 0.90, 0.90, 5.2),
+     cost<TinyShape>(kTiny, 0.50, 0.50, 4.4)},
+    {direct_fast(1.65), cost<MiddleShape>(kMiddle, 0.96, 0.70, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
+     cost<TinyShape>(kTiny, 0.52, 0.52, 4.4)}};
 const FormCost kStagedCosts[] = {cost<MiddleShape>(kMiddle, 1.15, 1.0, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)};
 const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<SmallShape>(kSmall, 2.35, 2.35, 4.5),
                                cost<TinyShape>(kTiny, 1.1, 1.1, 4.5)};
@@ -845,6 +983,11 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int bytes = dtype == 1 ? 2 : 4;
   const int64_t deep = 128 / bytes, stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
   LinPlan best{};
+  if (epi == kEpiLayer && a.i <= kMaxRows) {
+    best.form = kRows;
+    best.splits = 1;
+    return best;
+  }
   Operand o[4];
   operands(a, epi, bytes, o);
   int32_t off = 0;  // operands whose rows do not start and end on 16 bytes
@@ -855,13 +998,13 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       moved += 2.0 * (double)o[k].rows * (double)o[k].run * bytes;
     }
   if (dtype == 1) {
-    const double direct = choose(kDirectCosts, a, stages, best);
+    const double direct = choose(kDirectCosts[epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0], a, stages, best);
     best.direct = 1;
     if (off) {
       // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
       LinPlan staged{};
       const double through = choose(kStagedCosts, a, stages, staged);
-      if (through <= direct + 4.0 + moved / 4.5e6)
+      if (through <= direct + 6.0 + moved / 3.0e6)
         best = staged;
       else
         best.pack = off;
@@ -926,6 +1069,29 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
         e = hipGetLastError();
       }
     }
+    if constexpr (ep() == kEpiLayer) {
+      if (plan.form == kRows) {
+        // a checkpoint's blocks need 32 columns; without one narrower blocks until there are enough of them
+        const auto launch = [&](auto jb) {
+          const dim3 grid((uint32_t)div_up(a.j, jb())), block(64 * kRowsWaves);
+          if (a.i == 1)
+            k_linear_rows<T, 1, jb()><<<grid, block, 0, stream>>>(a);
+          else if (a.i == 2)
+            k_linear_rows<T, 2, jb()><<<grid, block, 0, stream>>>(a);
+          else if (a.i <= 4)
+            k_linear_rows<T, 4, jb()><<<grid, block, 0, stream>>>(a);
+          else
+            k_linear_rows<T, 8, jb()><<<grid, block, 0, stream>>>(a);
+        };
+        if (a.codes || a.j >= 32 * kComputeUnits)
+          launch(std::integral_constant<int, 32>());
+        else if (a.j >= 16 * kComputeUnits)
+          launch(std::integral_constant<int, 16>());
+        else
+          launch(std::integral_constant<int, 8>());
+        e = hipGetLastError();
+      }
+    }
     if (plan.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
     if (plan.form == kSmall) e = launch_group<SmallShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
     if (plan.form == kTiny) e = launch_group<TinyShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
@@ -936,27 +1102,15 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
   return e;
 }
 
-size_t column_sum_workspace(int64_t rows, int64_t cols) { return (size_t)div_up(rows, kSumRows) * (size_t)cols * 4; }
-
 hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t cols, int dtype, void* db,
-                             void* workspace, hipStream_t stream) {
-  const int64_t shares = div_up(rows, kSumRows);
-  float* partial = static_cast<float*>(workspace);
-  hipError_t e = hipSuccess;
+                             hipStream_t stream) {
   with_element(dtype, [&](auto t) {
     using T = decltype(t);
     using Mem = typename El<T>::Mem;
-    if (shares > 0) {
-      k_column_sum<T><<<dim3((uint32_t)div_up(cols, 64), (uint32_t)shares), dim3(256), 0, stream>>>(
-          static_cast<const Mem*>(dy), ld, rows, cols, partial);
-      e = hipGetLastError();
-    }
-    if (e != hipSuccess) return;
-    k_column_join<T><<<dim3((uint32_t)div_up(cols, 256)), dim3(256), 0, stream>>>(partial, cols, (int32_t)shares,
-                                                                                  static_cast<Mem*>(db));
-    e = hipGetLastError();
+    k_column_sum<T><<<dim3((uint32_t)div_up(cols, kSumCols)), dim3(kSumThreads), 0, stream>>>(
+        static_cast<const Mem*>(dy), ld, rows, cols, static_cast<Mem*>(db));
   });
-  return e;
+  return hipGetLastError();
 }
 
 }  // namespace smat

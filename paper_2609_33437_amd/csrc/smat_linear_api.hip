@@ -199,10 +199,10 @@ smat_status dgrad_call(const smat_linear_dgrad_args* g, Call* c, const char* whe
   return SMAT_OK;
 }
 
-// The workspace of a weight gradient: the partial sums of dw, those of db, and x read back from its checkpoint.
+// The workspace of a weight gradient: the product's, and x read back from its checkpoint.
 struct WgradCall : Call {
-  size_t sums = 0, db = 0, x = 0;
-  size_t bytes() const { return sums + db + x; }
+  size_t product = 0, x = 0;
+  size_t bytes() const { return product + x; }
 };
 size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
 
@@ -239,10 +239,9 @@ smat_status wgrad_call(const smat_linear_wgrad_args* g, WgradCall* c, const char
   if (!c->empty) {
     if (ckpt) a.prod[0].ldq = smat::ckpt_blocks(g->k) * smat::kCkptBlock;  // as it is read back into the workspace
     c->plan = smat::linear_plan(a, g->dtype, smat::kEpiStore);
-    c->sums = round16(c->plan.workspace);
+    c->product = round16(c->plan.workspace);
     if (ckpt) c->x = (size_t)g->m * (size_t)(smat::ckpt_blocks(g->k) * smat::kCkptBlock) * dtype_bytes(g->dtype);
   }
-  if (g->db) c->db = round16(smat::column_sum_workspace(g->m, g->n));
   return SMAT_OK;
 }
 
@@ -339,10 +338,10 @@ extern "C" smat_status smat_linear_wgrad(const smat_linear_wgrad_args* args, voi
   if (smat_status st = check_workspace(workspace, workspace_bytes, c.bytes(), "smat_linear_wgrad")) return st;
   char* ws = static_cast<char*>(workspace);
   if (args->db && args->n > 0)
-    SMAT_HIP(smat::launch_column_sum(args->dy, args->lddy, args->m, args->n, args->dtype, args->db, ws + c.sums, stream));
+    SMAT_HIP(smat::launch_column_sum(args->dy, args->lddy, args->m, args->n, args->dtype, args->db, stream));
   if (c.empty) return SMAT_OK;
   if (c.x) {
-    void* x = ws + c.sums + c.db;
+    void* x = ws + c.product;
     SMAT_HIP(smat::launch_ckpt_read(args->x_codes, args->x_exps, nullptr, nullptr, SMAT_ACT_NONE, args->m, args->k,
                                     args->dtype, x, c.a.prod[0].ldq, stream));
     c.a.prod[0].q = x;

@@ -179,19 +179,24 @@ __device__ __forceinline__ uint32_t ckpt_byte(uint32_t bits) {
   const int e = (int)(bits >> 23) - 6;
   return bits >= 0x7F800000u ? 255u : (uint32_t)(e > 1 ? e : 1);
 }
-// 2^-E, 0 for a block of byte 255.
-__device__ __forceinline__ float ckpt_inverse(uint32_t byte) {
-  return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);
-}
-__device__ __forceinline__ uint32_t ckpt_code(float x, uint32_t byte, float inverse) {
-  const float q = byte == 255u ? 0.f : fminf(fmaxf(rintf(x * inverse), -127.f), 127.f);
-  return (uint32_t)(int)q & 255u;
-}
+// Codes of eight values.  Adding 1.5 * 2^23 rounds x 2^-E to nearest even and leaves the integer, in two's complement,
+// in the low bits; held to +-127 there, its low byte is the code.
 __device__ __forceinline__ u32x2 ckpt_pack8(const float v[8], uint32_t byte) {
-  const float inv = ckpt_inverse(byte);
-  u32x2 out = {0u, 0u};
+  constexpr float kMagic = 12582912.f;
+  constexpr int kMagicBits = 0x4B400000;
+  const float inverse = __uint_as_float((254u - byte) << 23);  // 2^-E; unused for a block of byte 255
+  u32x2 out;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) out[e / 4] |= ckpt_code(v[e], byte, inv) << (8 * (e % 4));
+  for (int h = 0; h < 2; ++h) {
+    uint32_t q[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int bits = (int)__float_as_uint(__builtin_fmaf(v[4 * h + e], inverse, kMagic));
+      q[e] = (uint32_t)min(max(bits, kMagicBits - 127), kMagicBits + 127);
+    }
+    const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u);
+    out[h] = byte == 255u ? 0u : lo | hi << 16;
+  }
   return out;
 }
 __device__ __forceinline__ void ckpt_unpack8(u32x2 codes, uint32_t byte, float v[8]) {
