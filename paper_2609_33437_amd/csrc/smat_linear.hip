@@ -207,11 +207,8 @@ typedef __attribute__((address_space(3))) char lds_char;
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // A buffer descriptor of `bytes` bytes: offsets past them read as zeros.
-__device__ __forceinline__ i32x4 make_rsrc(const void* p, uint32_t bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(p);
-  return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
-               __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF),
-               __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+__device__ __forceinline__ i32x4 make_rsrc(uint64_t p, uint32_t bytes) {
+  return i32x4{(int)(uint32_t)p, (int)((uint32_t)(p >> 32) & 0xFFFFu), (int)bytes, 0x00020000};
 }
 // 16 bytes a lane from `offset` of the buffer to LDS bytes lds + 16 lane.
 __device__ __forceinline__ void copy_to_lds(i32x4 rsrc, uint32_t offset, uint32_t lds) {
@@ -222,52 +219,71 @@ __device__ __forceinline__ void copy_to_lds(i32x4 rsrc, uint32_t offset, uint32_
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer
 
-// Copies of NI KB of a stage by one of the waves that share it: rows (columns) row0 .. row0 + B of the operand, `rows`
-// of them in all.
+// Where the next stage of an operand lies: rows (columns) from row0 on, r from r0 on.  Moved on by additions alone; the
+// 64-bit products of a fresh address each stage took longer than the stage's reads.
+template <typename T, bool TRANS, bool Q>
+struct Stream {
+  static constexpr int kBytes = El<T>::kBytes, kDeep = 128 / kBytes;
+  uint64_t base;
+  uint64_t step;
+  int64_t left;  // r that are left; transposed: bytes up to the operand's end, to whole 16
+  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows, int64_t r0) {
+    const int64_t ld = Q ? pr.ldq : pr.ldp;
+    base = reinterpret_cast<uint64_t>(Q ? pr.q : pr.p) + (uint64_t)(TRANS ? r0 * ld + row0 : row0 * ld + r0) * kBytes;
+    if constexpr (TRANS) {
+      step = (uint64_t)ld * 128;
+      left = r0 < pr.r && row0 < rows ? (((pr.r - r0 - 1) * ld + rows - row0) * kBytes + 15) & ~(int64_t)15 : 0;
+    } else {
+      step = 128;
+      left = pr.r - r0;
+    }
+  }
+  __device__ __forceinline__ void next() {
+    base += step;
+    left -= TRANS ? (int64_t)step : (int64_t)kDeep;
+  }
+  // offsets past the bytes read as zeros; `on`: there is a stage
+  __device__ __forceinline__ i32x4 rsrc(bool on) const {
+    const int64_t some = left < 0x7FFFFFF0 ? left : 0x7FFFFFF0;
+    return make_rsrc(base, TRANS ? (on && some > 0 ? (uint32_t)some : 0u) : 0x7FFFFFF0u);
+  }
+  // direct: r of the stage that exist
+  __device__ __forceinline__ int32_t deep(bool on) const {
+    return on && left > 0 ? (int32_t)(left < kDeep ? left : kDeep) : 0;
+  }
+};
+
+// Copies of NI KB of a stage by one of the waves that share it: B rows (columns), the first `skip` behind the stream's.
 template <typename T, bool TRANS, bool Q, int B, int NI>
 struct Copy {
-  static constexpr int kBytes = El<T>::kBytes, kChunk = 16 / kBytes, kDeep = 128 / kBytes;
-  const typename El<T>::Mem* base;  // of the first row or column
-  int64_t ld, left;      // left: rows or columns from the first one
-  int64_t r;             // of the product
-  uint32_t off[NI];      // this lane's byte offset at r0 = 0
-  uint32_t chunk[NI];    // this lane's first r of the stage (direct)
-  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows, int wave) {
+  static constexpr int kBytes = El<T>::kBytes, kChunk = 16 / kBytes;
+  uint32_t off[NI];  // this lane's bytes from the stream's place
+  int32_t chunk[NI]; // its first r of the stage (direct)
+  // rows: the operand's from the stream's first on
+  __device__ __forceinline__ void set(const LinProduct& pr, int skip, int64_t rows, int wave) {
     const int lane = (int)threadIdx.x & 63;
-    r = pr.r;
-    ld = Q ? pr.ldq : pr.ldp;
-    left = rows - row0;
-    base = static_cast<const typename El<T>::Mem*>(Q ? pr.q : pr.p) + (TRANS ? row0 : row0 * ld);
+    const uint32_t ld = (uint32_t)(Q ? pr.ldq : pr.ldp);
 #pragma unroll
     for (int u = 0; u < NI; ++u) {
       if constexpr (!TRANS) {
         const int row = (wave * NI + u) * 8 + lane / 8, c = (lane % 8) ^ direct_swizzle<Q>(row);
-        chunk[u] = (uint32_t)(c * kChunk);
-        off[u] = row < left ? (uint32_t)(row * ld * kBytes) + (uint32_t)c * 16 : kNowhere;
+        chunk[u] = c * kChunk;
+        off[u] = skip + row < rows ? (uint32_t)(skip + row) * ld * kBytes + (uint32_t)c * 16 : kNowhere;
       } else {
         constexpr int kChunks = B / kChunk;
         const int rr = (wave * NI + u) * (64 / kChunks) + lane / kChunks;
         const int c = (lane % kChunks) ^ transposed_swizzle<T, Q, B>(rr);
-        off[u] = (uint32_t)(rr * ld * kBytes) + (uint32_t)(c * 16);
+        off[u] = (uint32_t)rr * ld * kBytes + (uint32_t)(skip * kBytes + c * 16);
       }
     }
   }
-  // the stage that starts at r0, into LDS bytes `lds` .. of this wave's first KB
-  __device__ __forceinline__ void start(int64_t r0, uint32_t lds) const {
-    i32x4 rsrc;
-    if constexpr (!TRANS) {
-      rsrc = make_rsrc(base + r0, 0x7FFFFFF0u);
-    } else {
-      const int64_t deep = r - r0 < kDeep ? r - r0 : kDeep;
-      const int64_t bytes = deep > 0 && left > 0 ? (((deep - 1) * ld + left) * kBytes + 15) & ~(int64_t)15 : 0;
-      rsrc = make_rsrc(base + r0 * ld, (uint32_t)(bytes < 0x7FFFFFF0 ? bytes : 0x7FFFFFF0));
-    }
+  // the stream's stage into LDS bytes `lds` .. of this wave's first KB
+  __device__ __forceinline__ void start(const Stream<T, TRANS, Q>& s, bool on, uint32_t lds) const {
+    const i32x4 rsrc = s.rsrc(on);
+    const int32_t deep = TRANS ? 0 : s.deep(on);
 #pragma unroll
-    for (int u = 0; u < NI; ++u) {
-      uint32_t o = off[u];
-      if constexpr (!TRANS) o = r0 + chunk[u] < r ? o : kNowhere;
-      copy_to_lds(rsrc, o, lds + u * 1024);
-    }
+    for (int u = 0; u < NI; ++u)
+      copy_to_lds(rsrc, TRANS || chunk[u] < deep ? off[u] : kNowhere, lds + u * 1024);
   }
 };
 
@@ -278,14 +294,15 @@ struct Staged {
   static constexpr int kAcross = TRANS ? B / kChunk : 8;  // chunks a row of the stage
   static constexpr int kRows = 64 / kAcross;              // rows of the stage a KB
   const typename El<T>::Mem* base;                        // of the first row or column
-  int64_t ld, r;
-  int32_t left;   // rows or columns from the first one, as far as the stage reaches
-  int32_t row, c;  // this lane's row of the stage in the first KB, and its chunk
-  int64_t off;    // its elements from base at r0 = 0
+  int64_t ld, r, r0;  // r0: of the next stage
+  int32_t left;       // rows or columns from the first one, as far as the stage reaches
+  int32_t row, c;     // this lane's row of the stage in the first KB, and its chunk
+  int64_t off;        // its elements from base at r0 = 0
   u32x4 x[NI];
-  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows, int wave) {
+  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows, int64_t from, int wave) {
     const int lane = (int)threadIdx.x & 63;
     r = pr.r;
+    r0 = from;
     ld = Q ? pr.ldq : pr.ldp;
     left = (int32_t)(rows - row0 < B ? rows - row0 : B);
     base = static_cast<const typename El<T>::Mem*>(Q ? pr.q : pr.p) + (TRANS ? row0 : row0 * ld);
@@ -293,8 +310,9 @@ struct Staged {
     c = lane % kAcross;
     off = row * ld + c * kChunk;
   }
-  __device__ __forceinline__ void load(int64_t r0) {
-    const int32_t deep = (int32_t)(r - r0 < kDeep ? r - r0 : kDeep);  // r of this stage, <= 0 past the last
+  __device__ __forceinline__ void load(bool on) {
+    // r of this stage, <= 0 past the last
+    const int32_t deep = on ? (int32_t)(r - r0 < kDeep ? r - r0 : kDeep) : 0;
     const int32_t short_ld = (int32_t)(ld < kChunk ? ld : kChunk);
     const auto* p = base + (TRANS ? r0 * ld : r0);
 #pragma unroll
@@ -310,6 +328,7 @@ struct Staged {
       x[u] = load_chunk<T>(p + u * kRows * ld + off, valid);
     }
   }
+  __device__ __forceinline__ void next() { r0 += kDeep; }
   __device__ __forceinline__ void store(char* stage) const {
 #pragma unroll
     for (int u = 0; u < NI; ++u) {
@@ -321,24 +340,19 @@ struct Staged {
 };
 
 // The stages of r that a wave copies, in the order of the sum: those of prod[0], then those of prod[1].
-template <int DEEP>
 struct Stages {
-  int64_t at, here, todo, n0, n;  // next stage in its product, stages of that product, stages left, stages of prod[0], of both
-  __device__ __forceinline__ void set(const LinArgs& a, int64_t first, int64_t last, int64_t n0_, int64_t n_) {
-    n0 = n0_;
-    n = n_;
-    at = first >= n0 ? first - n0 : first;
-    here = first >= n0 ? n - n0 : n0;
-    todo = last - first;
+  int32_t todo, here, more;  // stages left, left of this product, of prod[1]
+  __device__ __forceinline__ void set(int64_t first, int64_t last, int64_t n0, int64_t n) {
+    todo = (int32_t)(last - first);
+    here = (int32_t)(first >= n0 ? n - first : n0 - first);
+    more = (int32_t)(n - n0);
   }
-  // the next stage's first r; a place past the end once there is none
-  __device__ __forceinline__ int64_t r0(int64_t r) const { return todo > 0 ? at * DEEP : r; }
+  __device__ __forceinline__ bool on() const { return todo > 0; }
   // whether the next stage is the first of prod[1]
   __device__ __forceinline__ bool advance() {
     --todo;
-    if (++at != here || todo <= 0) return false;
-    at = 0;
-    here = n - n0;
+    if (--here != 0 || todo <= 0) return false;
+    here = more;
     return true;
   }
 };
@@ -365,27 +379,31 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
   const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
+  Stream<T, PT, false> sp;
+  Stream<T, QT, true> sq;
   Copy<T, PT, false, kFastHalf, 2> cp[2];
   Copy<T, QT, true, kFastHalf, 2> cq[2];
-  const auto set = [&](const LinProduct& pr) {
+  const auto set = [&](const LinProduct& pr, int64_t r0) {
+    sp.set(pr, i0, a.i, r0);
+    sq.set(pr, j0, a.j, r0);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      cp[h].set(pr, i0 + h * kFastHalf, a.i, wave);
-      cq[h].set(pr, j0 + h * kFastHalf, a.j, wave);
+      cp[h].set(pr, h * kFastHalf, a.i - i0, wave);
+      cq[h].set(pr, h * kFastHalf, a.j - j0, wave);
     }
   };
-  set(a.prod[first >= n0]);
-  Stages<64> todo;
-  todo.set(a, first, last, n0, n);
+  set(a.prod[first >= n0], (first >= n0 ? first - n0 : first) * 64);
+  Stages todo;
+  todo.set(first, last, n0, n);
   const uint32_t mine = lds0 + (uint32_t)wave * 2048;
   const auto copy_p = [&](int h, int buf) {  // half h of the next stage to copy
-    cp[h].start(todo.r0(cp[h].r), mine + (buf * 4 + h) * kHalfBytes);
+    cp[h].start(sp, todo.on(), mine + (buf * 4 + h) * kHalfBytes);
   };
-  const auto copy_q = [&](int h, int buf) {
-    cq[h].start(todo.r0(cq[h].r), mine + (buf * 4 + 2 + h) * kHalfBytes);
-  };
+  const auto copy_q = [&](int h, int buf) { cq[h].start(sq, todo.on(), mine + (buf * 4 + 2 + h) * kHalfBytes); };
   const auto advance = [&] {
-    if (todo.advance()) set(a.prod[1]);
+    sp.next();
+    sq.next();
+    if (todo.advance()) set(a.prod[1], 0);
   };
   f32x4 acc[8][4] = {};  // [half of P, tile][half of Q, tile]
   Frag<T> fp[4][2], fq[2][2][2];  // [tile][kk], [half][tile][kk]
@@ -505,34 +523,48 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   const int64_t first = split_start(n, share, a.splits * S::G), last = split_start(n, share + 1, a.splits * S::G);
   // every group of a block takes the same number of steps, so that barriers meet (shares differ by one stage)
   const int64_t steps = (n + a.splits * S::G - 1) / (a.splits * S::G);
-  using OperandP = typename std::conditional<DIRECT, Copy<T, PT, false, S::kI, kNp>, Staged<T, PT, false, S::kI, kNp>>::type;
-  using OperandQ = typename std::conditional<DIRECT, Copy<T, QT, true, S::kJ, kNq>, Staged<T, QT, true, S::kJ, kNq>>::type;
-  OperandP op;
-  OperandQ oq;
-  const auto set = [&](const LinProduct& pr) {
-    op.set(pr, i0, a.i, w);
-    oq.set(pr, j0, a.j, w);
+  Stream<T, PT, false> sp;
+  Stream<T, QT, true> sq;
+  Copy<T, PT, false, S::kI, kNp> cp;
+  Copy<T, QT, true, S::kJ, kNq> cq;
+  Staged<T, PT, false, S::kI, kNp> rp;
+  Staged<T, QT, true, S::kJ, kNq> rq;
+  const auto set = [&](const LinProduct& pr, int64_t r0) {
+    if constexpr (DIRECT) {
+      sp.set(pr, i0, a.i, r0);
+      sq.set(pr, j0, a.j, r0);
+      cp.set(pr, 0, a.i - i0, w);
+      cq.set(pr, 0, a.j - j0, w);
+    } else {
+      rp.set(pr, i0, a.i, r0, w);
+      rq.set(pr, j0, a.j, r0, w);
+    }
   };
-  set(a.prod[first >= n0 && a.prod[1].r > 0]);
-  Stages<kDeep> todo;
-  todo.set(a, first, last, n0, n);
+  const bool second = first >= n0 && a.prod[1].r > 0;
+  set(a.prod[second], (second ? first - n0 : first) * kDeep);
+  Stages todo;
+  todo.set(first, last, n0, n);
   char* const mine = smem + group * S::NBUF * S::kStage;
   // the next stage on its way: into buffer `buf`, or into registers
   const auto fetch = [&](int buf) {
     if constexpr (DIRECT) {
       const uint32_t lds = (uint32_t)(uintptr_t)(lds_char*)mine + (uint32_t)(buf * S::kStage);
-      op.start(todo.r0(op.r), lds + (uint32_t)(w * kNp * 1024));
-      oq.start(todo.r0(oq.r), lds + (uint32_t)(S::kI * 128 + w * kNq * 1024));
+      cp.start(sp, todo.on(), lds + (uint32_t)(w * kNp * 1024));
+      cq.start(sq, todo.on(), lds + (uint32_t)(S::kI * 128 + w * kNq * 1024));
+      sp.next();
+      sq.next();
     } else {
-      op.load(todo.r0(op.r));
-      oq.load(todo.r0(oq.r));
+      rp.load(todo.on());
+      rq.load(todo.on());
+      rp.next();
+      rq.next();
     }
-    if (todo.advance()) set(a.prod[1]);
+    if (todo.advance()) set(a.prod[1], 0);
   };
   const auto place = [&](int buf) {
     if constexpr (!DIRECT) {
-      op.store(mine + buf * S::kStage);
-      oq.store(mine + buf * S::kStage + S::kI * 128);
+      rp.store(mine + buf * S::kStage);
+      rq.store(mine + buf * S::kStage + S::kI * 128);
     }
   };
   f32x4 acc[kXi][kXj] = {};
