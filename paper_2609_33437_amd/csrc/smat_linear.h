@@ -51,15 +51,21 @@ struct LinArgs {
   float* partial;
 };
 
-// Element types by smat_dtype code: 0 = fp32, 1 = bf16.
+// How a product is computed: rows [0, part[0].rows) of out by one launch (and a join), the rest by another.
+struct LinPart {
+  int64_t rows;
+  int32_t form;    // which tile (smat_linear.hip)
+  int32_t splits;  // ranges of r
+};
 struct LinPlan {
-  int32_t form;      // which tile (smat_linear.hip)
+  LinPart part[2];
+  int32_t parts;
   int32_t direct;    // operands go to LDS without passing registers
-  int32_t splits;
   int32_t pack;      // bits: operands copied to 16-byte rows first (P, Q of prod[0], then of prod[1])
   size_t packed[4];  // where in the workspace
   size_t workspace;  // bytes
 };
+// Element types by smat_dtype code: 0 = fp32, 1 = bf16.
 LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi);
 hipError_t launch_linear(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
                          hipStream_t stream);

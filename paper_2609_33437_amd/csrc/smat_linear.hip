@@ -955,39 +955,86 @@ template <typename S>
 constexpr FormCost cost(int32_t form, double stage, double alone, double rest) {
   return {form, S::kI, S::kJ, S::kResident, S::G, stage, alone, rest};
 }
-// bf16 with stages copied to LDS directly (the 256 x 256 tile's stage by how many operands are transposed); by way
-// of registers (64 x 64 tiles, one wave a SIMD, took twice as long then and are left out); fp32, whose matrix
+// bf16 with stages copied to LDS directly, by how many operands are transposed; the same by way of registers (64 x 64 tiles, one wave a SIMD, took twice as long then and are left out); fp32, whose matrix
 // instructions take 16 times as long.
 constexpr FormCost direct_fast(double stage) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, 10.0}; }
 const FormCost kDirectCosts[3][4] = {
-    {direct_fast(1.38), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
+    {direct_fast(1.40), cost<MiddleShape>(kMiddle, 0.90, 0.66, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
      cost<TinyShape>(kTiny, 0.46, 0.46, 4.4)},
-    {direct_fast(1.48), cost<MiddleShape>(kMiddle, 0.94, 0.66, 6.0), cost<SmallShape>(kSmall, 0.90, 0.90, 5.2),
+    {direct_fast(1.43), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0), cost<SmallShape>(kSmall, 0.90, 0.90, 5.2),
      cost<TinyShape>(kTiny, 0.50, 0.50, 4.4)},
-    {direct_fast(1.65), cost<MiddleShape>(kMiddle, 0.96, 0.70, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
+    {direct_fast(1.46), cost<MiddleShape>(kMiddle, 0.94, 0.70, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
      cost<TinyShape>(kTiny, 0.52, 0.52, 4.4)}};
-const FormCost kStagedCosts[] = {cost<MiddleShape>(kMiddle, 1.15, 1.0, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)};
+const FormCost kStagedCosts[3][2] = {{cost<MiddleShape>(kMiddle, 1.15, 1.02, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)},
+                                     {cost<MiddleShape>(kMiddle, 1.31, 1.45, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)},
+                                     {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)}};
 const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<SmallShape>(kSmall, 2.35, 2.35, 4.5),
                                cost<TinyShape>(kTiny, 1.1, 1.1, 4.5)};
 
-// The least-time tile and number of ranges of r by those costs.
-template <size_t N>
-double choose(const FormCost (&costs)[N], const LinArgs& a, int64_t stages, LinPlan& plan) {
+// A product's sizes as the choice sees them: of out, its stages of r, and the microseconds that 65,536 values' epilogue
+// keeps a compute unit's vector units busy.
+struct Sizes {
+  int64_t i, j, stages;
+  double epilogue;
+};
+
+// Microseconds of `splits` ranges of r with tile f.
+double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
+  const int64_t blocks = div_up(z.i, f.i) * div_up(z.j, f.j) * splits, slots = (int64_t)kComputeUnits * f.resident;
+  const int64_t rounds = blocks / slots, left = blocks % slots;
+  const double steps = (double)div_up(z.stages, splits * f.groups);
+  const double end = splits > 1 ? 0.0 : z.epilogue * (double)(f.i * f.j) / 65536.0;
+  const double full = f.rest + steps * f.stage + end * f.resident;
+  double us = (double)rounds * full;
+  if (left) us += left > kComputeUnits || rounds ? full : f.rest + steps * f.alone + end;
+  // the partial sums are written and read, and another launch joins them
+  if (splits > 1) us += 2.5 + (double)splits * (double)z.i * (double)z.j * 8.0 / 8e6;
+  return us;
+}
+
+// The least-time tile and number of ranges of r by those costs.  Ranges beyond one block a place only cost.
+double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part) {
   double least = 1e30;
-  for (const FormCost& f : costs) {
-    const int64_t tiles = div_up(a.i, f.i) * div_up(a.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
-    for (int64_t splits = 1; splits <= 16 && (splits == 1 || splits * f.groups * 2 <= stages); ++splits) {
-      const int64_t blocks = tiles * splits, rounds = blocks / slots, left = blocks % slots;
-      const double steps = (double)div_up(stages, splits * f.groups), full = f.rest + steps * f.stage;
-      double us = (double)rounds * full;
-      if (left) us += left > kComputeUnits || rounds ? full : f.rest + steps * f.alone;
-      // the partial sums are written and read, and another launch joins them
-      if (splits > 1) us += 2.5 + (double)splits * (double)a.i * (double)a.j * 8.0 / 8e6;
+  for (int c = 0; c < count; ++c) {
+    const FormCost& f = costs[c];
+    const int64_t tiles = div_up(z.i, f.i) * div_up(z.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
+    int64_t most = slots / tiles + 1;
+    if (most > 16) most = 16;
+    if (most > z.stages / (2 * f.groups)) most = z.stages / (2 * f.groups);
+    for (int64_t splits = 1; splits == 1 || splits <= most; ++splits) {
+      const double us = time_of(f, z, splits);
       if (us < least) {
         least = us;
-        plan.form = f.form;
-        plan.splits = (int32_t)splits;
+        part = {z.i, f.form, (int32_t)splits};
       }
+    }
+  }
+  return least;
+}
+
+// The same in one launch or two: rounds of blocks that fill every compute unit, then the rows that are left with the
+// tile that suits them, where that beats a last round of few blocks.  (4096 x 8960 x 1536 with a gated epilogue: three
+// rounds of 256 x 256 tiles, the last of 48, took 200 us.)
+double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& plan) {
+  constexpr double kWorthIt = 15.0, kLaunch = 2.0;
+  double least = choose(costs, count, z, plan.part[0]);
+  plan.parts = 1;
+  if (least < kWorthIt) return least;
+  for (int c = 0; c < count; ++c) {
+    const FormCost& f = costs[c];
+    const int64_t across = div_up(z.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
+    const int64_t rounds = div_up(z.i, f.i) * across / slots, rows = rounds * slots / across * f.i;
+    if (rows <= 0 || rows >= z.i) continue;
+    Sizes first = z, rest = z;
+    first.i = rows;
+    rest.i = z.i - rows;
+    LinPart other;
+    const double us = time_of(f, first, 1) + kLaunch + choose(costs, count, rest, other);
+    if (us < least) {
+      least = us;
+      plan.part[0] = {rows, f.form, 1};
+      plan.part[1] = other;
+      plan.parts = 2;
     }
   }
   return least;
@@ -1013,13 +1060,16 @@ int64_t packed_ld(int64_t run, int bytes) { return div_up(run * bytes, 16) * 16 
 
 LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int bytes = dtype == 1 ? 2 : 4;
-  const int64_t deep = 128 / bytes, stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
+  const int64_t deep = 128 / bytes;
   LinPlan best{};
   if (epi == kEpiLayer && a.i <= kMaxRows) {
-    best.form = kRows;
-    best.splits = 1;
+    best.part[0] = {a.i, kRows, 1};
+    best.parts = 1;
     return best;
   }
+  Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0};
+  if (epi == kEpiLayer) z.epilogue = (a.act ? 8.0 : 0.0) + (a.codes ? 6.0 : 0.0) + (a.mul ? 2.0 : 0.0) + (a.residual ? 2.0 : 0.0);
+  if (epi == kEpiDgrad) z.epilogue = a.up_codes ? 22.0 : a.z_codes ? 13.0 : 0.0;
   Operand o[4];
   operands(a, epi, bytes, o);
   int32_t off = 0;  // operands whose rows do not start and end on 16 bytes
@@ -1030,23 +1080,28 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       moved += 2.0 * (double)o[k].rows * (double)o[k].run * bytes;
     }
   if (dtype == 1) {
-    const double direct = choose(kDirectCosts[epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0], a, stages, best);
+    const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
+    const double direct = choose_parts(kDirectCosts[transposed], 4, z, best);
     best.direct = 1;
     if (off) {
       // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
       LinPlan staged{};
-      const double through = choose(kStagedCosts, a, stages, staged);
+      const double through = choose_parts(kStagedCosts[transposed], 2, z, staged);
       if (through <= direct + 6.0 + moved / 3.0e6)
         best = staged;
       else
         best.pack = off;
     }
   } else {
-    choose(kFp32Costs, a, stages, best);
+    choose_parts(kFp32Costs, 3, z, best);
     best.direct = off == 0;
   }
-  const size_t sums = best.splits > 1 ? (size_t)best.splits * (size_t)a.i * (size_t)(div_up(a.j, 8) * 8) * 4 : 0;
-  best.workspace = sums;
+  // the parts run one after the other and share the place of their partial sums
+  for (int p = 0; p < best.parts; ++p) {
+    const LinPart& q = best.part[p];
+    const size_t sums = q.splits > 1 ? (size_t)q.splits * (size_t)q.rows * (size_t)(div_up(a.j, 8) * 8) * 4 : 0;
+    if (sums > best.workspace) best.workspace = sums;
+  }
   for (int k = 0; k < 4; ++k)
     if (best.pack >> k & 1) {
       best.packed[k] = best.workspace;
@@ -1067,16 +1122,62 @@ hipError_t launch_group(const LinArgs& a, bool direct, hipStream_t stream) {
 }
 }  // namespace
 
+namespace {
+const void* skip_bytes(const void* p, int64_t bytes) { return p ? static_cast<const char*>(p) + bytes : p; }
+void* skip_bytes(void* p, int64_t bytes) { return p ? static_cast<char*>(p) + bytes : p; }
+
+// Rows [from, from + rows) of a product.
+LinArgs rows_of(LinArgs a, int64_t from, int64_t rows, int bytes, bool pt) {
+  const int64_t nb = ckpt_blocks(a.j);
+  for (LinProduct& pr : a.prod)
+    if (pr.r > 0) pr.p = skip_bytes(pr.p, (pt ? from : from * pr.ldp) * bytes);
+  a.i = rows;
+  a.out = skip_bytes(a.out, from * a.ldout * bytes);
+  a.mul = skip_bytes(a.mul, from * a.ldmul * bytes);
+  a.residual = skip_bytes(a.residual, from * a.ldres * bytes);
+  a.out_up = skip_bytes(a.out_up, from * a.ldup * bytes);
+  a.codes = static_cast<int8_t*>(skip_bytes(a.codes, from * nb * kCkptBlock));
+  a.exps = static_cast<uint8_t*>(skip_bytes(a.exps, from * nb));
+  a.z_codes = static_cast<const int8_t*>(skip_bytes(a.z_codes, from * nb * kCkptBlock));
+  a.z_exps = static_cast<const uint8_t*>(skip_bytes(a.z_exps, from * nb));
+  a.up_codes = static_cast<const int8_t*>(skip_bytes(a.up_codes, from * nb * kCkptBlock));
+  a.up_exps = static_cast<const uint8_t*>(skip_bytes(a.up_exps, from * nb));
+  return a;
+}
+
+template <typename T>
+hipError_t launch_rows(const LinArgs& a, hipStream_t stream) {
+  // a checkpoint's blocks need 32 columns; without one narrower blocks until there are enough of them
+  const auto launch = [&](auto jb) {
+    const dim3 grid((uint32_t)div_up(a.j, jb())), block(64 * kRowsWaves);
+    if (a.i == 1)
+      k_linear_rows<T, 1, jb()><<<grid, block, 0, stream>>>(a);
+    else if (a.i == 2)
+      k_linear_rows<T, 2, jb()><<<grid, block, 0, stream>>>(a);
+    else if (a.i <= 4)
+      k_linear_rows<T, 4, jb()><<<grid, block, 0, stream>>>(a);
+    else
+      k_linear_rows<T, 8, jb()><<<grid, block, 0, stream>>>(a);
+  };
+  if (a.codes || a.j >= 32 * kComputeUnits)
+    launch(std::integral_constant<int, 32>());
+  else if (a.j >= 16 * kComputeUnits)
+    launch(std::integral_constant<int, 16>());
+  else
+    launch(std::integral_constant<int, 8>());
+  return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
                          hipStream_t stream) {
-  LinArgs a = args;
-  a.splits = plan.splits;
-  a.partial = static_cast<float*>(workspace);
+  LinArgs whole = args;
+  whole.partial = static_cast<float*>(workspace);
   hipError_t e = hipSuccess;
   if (plan.pack) {
     PackJobs jobs{};
     Operand o[4];
-    operands(a, epi, 2, o);
+    operands(whole, epi, 2, o);
     for (int k = 0; k < 4; ++k)
       if (plan.pack >> k & 1) {
         uint16_t* to = reinterpret_cast<uint16_t*>(static_cast<char*>(workspace) + plan.packed[k]);
@@ -1085,52 +1186,39 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
         j = {static_cast<const uint16_t*>(o[k].p), to, o[k].ld, o[k].run, ld / 8, o[k].rows * (ld / 8), 256 / (ld / 8), 256 % (ld / 8)};
         jobs.blocks += (uint32_t)div_up(j.chunks, kPackChunks);
         j.end = jobs.blocks;
-        LinProduct& pr = a.prod[k / 2];
+        LinProduct& pr = whole.prod[k / 2];
         (k % 2 ? pr.q : pr.p) = to;
         (k % 2 ? pr.ldq : pr.ldp) = ld;
       }
     k_pack<<<dim3(jobs.blocks), dim3(256), 0, stream>>>(jobs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
-    using T = decltype(t);
-    if constexpr (std::is_same<T, Bf16>::value) {
-      if (plan.form == kFast) {
-        const dim3 grid((uint32_t)(div_up(a.i, kFastB) * div_up(a.j, kFastB)), (uint32_t)a.splits);
-        k_linear_fast<pt(), qt(), ep()><<<grid, dim3(kFastThreads), 8 * kHalfBytes, stream>>>(a);
-        e = hipGetLastError();
+  int64_t from = 0;
+  for (int p = 0; p < plan.parts && e == hipSuccess; ++p) {
+    const LinPart& part = plan.part[p];
+    LinArgs a = rows_of(whole, from, part.rows, dtype == 1 ? 2 : 4, epi == kEpiStore);
+    a.splits = part.splits;
+    from += part.rows;
+    with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
+      using T = decltype(t);
+      if constexpr (std::is_same<T, Bf16>::value) {
+        if (part.form == kFast) {
+          const dim3 grid((uint32_t)(div_up(a.i, kFastB) * div_up(a.j, kFastB)), (uint32_t)a.splits);
+          k_linear_fast<pt(), qt(), ep()><<<grid, dim3(kFastThreads), 8 * kHalfBytes, stream>>>(a);
+          e = hipGetLastError();
+        }
       }
-    }
-    if constexpr (ep() == kEpiLayer) {
-      if (plan.form == kRows) {
-        // a checkpoint's blocks need 32 columns; without one narrower blocks until there are enough of them
-        const auto launch = [&](auto jb) {
-          const dim3 grid((uint32_t)div_up(a.j, jb())), block(64 * kRowsWaves);
-          if (a.i == 1)
-            k_linear_rows<T, 1, jb()><<<grid, block, 0, stream>>>(a);
-          else if (a.i == 2)
-            k_linear_rows<T, 2, jb()><<<grid, block, 0, stream>>>(a);
-          else if (a.i <= 4)
-            k_linear_rows<T, 4, jb()><<<grid, block, 0, stream>>>(a);
-          else
-            k_linear_rows<T, 8, jb()><<<grid, block, 0, stream>>>(a);
-        };
-        if (a.codes || a.j >= 32 * kComputeUnits)
-          launch(std::integral_constant<int, 32>());
-        else if (a.j >= 16 * kComputeUnits)
-          launch(std::integral_constant<int, 16>());
-        else
-          launch(std::integral_constant<int, 8>());
-        e = hipGetLastError();
+      if constexpr (ep() == kEpiLayer) {
+        if (part.form == kRows) e = launch_rows<T>(a, stream);
       }
-    }
-    if (plan.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
-    if (plan.form == kSmall) e = launch_group<SmallShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
-    if (plan.form == kTiny) e = launch_group<TinyShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
-    if (e != hipSuccess || a.splits <= 1) return;
-    k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
-    e = hipGetLastError();
-  });
+      if (part.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
+      if (part.form == kSmall) e = launch_group<SmallShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
+      if (part.form == kTiny) e = launch_group<TinyShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
+      if (e != hipSuccess || a.splits <= 1) return;
+      k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
+      e = hipGetLastError();
+    });
+  }
   return e;
 }
 
