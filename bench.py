@@ -92,6 +92,9 @@ def parse_args():
                          "issued from the host against the same step replayed from one captured HIP graph of "
                          "the device-driven calls, on the chosen list; print that as the JSON line and exit")
     ap.add_argument("--experts", type=int, default=7)
+    ap.add_argument("--train-mlp", choices=("torch", "checkpointed"), default="torch",
+                    help="--train: the decoder's MLPs as torch modules, or through the fused products with activations "
+                         "saved in 8 bits")
     ap.add_argument("--train-batch", type=int, default=8)
     ap.add_argument("--train-seq", type=int, default=512)
     ap.add_argument("--train-reps", type=int, default=3)
@@ -944,7 +947,7 @@ def bench_train(args, torch, smat) -> int:
     W = max(t, -(-args.warmup // t) * t)
     clip = 1.0
     log(f"building the decoder ({parameter_count(shape) / 1e9:.2f}B params), batch {B} x {S} tokens")
-    model = make_decoder(shape, 0, "cuda")
+    model = make_decoder(shape, 0, "cuda", checkpointed=args.train_mlp == "checkpointed")
     batches = token_batches(shape, B, S, 8, 1, "cuda")
     params = list(model.parameters())
     opt = torch.optim.AdamW(params, lr=2e-5, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-3, fused=True)
@@ -995,6 +998,7 @@ def bench_train(args, torch, smat) -> int:
         for _ in range(W):
             step(mode, False)
     torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
     times = {m: [] for m in modes}
     for r in range(args.train_reps):
         for mode in modes:
@@ -1026,6 +1030,8 @@ def bench_train(args, torch, smat) -> int:
         "overhead_vs_ft": {m: round(med[m] / med["ft"] - 1.0, 4) for m in modes[1:]},
         "tokens_per_s": {m: round(tokens / (med[m] * 1e-3), 1) for m in modes},
         "begin_ms_per_simulated_step": round(begin_ms, 3),
+        "mlp": args.train_mlp,
+        "peak_allocated_gib": round(torch.cuda.max_memory_allocated() / 2 ** 30, 3),
         "config": {"workload": f"decoder d={shape.d} L={shape.layers} heads={shape.heads} ffn={shape.ffn} "
                                f"vocab={shape.vocab} tied, {parameter_count(shape)} params",
                    "batch": B, "seq_len": S, "optimizer": "torch.optim.AdamW(fused=True) lr 2e-5 wd 1e-3",

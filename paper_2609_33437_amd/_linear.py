@@ -61,7 +61,7 @@ def _matrix(t, rows: int, cols: int, like, what: str):
     if not t.is_cuda or t.get_device() != like.get_device():
         raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the same GPU as the call's first matrix")
     ld, step = t.stride()
-    if cols > 1 and step != 1:
+    if cols > 1 and rows > 0 and step != 1:
         raise SmatError(SMAT_ERR_INVALID, f"{what} must have contiguous rows")
     if rows <= 1 or cols == 0:
         ld = cols           # the stride of a single row (or of empty rows) addresses nothing

@@ -81,25 +81,37 @@ class MLP(nn.Module):
         return self.down_proj(F.silu(self.gate_proj(x)) * self.up_proj(x))
 
 
+class CheckpointedMLP(MLP):
+    """The same block through the package's operators: one product each for gate, up and down projection with
+    the activation, the gate and the residual in their epilogues, activations saved in 8 bits."""
+
+    def forward(self, x, residual):
+        from paper_2609_33437_amd import layers
+
+        return layers.gated_mlp(x, self.gate_proj.weight, self.up_proj.weight, self.down_proj.weight, residual=residual)
+
+
 class Block(nn.Module):
-    def __init__(self, d: int, heads: int, ffn: int):
+    def __init__(self, d: int, heads: int, ffn: int, checkpointed: bool = False):
         super().__init__()
         self.input_norm = RMSNorm(d)
         self.attn = Attention(d, heads)
         self.post_norm = RMSNorm(d)
-        self.mlp = MLP(d, ffn)
+        self.mlp = (CheckpointedMLP if checkpointed else MLP)(d, ffn)
 
     def forward(self, x):
         x = x + self.attn(self.input_norm(x))
+        if isinstance(self.mlp, CheckpointedMLP):
+            return self.mlp(self.post_norm(x), x)
         return x + self.mlp(self.post_norm(x))
 
 
 class Decoder(nn.Module):
-    def __init__(self, shape: DecoderShape):
+    def __init__(self, shape: DecoderShape, checkpointed: bool = False):
         super().__init__()
         self.shape = shape
         self.embed = nn.Embedding(shape.vocab, shape.d)
-        self.blocks = nn.ModuleList([Block(shape.d, shape.heads, shape.ffn) for _ in range(shape.layers)])
+        self.blocks = nn.ModuleList([Block(shape.d, shape.heads, shape.ffn, checkpointed) for _ in range(shape.layers)])
         self.norm = RMSNorm(shape.d)
         self.lm_head = nn.Linear(shape.d, shape.vocab, bias=False)
         self.lm_head.weight = self.embed.weight
@@ -117,10 +129,11 @@ class Decoder(nn.Module):
         return F.cross_entropy(logits.float().reshape(-1, logits.shape[-1]), tokens[:, 1:].reshape(-1))
 
 
-def make_decoder(shape: DecoderShape, seed: int, device="cpu") -> Decoder:
-    """Random-initialised decoder (normal(0, 0.02) linear and embedding weights, unit norms)."""
+def make_decoder(shape: DecoderShape, seed: int, device="cpu", checkpointed: bool = False) -> Decoder:
+    """Random-initialised decoder (normal(0, 0.02) linear and embedding weights, unit norms).  With
+    `checkpointed` its MLPs run through the package's operators (GPU only); the weights are the same."""
     g = torch.Generator().manual_seed(seed)
-    model = Decoder(shape)
+    model = Decoder(shape, checkpointed)
     with torch.no_grad():
         for name, p in model.named_parameters():
             if p.dim() >= 2:
