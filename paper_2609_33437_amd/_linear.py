@@ -54,19 +54,20 @@ class ActCheckpoint:
 # ------------------------------------------------------------------ marshalling helpers
 def _matrix(t, rows: int, cols: int, like, what: str):
     """(pointer, row stride) of a matrix [rows, cols] of like's dtype on like's GPU."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise SmatError(SMAT_ERR_INVALID, f"{what} has shape {tuple(t.shape)}, expected ({rows}, {cols})")
-    if t.dtype != like.dtype:
+    if t.dtype is not like.dtype:
         raise SmatError(SMAT_ERR_DTYPE, f"{what} has dtype {t.dtype}, expected {like.dtype}")
-    if not t.is_cuda or t.get_device() != like.get_device():
+    if t.get_device() != like.get_device():     # -1 on the host; like is a GPU tensor
         raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the same GPU as the call's first matrix")
     ld, step = t.stride()
-    if cols > 1 and rows > 0 and step != 1:
-        raise SmatError(SMAT_ERR_INVALID, f"{what} must have contiguous rows")
-    if rows <= 1 or cols == 0:
-        ld = cols           # the stride of a single row (or of empty rows) addresses nothing
-    elif ld < cols:
-        raise SmatError(SMAT_ERR_INVALID, f"rows of {what} overlap (row stride {ld}, {cols} columns)")
+    if step != 1 or ld < cols:
+        if cols > 1 and rows > 0 and step != 1:
+            raise SmatError(SMAT_ERR_INVALID, f"{what} must have contiguous rows")
+        if rows <= 1 or cols == 0:
+            ld = cols           # the stride of a single row (or of empty rows) addresses nothing
+        elif ld < cols:
+            raise SmatError(SMAT_ERR_INVALID, f"rows of {what} overlap (row stride {ld}, {cols} columns)")
     return t.data_ptr(), ld
 
 
@@ -80,11 +81,11 @@ def _first(t, what: str):
 
 
 def _vector(t, n: int, like, what: str) -> int:
-    if t.dim() != 1 or t.shape[0] != n:
+    if t.shape != (n,):
         raise SmatError(SMAT_ERR_INVALID, f"{what} has shape {tuple(t.shape)}, expected ({n},)")
-    if t.dtype != like.dtype:
+    if t.dtype is not like.dtype:
         raise SmatError(SMAT_ERR_DTYPE, f"{what} has dtype {t.dtype}, expected {like.dtype}")
-    if not t.is_cuda or t.get_device() != like.get_device():
+    if t.get_device() != like.get_device():
         raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the same GPU as the call's first matrix")
     if n > 1 and t.stride(0) != 1:
         raise SmatError(SMAT_ERR_INVALID, f"{what} must be contiguous")

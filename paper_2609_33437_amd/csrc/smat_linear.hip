@@ -496,6 +496,7 @@ __device__ __forceinline__ void wait_copies() {
 template <int TI_, int TJ_, int WI_, int WJ_, int G_, int NBUF_>
 struct GroupShape {
   static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, G = G_, NBUF = NBUF_;
+  using Staged = GroupShape<TI_, TJ_, WI_, WJ_, G_, 2>;      // as stages by way of registers need it
   static constexpr int kI = TI * WI, kJ = TJ * WJ, kThreads = 64 * WI * WJ * G;
   static constexpr int kStage = (kI + kJ) * 128;             // bytes
   static constexpr int kSumLd = kJ + 4;                      // floats a row of a group's sums (rows 16 bytes apart in banks)
@@ -939,10 +940,11 @@ void with_form(int dtype, LinEpilogue epi, F&& fn) {
 
 namespace {
 // The tiles a product can be computed with.
-enum TileForm : int32_t { kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4, kRows = 5 };
+enum TileForm : int32_t { kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4, kRows = 5, kNarrow = 6 };
 using MiddleShape = GroupShape<64, 64, 2, 2, 1, 2>;  // 128 x 128, two blocks a compute unit
 using SmallShape = GroupShape<64, 64, 1, 1, 4, 2>;   // 64 x 64, r in four
-using TinyShape = GroupShape<32, 32, 1, 1, 8, 2>;    // 32 x 32, r in eight
+using NarrowShape = GroupShape<32, 64, 1, 1, 4, 3>;  // 32 x 64, r in four
+using TinyShape = GroupShape<16, 32, 1, 1, 4, 3>;    // 16 x 32, r in four, two blocks a compute unit
 
 // What the choice of a tile goes by: the tile, blocks that run together on a compute unit, stages of r that a block
 // takes together (its groups), and measured microseconds: of a stage with as many blocks on each unit, of one with one
@@ -958,24 +960,25 @@ constexpr FormCost cost(int32_t form, double stage, double alone, double rest) {
 // bf16 with stages copied to LDS directly, by how many operands are transposed; the same by way of registers (64 x 64 tiles, one wave a SIMD, took twice as long then and are left out); fp32, whose matrix
 // instructions take 16 times as long.
 constexpr FormCost direct_fast(double stage) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, 10.0}; }
-const FormCost kDirectCosts[3][4] = {
+const FormCost kDirectCosts[3][5] = {
     {direct_fast(1.40), cost<MiddleShape>(kMiddle, 0.90, 0.66, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
-     cost<TinyShape>(kTiny, 0.46, 0.46, 4.4)},
+     cost<NarrowShape>(kNarrow, 0.55, 0.55, 5.0), cost<TinyShape>(kTiny, 0.45, 0.28, 4.2)},
     {direct_fast(1.43), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0), cost<SmallShape>(kSmall, 0.90, 0.90, 5.2),
-     cost<TinyShape>(kTiny, 0.50, 0.50, 4.4)},
+     cost<NarrowShape>(kNarrow, 0.58, 0.58, 5.0), cost<TinyShape>(kTiny, 0.48, 0.30, 4.2)},
     {direct_fast(1.46), cost<MiddleShape>(kMiddle, 0.94, 0.70, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
-     cost<TinyShape>(kTiny, 0.52, 0.52, 4.4)}};
-const FormCost kStagedCosts[3][2] = {{cost<MiddleShape>(kMiddle, 1.15, 1.02, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)},
-                                     {cost<MiddleShape>(kMiddle, 1.31, 1.45, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)},
-                                     {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape>(kTiny, 1.15, 1.15, 6.8)}};
+     cost<NarrowShape>(kNarrow, 0.60, 0.60, 5.0), cost<TinyShape>(kTiny, 0.50, 0.32, 4.2)}};
+const FormCost kStagedCosts[3][2] = {{cost<MiddleShape>(kMiddle, 1.15, 1.02, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)},
+                                     {cost<MiddleShape>(kMiddle, 1.31, 1.45, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)},
+                                     {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)}};
 const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<SmallShape>(kSmall, 2.35, 2.35, 4.5),
-                               cost<TinyShape>(kTiny, 1.1, 1.1, 4.5)};
+                               cost<TinyShape>(kTiny, 0.6, 0.4, 4.5)};
 
 // A product's sizes as the choice sees them: of out, its stages of r, and the microseconds that 65,536 values' epilogue
 // keeps a compute unit's vector units busy.
 struct Sizes {
   int64_t i, j, stages;
   double epilogue;
+  double stream;  // microseconds in which memory delivers the operands
 };
 
 // Microseconds of `splits` ranges of r with tile f.
@@ -989,7 +992,8 @@ double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
   if (left) us += left > kComputeUnits || rounds ? full : f.rest + steps * f.alone + end;
   // the partial sums are written and read, and another launch joins them
   if (splits > 1) us += 2.5 + (double)splits * (double)z.i * (double)z.j * 8.0 / 8e6;
-  return us;
+  // no faster than memory, and between tiles that it bounds the one with the least work
+  return (us > z.stream ? us : z.stream) + 0.1 * us;
 }
 
 // The least-time tile and number of ranges of r by those costs.  Ranges beyond one block a place only cost.
@@ -1067,13 +1071,15 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
     best.parts = 1;
     return best;
   }
-  Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0};
+  Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0, 0.0};
   if (epi == kEpiLayer) z.epilogue = (a.act ? 8.0 : 0.0) + (a.codes ? 6.0 : 0.0) + (a.mul ? 2.0 : 0.0) + (a.residual ? 2.0 : 0.0);
   if (epi == kEpiDgrad) z.epilogue = a.up_codes ? 22.0 : a.z_codes ? 13.0 : 0.0;
   Operand o[4];
   operands(a, epi, bytes, o);
   int32_t off = 0;  // operands whose rows do not start and end on 16 bytes
   double moved = 0.0;
+  z.stream = 4.5;
+  for (int k = 0; k < 4; ++k) z.stream += (double)o[k].rows * (double)o[k].run * bytes / 5.6e6;
   for (int k = 0; k < 4; ++k)
     if (!o[k].fits) {
       off |= 1 << k;
@@ -1081,13 +1087,13 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
     }
   if (dtype == 1) {
     const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
-    const double direct = choose_parts(kDirectCosts[transposed], 4, z, best);
+    const double direct = choose_parts(kDirectCosts[transposed], 5, z, best);
     best.direct = 1;
     if (off) {
       // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
       LinPlan staged{};
       const double through = choose_parts(kStagedCosts[transposed], 2, z, staged);
-      if (through <= direct + 6.0 + moved / 3.0e6)
+      if (through <= direct + 6.0 + moved / 5.0e6)
         best = staged;
       else
         best.pack = off;
@@ -1114,10 +1120,12 @@ namespace {
 template <typename S, typename T, bool PT, bool QT, int EPI>
 hipError_t launch_group(const LinArgs& a, bool direct, hipStream_t stream) {
   const dim3 grid((uint32_t)(div_up(a.i, S::kI) * div_up(a.j, S::kJ)), (uint32_t)a.splits);
-  if (direct)
+  if (direct) {
     k_linear_group<T, PT, QT, EPI, S, true><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
-  else if constexpr (sizeof(typename El<T>::Mem) == 4 || !std::is_same<S, SmallShape>::value)
-    k_linear_group<T, PT, QT, EPI, S, false><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
+  } else if constexpr (sizeof(typename El<T>::Mem) == 4 || std::is_same<S, MiddleShape>::value || std::is_same<S, TinyShape>::value) {
+    using R = typename S::Staged;
+    k_linear_group<T, PT, QT, EPI, R, false><<<grid, dim3(R::kThreads), R::kLds, stream>>>(a);
+  }
   return hipGetLastError();
 }
 }  // namespace
@@ -1213,6 +1221,9 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
       }
       if (part.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
       if (part.form == kSmall) e = launch_group<SmallShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
+      if constexpr (std::is_same<T, Bf16>::value) {
+        if (part.form == kNarrow) e = launch_group<NarrowShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
+      }
       if (part.form == kTiny) e = launch_group<TinyShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
       if (e != hipSuccess || a.splits <= 1) return;
       k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
