@@ -46,12 +46,19 @@ template <>
 struct Frag<float> {
   f32x4 v;
 };
+// Instruction E of a fragment pair's kSteps.  One fp32 instruction after another on the same sum waits for it, so callers
+// go through all sums before the next E.
+template <typename T>
+constexpr int kSteps = 1;
+template <>
+constexpr int kSteps<float> = 4;
+template <int E>
 __device__ __forceinline__ void mma(const Frag<Bf16>& q, const Frag<Bf16>& p, f32x4& c) {
   c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.v, p.v, c, 0, 0, 0);
 }
+template <int E>
 __device__ __forceinline__ void mma(const Frag<float>& q, const Frag<float>& p, f32x4& c) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(q.v[e], p.v[e], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_16x16x4f32(q.v[E], p.v[E], c, 0, 0, 0);
 }
 
 // The fragment of rows row0 .. row0 + 16 of P (of the pair's instruction t of rows row0 .. row0 + 32 of Q)
@@ -277,13 +284,15 @@ struct Copy {
       }
     }
   }
-  // the stream's stage into LDS bytes `lds` .. of this wave's first KB
+  // KB u of the stream's stage (rsrc and deep are the stream's), into LDS bytes `lds` .. of this wave's first KB
+  __device__ __forceinline__ void one(int u, i32x4 rsrc, int32_t deep, uint32_t lds) const {
+    copy_to_lds(rsrc, TRANS || chunk[u] < deep ? off[u] : kNowhere, lds + u * 1024);
+  }
   __device__ __forceinline__ void start(const Stream<T, TRANS, Q>& s, bool on, uint32_t lds) const {
     const i32x4 rsrc = s.rsrc(on);
     const int32_t deep = TRANS ? 0 : s.deep(on);
 #pragma unroll
-    for (int u = 0; u < NI; ++u)
-      copy_to_lds(rsrc, TRANS || chunk[u] < deep ? off[u] : kNowhere, lds + u * 1024);
+    for (int u = 0; u < NI; ++u) one(u, rsrc, deep, lds);
   }
 };
 
@@ -432,7 +441,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) mma(fq[y / 2][y % 2][kk], fp[x][kk], acc[4 * hp + x][y]);
+        for (int y = 0; y < 4; ++y) mma<0>(fq[y / 2][y % 2][kk], fp[x][kk], acc[4 * hp + x][y]);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
@@ -546,21 +555,28 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   Stages todo;
   todo.set(first, last, n0, n);
   char* const mine = smem + group * S::NBUF * S::kStage;
-  // the next stage on its way: into buffer `buf`, or into registers
-  const auto fetch = [&](int buf) {
+  const uint32_t mine_p = (uint32_t)(uintptr_t)(lds_char*)mine + (uint32_t)(w * kNp * 1024);
+  const uint32_t mine_q = (uint32_t)(uintptr_t)(lds_char*)mine + (uint32_t)(S::kI * 128 + w * kNq * 1024);
+  const auto advance = [&] {
     if constexpr (DIRECT) {
-      const uint32_t lds = (uint32_t)(uintptr_t)(lds_char*)mine + (uint32_t)(buf * S::kStage);
-      cp.start(sp, todo.on(), lds + (uint32_t)(w * kNp * 1024));
-      cq.start(sq, todo.on(), lds + (uint32_t)(S::kI * 128 + w * kNq * 1024));
       sp.next();
       sq.next();
     } else {
-      rp.load(todo.on());
-      rq.load(todo.on());
       rp.next();
       rq.next();
     }
     if (todo.advance()) set(a.prod[1], 0);
+  };
+  // the next stage on its way: into buffer `buf`, or into registers
+  const auto fetch = [&](int buf) {
+    if constexpr (DIRECT) {
+      cp.start(sp, todo.on(), mine_p + (uint32_t)(buf * S::kStage));
+      cq.start(sq, todo.on(), mine_q + (uint32_t)(buf * S::kStage));
+    } else {
+      rp.load(todo.on());
+      rq.load(todo.on());
+    }
+    advance();
   };
   const auto place = [&](int buf) {
     if constexpr (!DIRECT) {
@@ -570,16 +586,15 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   };
   f32x4 acc[kXi][kXj] = {};
   Frag<T> fp[2][kXi][2], fq[2][kXj][2];  // [parity][tile][kk]
-  const auto read = [&](int set_, int buf) {
+  // fragment number n of a stage: P's and Q's of kk = 0, then of kk = 1
+  constexpr int kFrags = 2 * (kXi + kXj);
+  const auto read_one = [&](int set_, int buf, int n) {
     const char* s = mine + buf * S::kStage;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-#pragma unroll
-      for (int x = 0; x < kXi; ++x) fp[set_][x][kk] = read_frag<T, PT, false, S::kI>(s, wi + 16 * x, 0, kk);
-#pragma unroll
-      for (int y = 0; y < kXj; ++y)
-        fq[set_][y][kk] = read_frag<T, QT, true, S::kJ>(s + S::kI * 128, wj + 32 * (y / 2), y % 2, kk);
-    }
+    const int kk = n / (kXi + kXj), x = n % (kXi + kXj), y = x - kXi;
+    if (x < kXi)
+      fp[set_][x][kk] = read_frag<T, PT, false, S::kI>(s, wi + 16 * x, 0, kk);
+    else
+      fq[set_][y][kk] = read_frag<T, QT, true, S::kJ>(s + S::kI * 128, wj + 32 * (y / 2), y % 2, kk);
   };
   const auto meet = [&] {
     if (kWaves > 1) {
@@ -589,23 +604,40 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
       asm volatile("" ::: "memory");
     }
   };
-  const auto multiply = [&](int set_) {
+  // a stage's products in kPieces parts: all Q of one row of P's tiles at one kk
+  constexpr int kPieces = 2 * kXi;
+  const auto multiply = [&](int set_, int piece) {
+    const int kk = piece / kXi, x = piece % kXi;
+    const auto all = [&](auto e) {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int x = 0; x < kXi; ++x)
-#pragma unroll
-        for (int y = 0; y < kXj; ++y) mma(fq[set_][y][kk], fp[set_][x][kk], acc[x][y]);
+      for (int y = 0; y < kXj; ++y) mma<decltype(e)::value>(fq[set_][y][kk], fp[set_][x][kk], acc[x][y]);
+    };
+    all(std::integral_constant<int, 0>());
+    if constexpr (kSteps<T> == 4) {
+      all(std::integral_constant<int, 1>());
+      all(std::integral_constant<int, 2>());
+      all(std::integral_constant<int, 3>());
+    }
   };
   int buf = 0;
-  // The fragments `set_` of this step have been asked for.  DIRECT: wait for them and for the next stage, fill their
-  // buffer again, ask for the next fragments, multiply.  Else: put the next stage into the other buffer (whose
-  // fragments every wave had before the last barrier), start loading the one after, wait, and the same.
+  // The fragments `set_` of this step have been asked for.  DIRECT: wait for them and for the next stage, then fill their
+  // buffer again, ask for the next fragments and multiply.  Else: put the next stage into the other buffer (whose
+  // fragments every wave had before the last barrier), start loading the one after, wait, and the same.  The copies and
+  // reads are dealt out between the matrix instructions, which run on while a wave issues them: one after the other
+  // they left the matrix cores idle for half of a stage.
   const auto step = [&](int set_) {
+    i32x4 rsrc_p, rsrc_q;
+    int32_t deep_p = 0, deep_q = 0;
+    uint32_t to_p = 0, to_q = 0;
     if constexpr (DIRECT) {
+      rsrc_p = sp.rsrc(todo.on());
+      rsrc_q = sq.rsrc(todo.on());
+      if (!PT) deep_p = sp.deep(todo.on());
+      if (!QT) deep_q = sq.deep(todo.on());
+      to_p = mine_p + (uint32_t)(buf * S::kStage);
+      to_q = mine_q + (uint32_t)(buf * S::kStage);
       wait_copies<(S::NBUF - 2) * (kNp + kNq)>();
       meet();
-      fetch(buf);
       buf = buf + 1 == S::NBUF ? 0 : buf + 1;
     } else {
       buf ^= 1;
@@ -614,8 +646,23 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       meet();
     }
-    read(set_ ^ 1, buf);
-    multiply(set_);
+#pragma unroll
+    for (int piece = 0; piece < kPieces; ++piece) {
+      multiply(set_, piece);
+      if constexpr (DIRECT) {
+#pragma unroll
+        for (int u = piece * (kNp + kNq) / kPieces; u < (piece + 1) * (kNp + kNq) / kPieces; ++u) {
+          if (u < kNp)
+            cp.one(u < kNp ? u : 0, rsrc_p, deep_p, to_p);
+          else
+            cq.one(u < kNp ? 0 : u - kNp, rsrc_q, deep_q, to_q);
+        }
+      }
+#pragma unroll
+      for (int n = piece * kFrags / kPieces; n < (piece + 1) * kFrags / kPieces; ++n) read_one(set_ ^ 1, buf, n);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (DIRECT) advance();
   };
   if constexpr (DIRECT) {
 #pragma unroll
@@ -628,7 +675,8 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
   meet();
-  read(0, 0);
+#pragma unroll
+  for (int n = 0; n < kFrags; ++n) read_one(0, 0, n);
   for (int64_t s = 0; s < steps; s += 2) {
     step(0);
     if (s + 1 < steps) step(1);
