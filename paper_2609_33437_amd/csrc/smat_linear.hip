@@ -36,6 +36,15 @@ __device__ __forceinline__ int transposed_swizzle(int r) {
   return (Q ? (r & 3) * 4 : ((r & 3) | ((r >> 1) & 4)) * 2) & (kChunks - 1);
 }
 
+// fn(0), fn(1), .., fn(N - 1) with constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void for_each(F&& fn) {
+  if constexpr (I < N) {
+    fn(std::integral_constant<int, I>());
+    for_each<N, I + 1>(fn);
+  }
+}
+
 template <typename T>
 struct Frag;
 template <>
@@ -217,46 +226,118 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ i32x4 make_rsrc(uint64_t p, uint32_t bytes) {
   return i32x4{(int)(uint32_t)p, (int)((uint32_t)(p >> 32) & 0xFFFFu), (int)bytes, 0x00020000};
 }
-// 16 bytes a lane from `offset` of the buffer to LDS bytes lds + 16 lane.
+// 16 bytes a lane from `offset` of the buffer to LDS bytes lds + PLUS + 16 lane.
+template <int PLUS>
 __device__ __forceinline__ void copy_to_lds(i32x4 rsrc, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
-               : "s"(lds), "v"(offset), "s"(rsrc)
-               : "memory");
+               : "s"(lds), "v"(offset), "s"(rsrc), "n"(PLUS)
+               : "memory", "scc");
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer
 
-// Where the next stage of an operand lies: rows (columns) from row0 on, r from r0 on.  Moved on by additions alone; the
-// 64-bit products of a fresh address each stage took longer than the stage's reads.
+constexpr uint32_t kMaxCopies = 63;  // what a wait can leave in flight
+
+// The wave's own reads of LDS have returned.  A builtin, so that the compiler knows; it would wait again later, for
+// reads that were asked for in between too.
+__device__ __forceinline__ void wait_reads() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0), any vmcnt and expcnt
+  asm volatile("" ::: "memory");
+}
+// All but N of its copies have landed, and its reads have returned.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N <= (int)kMaxCopies, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  wait_reads();
+}
+
+// Where the next stage of an operand lies, as the copies take it.
 template <typename T, bool TRANS, bool Q>
 struct Stream {
   static constexpr int kBytes = El<T>::kBytes, kDeep = 128 / kBytes;
-  uint64_t base;
-  uint64_t step;
-  int64_t left;  // r that are left; transposed: bytes up to the operand's end, to whole 16
-  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t rows, int64_t r0) {
-    const int64_t ld = Q ? pr.ldq : pr.ldp;
+  uint64_t base, step;
+  uint32_t bytes;  // offsets past them read as zeros
+  // rows (columns) from row0 on, stage number `at` of the product
+  __device__ __forceinline__ void set(const LinProduct& pr, int64_t row0, int64_t at) {
+    const int64_t ld = Q ? pr.ldq : pr.ldp, r0 = at * kDeep;
     base = reinterpret_cast<uint64_t>(Q ? pr.q : pr.p) + (uint64_t)(TRANS ? r0 * ld + row0 : row0 * ld + r0) * kBytes;
+    step = TRANS ? (uint64_t)ld * 128 : 128;
+    bytes = 0x7FFFFFF0u;
+  }
+  // the stage has `deep` r and is the product's last: a transposed one ends with its last row's last column, to whole 16
+  __device__ __forceinline__ void end(const LinProduct& pr, int64_t row0, int64_t rows, int32_t deep) {
     if constexpr (TRANS) {
-      step = (uint64_t)ld * 128;
-      left = r0 < pr.r && row0 < rows ? (((pr.r - r0 - 1) * ld + rows - row0) * kBytes + 15) & ~(int64_t)15 : 0;
-    } else {
-      step = 128;
-      left = pr.r - r0;
+      const int64_t some = row0 < rows ? (((deep - 1) * (Q ? pr.ldq : pr.ldp) + rows - row0) * kBytes + 15) & ~(int64_t)15 : 0;
+      bytes = (uint32_t)(some < 0x7FFFFFF0 ? some : 0x7FFFFFF0);
     }
   }
-  __device__ __forceinline__ void next() {
-    base += step;
-    left -= TRANS ? (int64_t)step : (int64_t)kDeep;
+  __device__ __forceinline__ i32x4 rsrc() const { return make_rsrc(base, bytes); }
+};
+
+// The stages of r that a block (a group) takes, in the order of the sum: those of prod[0], then those of prod[1].  Runs of
+// whole stages are passed by additions alone, since what a stage adds to a wave's instructions delays its matrix
+// instructions; a product's last stage and the end of the share are set up apart.
+// set(product) deals the operands' rows to the copies, end(r) cuts the copies of direct operands to the first r of the stage.
+template <typename T, bool PT, bool QT>
+struct Feed {
+  static constexpr int kDeep = 128 / El<T>::kBytes;
+  Stream<T, PT, false> p;
+  Stream<T, QT, true> q;
+  int64_t i0, j0;
+  int32_t plain;              // stages left of this run
+  int32_t run, at, last, second;  // its length, its first stage and the share's end in its product, whether that is prod[1]
+  int32_t last_second;        // the share's end in prod[1]
+
+  template <typename Set, typename End>
+  __device__ __forceinline__ void begin(const LinArgs& a, int64_t i0_, int64_t j0_, int64_t first, int64_t end_, int64_t n0,
+                                        Set set, End end) {
+    i0 = i0_;
+    j0 = j0_;
+    second = first >= n0 && a.prod[1].r > 0;
+    at = (int32_t)(second ? first - n0 : first);
+    last_second = (int32_t)(end_ - n0);
+    last = second ? last_second : (int32_t)(end_ < n0 ? end_ : n0);
+    set(a.prod[second]);
+    next_run(a, n0, set, end);
   }
-  // offsets past the bytes read as zeros; `on`: there is a stage
-  __device__ __forceinline__ i32x4 rsrc(bool on) const {
-    const int64_t some = left < 0x7FFFFFF0 ? left : 0x7FFFFFF0;
-    return make_rsrc(base, TRANS ? (on && some > 0 ? (uint32_t)some : 0u) : 0x7FFFFFF0u);
+  template <typename Set, typename End>
+  __device__ __forceinline__ void next_run(const LinArgs& a, int64_t n0, Set set, End end) {
+    if (at >= last && !second && last_second > 0) {
+      second = 1;
+      at = 0;
+      last = last_second;
+      set(a.prod[1]);
+    }
+    const LinProduct& pr = a.prod[second];
+    p.set(pr, i0, at);
+    q.set(pr, j0, at);
+    if (at >= last) {  // none is left: what is copied from here on are zeros
+      p.bytes = q.bytes = 0;
+      p.step = q.step = 0;
+      end(0);
+      run = INT32_MAX;
+    } else {
+      const int32_t whole = (int32_t)((pr.r + kDeep - 1) / kDeep) - 1;  // the product's last stage
+      run = (whole < last ? whole : last) - at;
+      if (run <= 0) {
+        const int32_t deep = (int32_t)(pr.r - (int64_t)at * kDeep);
+        p.end(pr, i0, a.i, deep);
+        q.end(pr, j0, a.j, deep);
+        end(deep);
+        run = 1;
+      }
+    }
+    plain = run;
   }
-  // direct: r of the stage that exist
-  __device__ __forceinline__ int32_t deep(bool on) const {
-    return on && left > 0 ? (int32_t)(left < kDeep ? left : kDeep) : 0;
+  template <typename Set, typename End>
+  __device__ __forceinline__ void advance(const LinArgs& a, int64_t n0, Set set, End end) {
+    p.base += p.step;
+    q.base += q.step;
+    if (--plain == 0) {
+      at += run;
+      next_run(a, n0, set, end);
+    }
   }
 };
 
@@ -265,7 +346,11 @@ template <typename T, bool TRANS, bool Q, int B, int NI>
 struct Copy {
   static constexpr int kBytes = El<T>::kBytes, kChunk = 16 / kBytes;
   uint32_t off[NI];  // this lane's bytes from the stream's place
-  int32_t chunk[NI]; // its first r of the stage (direct)
+  static __device__ __forceinline__ int chunk_of(int u, int wave, int& row) {
+    const int lane = (int)threadIdx.x & 63;
+    row = (wave * NI + u) * 8 + lane / 8;
+    return (lane % 8) ^ direct_swizzle<Q>(row);
+  }
   // rows: the operand's from the stream's first on
   __device__ __forceinline__ void set(const LinProduct& pr, int skip, int64_t rows, int wave) {
     const int lane = (int)threadIdx.x & 63;
@@ -273,26 +358,39 @@ struct Copy {
 #pragma unroll
     for (int u = 0; u < NI; ++u) {
       if constexpr (!TRANS) {
-        const int row = (wave * NI + u) * 8 + lane / 8, c = (lane % 8) ^ direct_swizzle<Q>(row);
-        chunk[u] = c * kChunk;
+        int row;
+        const int c = chunk_of(u, wave, row);
         off[u] = skip + row < rows ? (uint32_t)(skip + row) * ld * kBytes + (uint32_t)c * 16 : kNowhere;
       } else {
         constexpr int kChunks = B / kChunk;
         const int rr = (wave * NI + u) * (64 / kChunks) + lane / kChunks;
         const int c = (lane % kChunks) ^ transposed_swizzle<T, Q, B>(rr);
-        off[u] = (uint32_t)rr * ld * kBytes + (uint32_t)(skip * kBytes + c * 16);
+        // chunks lie inside their row's stride (a multiple of 16 bytes) as long as their first column does
+        off[u] = skip + c * kChunk < rows ? (uint32_t)rr * ld * kBytes + (uint32_t)(skip * kBytes + c * 16) : kNowhere;
       }
     }
   }
-  // KB u of the stream's stage (rsrc and deep are the stream's), into LDS bytes `lds` .. of this wave's first KB
-  __device__ __forceinline__ void one(int u, i32x4 rsrc, int32_t deep, uint32_t lds) const {
-    copy_to_lds(rsrc, TRANS || chunk[u] < deep ? off[u] : kNowhere, lds + u * 1024);
-  }
-  __device__ __forceinline__ void start(const Stream<T, TRANS, Q>& s, bool on, uint32_t lds) const {
-    const i32x4 rsrc = s.rsrc(on);
-    const int32_t deep = TRANS ? 0 : s.deep(on);
+  // The stage has only `left` r: the chunks past them lie nowhere, here and until set().
+  __device__ __forceinline__ void end(int32_t left, int wave) {
+    if constexpr (!TRANS) {
 #pragma unroll
-    for (int u = 0; u < NI; ++u) one(u, rsrc, deep, lds);
+      for (int u = 0; u < NI; ++u) {
+        int row;
+        if (chunk_of(u, wave, row) * kChunk >= left) off[u] = kNowhere;
+      }
+    }
+  }
+  // KB U of the stage at rsrc into LDS bytes `lds` .. of this wave's first KB
+  template <int U>
+  __device__ __forceinline__ void one(i32x4 rsrc, uint32_t lds) const {
+    copy_to_lds<U * 1024>(rsrc, off[U], lds);
+  }
+  template <int U = 0>
+  __device__ __forceinline__ void all(i32x4 rsrc, uint32_t lds) const {
+    if constexpr (U < NI) {
+      one<U>(rsrc, lds);
+      all<U + 1>(rsrc, lds);
+    }
   }
 };
 
@@ -348,24 +446,6 @@ struct Staged {
   }
 };
 
-// The stages of r that a wave copies, in the order of the sum: those of prod[0], then those of prod[1].
-struct Stages {
-  int32_t todo, here, more;  // stages left, left of this product, of prod[1]
-  __device__ __forceinline__ void set(int64_t first, int64_t last, int64_t n0, int64_t n) {
-    todo = (int32_t)(last - first);
-    here = (int32_t)(first >= n0 ? n - first : n0 - first);
-    more = (int32_t)(n - n0);
-  }
-  __device__ __forceinline__ bool on() const { return todo > 0; }
-  // whether the next stage is the first of prod[1]
-  __device__ __forceinline__ bool advance() {
-    --todo;
-    if (--here != 0 || todo <= 0) return false;
-    here = more;
-    return true;
-  }
-};
-
 // Tile `b` of ti x tj in an order that keeps the tiles that run together close: consecutive blocks go to the
 // eight XCDs in turn, so each XCD takes one run of the order, in columns four tiles high.
 __device__ __forceinline__ void tile_place(uint32_t b, uint32_t ti, uint32_t tj, uint32_t& i, uint32_t& j) {
@@ -388,32 +468,30 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
   const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
-  Stream<T, PT, false> sp;
-  Stream<T, QT, true> sq;
+  Feed<T, PT, QT> feed;
   Copy<T, PT, false, kFastHalf, 2> cp[2];
   Copy<T, QT, true, kFastHalf, 2> cq[2];
-  const auto set = [&](const LinProduct& pr, int64_t r0) {
-    sp.set(pr, i0, a.i, r0);
-    sq.set(pr, j0, a.j, r0);
+  const auto set = [&](const LinProduct& pr) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       cp[h].set(pr, h * kFastHalf, a.i - i0, wave);
       cq[h].set(pr, h * kFastHalf, a.j - j0, wave);
     }
   };
-  set(a.prod[first >= n0], (first >= n0 ? first - n0 : first) * 64);
-  Stages todo;
-  todo.set(first, last, n0, n);
+  const auto end = [&](int32_t deep) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      cp[h].end(deep, wave);
+      cq[h].end(deep, wave);
+    }
+  };
+  feed.begin(a, i0, j0, first, last, n0, set, end);
   const uint32_t mine = lds0 + (uint32_t)wave * 2048;
   const auto copy_p = [&](int h, int buf) {  // half h of the next stage to copy
-    cp[h].start(sp, todo.on(), mine + (buf * 4 + h) * kHalfBytes);
+    cp[h].all(feed.p.rsrc(), mine + (buf * 4 + h) * kHalfBytes);
   };
-  const auto copy_q = [&](int h, int buf) { cq[h].start(sq, todo.on(), mine + (buf * 4 + 2 + h) * kHalfBytes); };
-  const auto advance = [&] {
-    sp.next();
-    sq.next();
-    if (todo.advance()) set(a.prod[1], 0);
-  };
+  const auto copy_q = [&](int h, int buf) { cq[h].all(feed.q.rsrc(), mine + (buf * 4 + 2 + h) * kHalfBytes); };
+  const auto advance = [&] { feed.advance(a, n0, set, end); };
   f32x4 acc[8][4] = {};  // [half of P, tile][half of Q, tile]
   Frag<T> fp[4][2], fq[2][2][2];  // [tile][kk], [half][tile][kk]
   const auto read_p = [&](int h, int buf) {
@@ -431,7 +509,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
       for (int kk = 0; kk < 2; ++kk) fq[h][y][kk] = read_frag<T, QT, true, kFastHalf>(s, wj, y, kk);
   };
   const auto multiply = [&](int hp) {
-    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+    wait_copies<8>();
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
@@ -475,9 +553,9 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   asm volatile("" ::: "memory");
   if (wave >= 4) __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_sched_barrier(0);
-  for (int64_t s = first; s < last; s += 2) {
+  for (int32_t s = (int32_t)(last - first); s > 0; s -= 2) {
     stage(0);
-    if (s + 1 < last) stage(1);
+    if (s > 1) stage(1);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy outlives the block's LDS
   if (wave < 4) __builtin_amdgcn_s_barrier();
@@ -494,14 +572,6 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
 //
 // A group's stages lie in NBUF buffers.  While a wave multiplies the fragments of one stage it reads those of the
 // next from LDS; a buffer is filled again once every wave of the group has read it.
-constexpr uint32_t kMaxCopies = 63;  // what a wait can leave in flight
-
-template <int N>
-__device__ __forceinline__ void wait_copies() {
-  static_assert(N <= (int)kMaxCopies, "the counter's range");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
-}
-
 template <int TI_, int TJ_, int WI_, int WJ_, int G_, int NBUF_>
 struct GroupShape {
   static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, G = G_, NBUF = NBUF_;
@@ -533,48 +603,50 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   const int64_t first = split_start(n, share, a.splits * S::G), last = split_start(n, share + 1, a.splits * S::G);
   // every group of a block takes the same number of steps, so that barriers meet (shares differ by one stage)
   const int64_t steps = (n + a.splits * S::G - 1) / (a.splits * S::G);
-  Stream<T, PT, false> sp;
-  Stream<T, QT, true> sq;
+  Feed<T, PT, QT> feed;
   Copy<T, PT, false, S::kI, kNp> cp;
   Copy<T, QT, true, S::kJ, kNq> cq;
   Staged<T, PT, false, S::kI, kNp> rp;
   Staged<T, QT, true, S::kJ, kNq> rq;
-  const auto set = [&](const LinProduct& pr, int64_t r0) {
-    if constexpr (DIRECT) {
-      sp.set(pr, i0, a.i, r0);
-      sq.set(pr, j0, a.j, r0);
-      cp.set(pr, 0, a.i - i0, w);
-      cq.set(pr, 0, a.j - j0, w);
-    } else {
-      rp.set(pr, i0, a.i, r0, w);
-      rq.set(pr, j0, a.j, r0, w);
-    }
+  const auto set = [&](const LinProduct& pr) {
+    cp.set(pr, 0, a.i - i0, w);
+    cq.set(pr, 0, a.j - j0, w);
   };
-  const bool second = first >= n0 && a.prod[1].r > 0;
-  set(a.prod[second], (second ? first - n0 : first) * kDeep);
-  Stages todo;
-  todo.set(first, last, n0, n);
+  const auto end = [&](int32_t deep) {
+    cp.end(deep, w);
+    cq.end(deep, w);
+  };
+  // by way of registers: the next stage's number, and of its product
+  int64_t at = first;
+  const auto stage_of = [&] {
+    const bool second = at >= n0 && a.prod[1].r > 0;
+    rp.set(a.prod[second], i0, a.i, (second ? at - n0 : at) * kDeep, w);
+    rq.set(a.prod[second], j0, a.j, (second ? at - n0 : at) * kDeep, w);
+  };
+  if constexpr (DIRECT)
+    feed.begin(a, i0, j0, first, last, n0, set, end);
+  else
+    stage_of();
   char* const mine = smem + group * S::NBUF * S::kStage;
   const uint32_t mine_p = (uint32_t)(uintptr_t)(lds_char*)mine + (uint32_t)(w * kNp * 1024);
   const uint32_t mine_q = (uint32_t)(uintptr_t)(lds_char*)mine + (uint32_t)(S::kI * 128 + w * kNq * 1024);
   const auto advance = [&] {
     if constexpr (DIRECT) {
-      sp.next();
-      sq.next();
+      feed.advance(a, n0, set, end);
     } else {
       rp.next();
       rq.next();
+      if (++at == n0) stage_of();
     }
-    if (todo.advance()) set(a.prod[1], 0);
   };
   // the next stage on its way: into buffer `buf`, or into registers
   const auto fetch = [&](int buf) {
     if constexpr (DIRECT) {
-      cp.start(sp, todo.on(), mine_p + (uint32_t)(buf * S::kStage));
-      cq.start(sq, todo.on(), mine_q + (uint32_t)(buf * S::kStage));
+      cp.all(feed.p.rsrc(), mine_p + (uint32_t)(buf * S::kStage));
+      cq.all(feed.q.rsrc(), mine_q + (uint32_t)(buf * S::kStage));
     } else {
-      rp.load(todo.on());
-      rq.load(todo.on());
+      rp.load(at < last);
+      rq.load(at < last);
     }
     advance();
   };
@@ -627,13 +699,10 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   // they left the matrix cores idle for half of a stage.
   const auto step = [&](int set_) {
     i32x4 rsrc_p, rsrc_q;
-    int32_t deep_p = 0, deep_q = 0;
     uint32_t to_p = 0, to_q = 0;
     if constexpr (DIRECT) {
-      rsrc_p = sp.rsrc(todo.on());
-      rsrc_q = sq.rsrc(todo.on());
-      if (!PT) deep_p = sp.deep(todo.on());
-      if (!QT) deep_q = sq.deep(todo.on());
+      rsrc_p = feed.p.rsrc();
+      rsrc_q = feed.q.rsrc();
       to_p = mine_p + (uint32_t)(buf * S::kStage);
       to_q = mine_q + (uint32_t)(buf * S::kStage);
       wait_copies<(S::NBUF - 2) * (kNp + kNq)>();
@@ -643,25 +712,25 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
       buf ^= 1;
       place(buf);
       fetch(buf);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      wait_reads();
       meet();
     }
-#pragma unroll
-    for (int piece = 0; piece < kPieces; ++piece) {
+    for_each<kPieces>([&](auto piece) {
+      constexpr int kFirst = piece * (kNp + kNq) / kPieces, kEnd = (piece + 1) * (kNp + kNq) / kPieces;
       multiply(set_, piece);
       if constexpr (DIRECT) {
-#pragma unroll
-        for (int u = piece * (kNp + kNq) / kPieces; u < (piece + 1) * (kNp + kNq) / kPieces; ++u) {
-          if (u < kNp)
-            cp.one(u < kNp ? u : 0, rsrc_p, deep_p, to_p);
+        for_each<kEnd - kFirst>([&](auto d) {
+          constexpr int u = kFirst + d;
+          if constexpr (u < kNp)
+            cp.template one<u>(rsrc_p, to_p);
           else
-            cq.one(u < kNp ? 0 : u - kNp, rsrc_q, deep_q, to_q);
-        }
+            cq.template one<u - kNp>(rsrc_q, to_q);
+        });
       }
 #pragma unroll
       for (int n = piece * kFrags / kPieces; n < (piece + 1) * kFrags / kPieces; ++n) read_one(set_ ^ 1, buf, n);
       __builtin_amdgcn_sched_barrier(0);
-    }
+    });
     if constexpr (DIRECT) advance();
   };
   if constexpr (DIRECT) {
@@ -672,14 +741,14 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
     fetch(0);
     place(0);
     fetch(1);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wait_reads();
   }
   meet();
 #pragma unroll
   for (int n = 0; n < kFrags; ++n) read_one(0, 0, n);
-  for (int64_t s = 0; s < steps; s += 2) {
+  for (int32_t s = 0; s < (int32_t)steps; s += 2) {
     step(0);
-    if (s + 1 < steps) step(1);
+    if (s + 1 < (int32_t)steps) step(1);
   }
   wait_copies<0>();  // no copy outlives the block's LDS, or lands on the sums
   if constexpr (S::G == 1) {
