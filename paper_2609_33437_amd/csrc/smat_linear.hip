@@ -1057,8 +1057,9 @@ void with_form(int dtype, LinEpilogue epi, F&& fn) {
 
 namespace {
 // The tiles a product can be computed with.
-enum TileForm : int32_t { kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4, kRows = 5, kNarrow = 6 };
+enum TileForm : int32_t { kFast = 1, kMiddle = 2, kSmall = 3, kTiny = 4, kRows = 5, kNarrow = 6, kPair = 7 };
 using MiddleShape = GroupShape<64, 64, 2, 2, 1, 2>;  // 128 x 128, two blocks a compute unit
+using PairShape = GroupShape<64, 64, 2, 2, 2, 2>;     // 128 x 128, r in two
 using SmallShape = GroupShape<64, 64, 1, 1, 4, 2>;   // 64 x 64, r in four
 using NarrowShape = GroupShape<32, 64, 1, 1, 4, 3>;  // 32 x 64, r in four
 using TinyShape = GroupShape<16, 32, 1, 1, 4, 3>;    // 16 x 32, r in four, two blocks a compute unit
@@ -1077,13 +1078,16 @@ constexpr FormCost cost(int32_t form, double stage, double alone, double rest) {
 // bf16 with stages copied to LDS directly, by how many operands are transposed; the same by way of registers (64 x 64 tiles, one wave a SIMD, took twice as long then and are left out); fp32, whose matrix
 // instructions take 16 times as long.
 constexpr FormCost direct_fast(double stage) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, 10.0}; }
-const FormCost kDirectCosts[3][5] = {
+const FormCost kDirectCosts[3][6] = {
     {direct_fast(1.40), cost<MiddleShape>(kMiddle, 0.90, 0.66, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
-     cost<NarrowShape>(kNarrow, 0.55, 0.55, 5.0), cost<TinyShape>(kTiny, 0.45, 0.28, 4.2)},
+     cost<NarrowShape>(kNarrow, 0.55, 0.55, 5.0), cost<TinyShape>(kTiny, 0.45, 0.28, 4.2),
+     cost<PairShape>(kPair, 0.95, 0.95, 7.2)},
     {direct_fast(1.43), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0), cost<SmallShape>(kSmall, 0.90, 0.90, 5.2),
-     cost<NarrowShape>(kNarrow, 0.58, 0.58, 5.0), cost<TinyShape>(kTiny, 0.48, 0.30, 4.2)},
+     cost<NarrowShape>(kNarrow, 0.58, 0.58, 5.0), cost<TinyShape>(kTiny, 0.48, 0.30, 4.2),
+     cost<PairShape>(kPair, 0.95, 0.95, 7.2)},
     {direct_fast(1.46), cost<MiddleShape>(kMiddle, 0.94, 0.70, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
-     cost<NarrowShape>(kNarrow, 0.60, 0.60, 5.0), cost<TinyShape>(kTiny, 0.50, 0.32, 4.2)}};
+     cost<NarrowShape>(kNarrow, 0.60, 0.60, 5.0), cost<TinyShape>(kTiny, 0.50, 0.32, 4.2),
+     cost<PairShape>(kPair, 0.95, 0.95, 7.2)}};
 const FormCost kStagedCosts[3][2] = {{cost<MiddleShape>(kMiddle, 1.15, 1.02, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)},
                                      {cost<MiddleShape>(kMiddle, 1.31, 1.45, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)},
                                      {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)}};
@@ -1204,7 +1208,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
     }
   if (dtype == 1) {
     const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
-    const double direct = choose_parts(kDirectCosts[transposed], 5, z, best);
+    const double direct = choose_parts(kDirectCosts[transposed], 6, z, best);
     best.direct = 1;
     if (off) {
       // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
@@ -1339,6 +1343,7 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
       if (part.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
       if (part.form == kSmall) e = launch_group<SmallShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
       if constexpr (std::is_same<T, Bf16>::value) {
+        if (part.form == kPair) e = launch_group<PairShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
         if (part.form == kNarrow) e = launch_group<NarrowShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
       }
       if (part.form == kTiny) e = launch_group<TinyShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
