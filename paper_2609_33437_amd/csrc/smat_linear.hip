@@ -940,12 +940,12 @@ __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
 }
 
 // ---------------------------------------------------------------- copies on 16-byte rows
-// bf16 operands off 16-byte rows, copied to rows of whole 16 bytes with zeros at their ends: every chunk is read once
-// at its element's address and written once.  A block takes kPackChunks of one operand.
+// Operands off 16-byte rows, copied to rows of whole 16 bytes with zeros at their ends: every chunk is read once at its
+// element's address and written once.  A block takes kPackChunks of one operand.
 constexpr int kPackChunks = 1024;
 struct PackJob {
-  const uint16_t* from;
-  uint16_t* to;
+  const void* from;
+  void* to;
   int64_t ld, run, across, chunks;  // chunks a row, and in all
   int64_t rows_on, chunks_on;       // from a thread's chunk to its next, 256 further
   uint32_t end;                     // the first block after this operand's
@@ -956,7 +956,10 @@ struct PackJobs {
   uint32_t blocks;
 };
 
+template <typename T>
 __global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
+  using Mem = typename El<T>::Mem;
+  constexpr int kChunk = 16 / El<T>::kBytes;
   int k = 0;
   while (k + 1 < jobs.count && blockIdx.x >= jobs.job[k].end) ++k;
   const PackJob& j = jobs.job[k];
@@ -966,8 +969,9 @@ __global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
   u32x4 x[kPackChunks / 256];
 #pragma unroll
   for (int u = 0; u < kPackChunks / 256; ++u) {
-    const int64_t left = j.run - c * 8;
-    if (first + u * 256 < j.chunks) x[u] = load_chunk<Bf16>(j.from + row * j.ld + c * 8, (int32_t)(left < 8 ? left : 8));
+    const int64_t left = j.run - c * kChunk;
+    if (first + u * 256 < j.chunks)
+      x[u] = load_chunk<T>(static_cast<const Mem*>(j.from) + row * j.ld + c * kChunk, (int32_t)(left < kChunk ? left : kChunk));
     row += j.rows_on;
     c += j.chunks_on;
     if (c >= j.across) {
@@ -977,7 +981,7 @@ __global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
   }
 #pragma unroll
   for (int u = 0; u < kPackChunks / 256; ++u)
-    if (first + u * 256 < j.chunks) *reinterpret_cast<u32x4*>(j.to + (first + u * 256) * 8) = x[u];
+    if (first + u * 256 < j.chunks) static_cast<u32x4*>(j.to)[first + u * 256] = x[u];
 }
 
 // ---------------------------------------------------------------- column sums
@@ -1075,8 +1079,9 @@ template <typename S>
 constexpr FormCost cost(int32_t form, double stage, double alone, double rest) {
   return {form, S::kI, S::kJ, S::kResident, S::G, stage, alone, rest};
 }
-// bf16 with stages copied to LDS directly, by how many operands are transposed; the same by way of registers (64 x 64 tiles, one wave a SIMD, took twice as long then and are left out); fp32, whose matrix
-// instructions take 16 times as long.
+// bf16 with stages copied to LDS directly, by how many operands are transposed; the same by way of registers, where
+// the other tiles are slower than these at every size tried (64 x 64, one wave a SIMD, twice as long); fp32 both ways,
+// whose matrix instructions take 16 times as long.
 constexpr FormCost direct_fast(double stage) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, 10.0}; }
 const FormCost kDirectCosts[3][6] = {
     {direct_fast(1.40), cost<MiddleShape>(kMiddle, 0.90, 0.66, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
@@ -1093,6 +1098,7 @@ const FormCost kStagedCosts[3][2] = {{cost<MiddleShape>(kMiddle, 1.15, 1.02, 9.0
                                      {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)}};
 const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<SmallShape>(kSmall, 2.35, 2.35, 4.5),
                                cost<TinyShape>(kTiny, 0.6, 0.4, 4.5)};
+const FormCost kFp32StagedCosts[] = {cost<MiddleShape>(kMiddle, 4.65, 2.5, 7.0), cost<TinyShape::Staged>(kTiny, 1.2, 0.75, 5.0)};
 
 // A product's sizes as the choice sees them: of out, its stages of r, and the microseconds that 65,536 values' epilogue
 // keeps a compute unit's vector units busy.
@@ -1206,22 +1212,17 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       off |= 1 << k;
       moved += 2.0 * (double)o[k].rows * (double)o[k].run * bytes;
     }
-  if (dtype == 1) {
-    const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
-    const double direct = choose_parts(kDirectCosts[transposed], 6, z, best);
-    best.direct = 1;
-    if (off) {
-      // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
-      LinPlan staged{};
-      const double through = choose_parts(kStagedCosts[transposed], 2, z, staged);
-      if (through <= direct + 6.0 + moved / 5.0e6)
-        best = staged;
-      else
-        best.pack = off;
-    }
-  } else {
-    choose_parts(kFp32Costs, 3, z, best);
-    best.direct = off == 0;
+  const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
+  const double direct = dtype == 1 ? choose_parts(kDirectCosts[transposed], 6, z, best) : choose_parts(kFp32Costs, 3, z, best);
+  best.direct = 1;
+  if (off) {
+    // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
+    LinPlan staged{};
+    const double through = dtype == 1 ? choose_parts(kStagedCosts[transposed], 2, z, staged) : choose_parts(kFp32StagedCosts, 2, z, staged);
+    if (through <= direct + 6.0 + moved / 5.0e6)
+      best = staged;
+    else
+      best.pack = off;
   }
   // the parts run one after the other and share the place of their partial sums
   for (int p = 0; p < best.parts; ++p) {
@@ -1243,7 +1244,7 @@ hipError_t launch_group(const LinArgs& a, bool direct, hipStream_t stream) {
   const dim3 grid((uint32_t)(div_up(a.i, S::kI) * div_up(a.j, S::kJ)), (uint32_t)a.splits);
   if (direct) {
     k_linear_group<T, PT, QT, EPI, S, true><<<grid, dim3(S::kThreads), S::kLds, stream>>>(a);
-  } else if constexpr (sizeof(typename El<T>::Mem) == 4 || std::is_same<S, MiddleShape>::value || std::is_same<S, TinyShape>::value) {
+  } else if constexpr (std::is_same<S, MiddleShape>::value || std::is_same<S, TinyShape>::value) {
     using R = typename S::Staged;
     k_linear_group<T, PT, QT, EPI, R, false><<<grid, dim3(R::kThreads), R::kLds, stream>>>(a);
   }
@@ -1300,32 +1301,33 @@ hipError_t launch_rows(const LinArgs& a, hipStream_t stream) {
 
 hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
                          hipStream_t stream) {
+  const int bytes = dtype == 1 ? 2 : 4;
   LinArgs whole = args;
   whole.partial = static_cast<float*>(workspace);
   hipError_t e = hipSuccess;
   if (plan.pack) {
     PackJobs jobs{};
     Operand o[4];
-    operands(whole, epi, 2, o);
+    operands(whole, epi, bytes, o);
     for (int k = 0; k < 4; ++k)
       if (plan.pack >> k & 1) {
-        uint16_t* to = reinterpret_cast<uint16_t*>(static_cast<char*>(workspace) + plan.packed[k]);
-        const int64_t ld = packed_ld(o[k].run, 2);
+        void* to = static_cast<char*>(workspace) + plan.packed[k];
+        const int64_t ld = packed_ld(o[k].run, bytes), across = ld * bytes / 16;
         PackJob& j = jobs.job[jobs.count++];
-        j = {static_cast<const uint16_t*>(o[k].p), to, o[k].ld, o[k].run, ld / 8, o[k].rows * (ld / 8), 256 / (ld / 8), 256 % (ld / 8)};
+        j = {o[k].p, to, o[k].ld, o[k].run, across, o[k].rows * across, 256 / across, 256 % across};
         jobs.blocks += (uint32_t)div_up(j.chunks, kPackChunks);
         j.end = jobs.blocks;
         LinProduct& pr = whole.prod[k / 2];
         (k % 2 ? pr.q : pr.p) = to;
         (k % 2 ? pr.ldq : pr.ldp) = ld;
       }
-    k_pack<<<dim3(jobs.blocks), dim3(256), 0, stream>>>(jobs);
+    with_element(dtype, [&](auto t) { k_pack<decltype(t)><<<dim3(jobs.blocks), dim3(256), 0, stream>>>(jobs); });
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   int64_t from = 0;
   for (int p = 0; p < plan.parts && e == hipSuccess; ++p) {
     const LinPart& part = plan.part[p];
-    LinArgs a = rows_of(whole, from, part.rows, dtype == 1 ? 2 : 4, epi == kEpiStore);
+    LinArgs a = rows_of(whole, from, part.rows, bytes, epi == kEpiStore);
     a.splits = part.splits;
     from += part.rows;
     with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
