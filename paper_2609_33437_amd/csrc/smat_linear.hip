@@ -1091,21 +1091,26 @@ const FormCost kDirectCosts[3][6] = {
      cost<NarrowShape>(kNarrow, 0.58, 0.58, 5.0), cost<TinyShape>(kTiny, 0.48, 0.30, 4.2),
      cost<PairShape>(kPair, 0.95, 0.95, 7.2)},
     {direct_fast(1.46), cost<MiddleShape>(kMiddle, 0.94, 0.70, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
-     cost<NarrowShape>(kNarrow, 0.60, 0.60, 5.0), cost<TinyShape>(kTiny, 0.50, 0.32, 4.2),
+     cost<NarrowShape>(kNarrow, 0.60, 0.60, 5.0), cost<TinyShape>(kTiny, 0.60, 0.60, 4.2),
      cost<PairShape>(kPair, 0.95, 0.95, 7.2)}};
 const FormCost kStagedCosts[3][2] = {{cost<MiddleShape>(kMiddle, 1.15, 1.02, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)},
                                      {cost<MiddleShape>(kMiddle, 1.31, 1.45, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)},
-                                     {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)}};
+                                     {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape::Staged>(kTiny, 1.3, 1.0, 6.5)}};
 const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<SmallShape>(kSmall, 2.35, 2.35, 4.5),
                                cost<TinyShape>(kTiny, 0.6, 0.4, 4.5)};
 const FormCost kFp32StagedCosts[] = {cost<MiddleShape>(kMiddle, 4.65, 2.5, 7.0), cost<TinyShape::Staged>(kTiny, 1.2, 0.75, 5.0)};
+
+// The kernel for few rows of x: its start, and the bytes a microsecond that it reads with 1, 2, 4 and 8 rows.  Against
+// 16 x 32 tiles with 5 rows: 14336 x 4096 31.5 us (23.6), 4096 x 4096 10.2 (9.8), 2048 x 2048 5.6 (6.2), 960 x 4096 7.0
+// (7.7); with 3 rows 25.6 (23.4), 8.8 (9.8), 4.8 (6.2) and 5.0 (7.7).
+constexpr double kRowsStart = 3.5, kRowsRate[4] = {5.8e6, 5.6e6, 4.9e6, 3.8e6};
 
 // A product's sizes as the choice sees them: of out, its stages of r, and the microseconds that 65,536 values' epilogue
 // keeps a compute unit's vector units busy.
 struct Sizes {
   int64_t i, j, stages;
   double epilogue;
-  double stream;  // microseconds in which memory delivers the operands
+  double bytes;  // of the operands
 };
 
 // Microseconds of `splits` ranges of r with tile f.
@@ -1117,10 +1122,14 @@ double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
   const double full = f.rest + steps * f.stage + end * f.resident;
   double us = (double)rounds * full;
   if (left) us += left > kComputeUnits || rounds ? full : f.rest + steps * f.alone + end;
+  // Memory delivers the operands at 5.6 TB/s after a start of 4.5 us, and to a block at 40 GB/s; between tiles that it
+  // bounds, the one with the least work.
+  const double rate = 40e3 * (double)blocks;
+  const double memory = 4.5 + z.bytes / (rate < 5.6e6 ? rate : 5.6e6);
+  double sum = (us > memory ? us : memory) + 0.1 * us;
   // the partial sums are written and read, and another launch joins them
-  if (splits > 1) us += 2.5 + (double)splits * (double)z.i * (double)z.j * 8.0 / 8e6;
-  // no faster than memory, and between tiles that it bounds the one with the least work
-  return (us > z.stream ? us : z.stream) + 0.1 * us;
+  if (splits > 1) sum += 2.0 + (double)splits * (double)z.i * (double)z.j * 8.0 / 8e6;
+  return sum;
 }
 
 // The least-time tile and number of ranges of r by those costs.  Ranges beyond one block a place only cost.
@@ -1193,11 +1202,6 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int bytes = dtype == 1 ? 2 : 4;
   const int64_t deep = 128 / bytes;
   LinPlan best{};
-  if (epi == kEpiLayer && a.i <= kMaxRows) {
-    best.part[0] = {a.i, kRows, 1};
-    best.parts = 1;
-    return best;
-  }
   Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0, 0.0};
   if (epi == kEpiLayer) z.epilogue = (a.act ? 8.0 : 0.0) + (a.codes ? 6.0 : 0.0) + (a.mul ? 2.0 : 0.0) + (a.residual ? 2.0 : 0.0);
   if (epi == kEpiDgrad) z.epilogue = a.up_codes ? 22.0 : a.z_codes ? 13.0 : 0.0;
@@ -1205,8 +1209,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   operands(a, epi, bytes, o);
   int32_t off = 0;  // operands whose rows do not start and end on 16 bytes
   double moved = 0.0;
-  z.stream = 4.5;
-  for (int k = 0; k < 4; ++k) z.stream += (double)o[k].rows * (double)o[k].run * bytes / 5.6e6;
+  for (int k = 0; k < 4; ++k) z.bytes += (double)o[k].rows * (double)o[k].run * bytes;
   for (int k = 0; k < 4; ++k)
     if (!o[k].fits) {
       off |= 1 << k;
@@ -1214,15 +1217,28 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
     }
   const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
   const double direct = dtype == 1 ? choose_parts(kDirectCosts[transposed], 6, z, best) : choose_parts(kFp32Costs, 3, z, best);
+  double least = direct;
   best.direct = 1;
   if (off) {
     // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
     LinPlan staged{};
     const double through = dtype == 1 ? choose_parts(kStagedCosts[transposed], 2, z, staged) : choose_parts(kFp32StagedCosts, 2, z, staged);
-    if (through <= direct + 6.0 + moved / 5.0e6)
+    least = direct + 6.0 + moved / 5.0e6;
+    if (through <= least) {
       best = staged;
-    else
+      least = through;
+    } else {
       best.pack = off;
+    }
+  }
+  // few rows: the kernel that takes operands of any alignment without a copy
+  if (epi == kEpiLayer && a.i <= kMaxRows) {
+    const double rate = kRowsRate[a.i > 4 ? 3 : a.i > 2 ? 2 : a.i - 1];
+    if (kRowsStart + z.bytes / rate <= least) {
+      best = LinPlan{};
+      best.part[0] = {a.i, kRows, 1};
+      best.parts = 1;
+    }
   }
   // the parts run one after the other and share the place of their partial sums
   for (int p = 0; p < best.parts; ++p) {
