@@ -144,18 +144,23 @@ __device__ __forceinline__ void finish_eights(const LinArgs& a, int64_t i0, int6
   constexpr int kEights = NI * NJ / 2, kAhead = WHOLE ? 4 : 1;
   const bool partial = a.splits > 1;
   const int64_t ld = (a.j + 7) & ~(int64_t)7;
+  Side<T, EPI> side[kAhead];
+  ColumnSide<T, EPI> column;
+  const auto load = [&](int which, ColumnSide<T, EPI>& c, Side<T, EPI> (&s)[kAhead]) {
+    const int64_t j = j0 + cols(which / NI);
+    column_load<T, EPI>(a, j, c);
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) side_load<T, EPI, WHOLE>(a, i0 + rows(which % NI + n), j, s[n]);
+  };
+  if (!partial) load(0, column, side);
 #pragma unroll 1
   for (int first = 0; first < kEights; first += kAhead) {
     const int which = __builtin_amdgcn_readfirstlane(first);
     float v[kAhead][8];
-    Side<T, EPI> side[kAhead];
-    ColumnSide<T, EPI> column;
+    Side<T, EPI> next_side[kAhead];
+    ColumnSide<T, EPI> next_column;
     const int64_t j = j0 + cols(which / NI);
-    if (!partial) {
-      column_load<T, EPI>(a, j, column);
-#pragma unroll
-      for (int n = 0; n < kAhead; ++n) side_load<T, EPI, WHOLE>(a, i0 + rows(which % NI + n), j, side[n]);
-    }
+    if (!partial && which + kAhead < kEights) load(which + kAhead, next_column, next_side);
 #pragma unroll
     for (int c = 0; c < kEights; c += kAhead) {
       if (which == c) {
@@ -179,6 +184,9 @@ __device__ __forceinline__ void finish_eights(const LinArgs& a, int64_t i0, int6
         epilogue8<T, EPI, 16, 32, WHOLE>(a, i, j, v[n], column, side[n]);
       }
     }
+    column = next_column;
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) side[n] = next_side[n];
   }
 }
 
@@ -1088,7 +1096,7 @@ const FormCost kDirectCosts[3][6] = {
      cost<NarrowShape>(kNarrow, 0.55, 0.55, 5.0), cost<TinyShape>(kTiny, 0.45, 0.28, 4.2),
      cost<PairShape>(kPair, 0.95, 0.95, 7.2)},
     {direct_fast(1.43), cost<MiddleShape>(kMiddle, 0.92, 0.66, 6.0), cost<SmallShape>(kSmall, 0.90, 0.90, 5.2),
-     cost<NarrowShape>(kNarrow, 0.58, 0.58, 5.0), cost<TinyShape>(kTiny, 0.48, 0.30, 4.2),
+     cost<NarrowShape>(kNarrow, 0.58, 0.58, 5.0), cost<TinyShape>(kTiny, 0.50, 0.30, 4.2),
      cost<PairShape>(kPair, 0.95, 0.95, 7.2)},
     {direct_fast(1.46), cost<MiddleShape>(kMiddle, 0.94, 0.70, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
      cost<NarrowShape>(kNarrow, 0.60, 0.60, 5.0), cost<TinyShape>(kTiny, 0.60, 0.60, 4.2),
@@ -1097,7 +1105,7 @@ const FormCost kStagedCosts[3][2] = {{cost<MiddleShape>(kMiddle, 1.15, 1.02, 9.0
                                      {cost<MiddleShape>(kMiddle, 1.31, 1.45, 9.0), cost<TinyShape::Staged>(kTiny, 0.8, 0.6, 6.5)},
                                      {cost<MiddleShape>(kMiddle, 1.74, 1.57, 9.0), cost<TinyShape::Staged>(kTiny, 1.3, 1.0, 6.5)}};
 const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<SmallShape>(kSmall, 2.35, 2.35, 4.5),
-                               cost<TinyShape>(kTiny, 0.6, 0.4, 4.5)};
+                               cost<TinyShape>(kTiny, 0.6, 0.32, 4.5)};
 const FormCost kFp32StagedCosts[] = {cost<MiddleShape>(kMiddle, 4.65, 2.5, 7.0), cost<TinyShape::Staged>(kTiny, 1.2, 0.75, 5.0)};
 
 // The kernel for few rows of x: its start, and the bytes a microsecond that it reads with 1, 2, 4 and 8 rows.  Against
@@ -1111,6 +1119,7 @@ struct Sizes {
   int64_t i, j, stages;
   double epilogue;
   double bytes;  // of the operands
+  int64_t line;  // columns of a transposed Q in a cache line, or 0
 };
 
 // Microseconds of `splits` ranges of r with tile f.
@@ -1122,9 +1131,10 @@ double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
   const double full = f.rest + steps * f.stage + end * f.resident;
   double us = (double)rounds * full;
   if (left) us += left > kComputeUnits || rounds ? full : f.rest + steps * f.alone + end;
-  // Memory delivers the operands at 5.6 TB/s after a start of 4.5 us, and to a block at 40 GB/s; between tiles that it
-  // bounds, the one with the least work.
-  const double rate = 40e3 * (double)blocks;
+  // Memory delivers the operands at 5.6 TB/s after a start of 4.5 us, and to a block at 40 GB/s, half of it where the
+  // block takes half of each cache line (32 x 4096 x 14336 with W read along its rows: 51 us in 128 tiles of 16 x 32,
+  // 31 us in 256 blocks of 32 x 64); between tiles that it bounds, the one with the least work.
+  const double rate = (f.j < z.line ? 20e3 : 40e3) * (double)blocks;
   const double memory = 4.5 + z.bytes / (rate < 5.6e6 ? rate : 5.6e6);
   double sum = (us > memory ? us : memory) + 0.1 * us;
   // the partial sums are written and read, and another launch joins them
@@ -1202,7 +1212,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int bytes = dtype == 1 ? 2 : 4;
   const int64_t deep = 128 / bytes;
   LinPlan best{};
-  Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0, 0.0};
+  Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0, 0.0, epi == kEpiLayer ? 0 : 128 / bytes};
   if (epi == kEpiLayer) z.epilogue = (a.act ? 8.0 : 0.0) + (a.codes ? 6.0 : 0.0) + (a.mul ? 2.0 : 0.0) + (a.residual ? 2.0 : 0.0);
   if (epi == kEpiDgrad) z.epilogue = a.up_codes ? 22.0 : a.z_codes ? 13.0 : 0.0;
   Operand o[4];
