@@ -55,8 +55,8 @@ template <>
 struct Frag<float> {
   f32x4 v;
 };
-// Instruction E of a fragment pair's kSteps.  One fp32 instruction after another on the same sum waits for it, so callers
-// go through all sums before the next E.
+// Instruction E of a fragment pair's kSteps.  One fp32 instruction after another on the same sum waits for it, so
+// callers go through all sums before the next E.
 template <typename T>
 constexpr int kSteps = 1;
 template <>
@@ -136,7 +136,9 @@ __device__ __forceinline__ u32x4 load_chunk(const typename El<T>::Mem* p, int32_
 // The epilogue of a wave's accumulators, or their store as a partial sum: four eights of values a lane at a
 // time, chosen by a branch on a uniform number.  Unrolled over all 16 eights an epilogue with an activation is 100 KB
 // of instructions that every tile reads anew; one eight at a time, its branches, its loads of other matrices and its
-// stores wait for each other (12 us a tile of 256 x 256, against 6.5 us for four).
+// stores wait for each other (12 us a tile of 256 x 256, against 6.5 us for four).  The next four's loads are asked for
+// before these four's stores, which a wait for loads asked for later would include (a gated gradient of
+// 4096 x 8960 x 1536 takes 179 us, 183 us with the loads after the stores).
 // Instruction tile p of the accumulators lies ROWS(p) rows below i0, pair q COLS(q) columns right of j0.
 template <typename T, int EPI, bool WHOLE, int NI, int NJ, typename R, typename C>
 __device__ __forceinline__ void finish_eights(const LinArgs& a, int64_t i0, int64_t j0, const f32x4 (&acc)[NI][NJ],
@@ -219,6 +221,10 @@ __device__ __forceinline__ int64_t split_start(int64_t n, uint32_t s, int32_t sp
 // into the halves that the previous phase emptied.  Waves 4 to 7 run half a phase behind waves 0 to 3, so on
 // each SIMD one wave's matrix instructions cover the other's memory instructions.  (With one quadrant a phase the
 // barriers left the matrix cores idle for a quarter of the time.)
+//
+// Bound by the matrix cores: 8192 x 4096 x 14336 with a residual takes 670 us, 1430 TFLOP/s, with them busy 90 % of the
+// time; a weight gradient of the same size, both operands transposed, 1370 TFLOP/s and 82 %.  256 x 256 is the largest
+// tile whose sums (128 registers a lane) and whose two stages (128 KB) a compute unit holds, and so reads LDS least.
 //
 // What orders the phases: a wave passes the barrier before its matrix instructions once its own reads of LDS have
 // returned and all but its last 8 copies (four halves) have landed.  So a half is read after a barrier
@@ -580,6 +586,11 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
 //
 // A group's stages lie in NBUF buffers.  While a wave multiplies the fragments of one stage it reads those of the
 // next from LDS; a buffer is filled again once every wave of the group has read it.
+//
+// Where tiles are few these kernels are bound by what a block's waves can issue and by their start and end (128 x 128 with
+// two groups: 0.95 us a step of two stages, 0.44 us of it in matrix instructions): 4096 x 1024 x 4096 takes 38.5 us,
+// 890 TFLOP/s (47 us without the second group), 2048 x 2048 x 2048 23 us, 300 x 1024 x 1024 6.5 us.  In fp32 128 x 128
+// tiles, two blocks a unit, are bound by the matrix cores: 4096 x 4096 x 4096 950 us, 145 TFLOP/s.
 template <int TI_, int TJ_, int WI_, int WJ_, int G_, int NBUF_>
 struct GroupShape {
   static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, G = G_, NBUF = NBUF_;
@@ -703,8 +714,8 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   // The fragments `set_` of this step have been asked for.  DIRECT: wait for them and for the next stage, then fill their
   // buffer again, ask for the next fragments and multiply.  Else: put the next stage into the other buffer (whose
   // fragments every wave had before the last barrier), start loading the one after, wait, and the same.  The copies and
-  // reads are dealt out between the matrix instructions, which run on while a wave issues them: one after the other
-  // they left the matrix cores idle for half of a stage.
+  // reads are dealt out between the matrix instructions, which run on while a wave issues them: fp32
+  // 2056 x 4096 x 1024 takes 138 us so, and 146 us with all of them first.
   const auto step = [&](int set_) {
     i32x4 rsrc_p, rsrc_q;
     uint32_t to_p = 0, to_q = 0;
@@ -811,7 +822,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
 // of W an instruction, whatever its alignment (a matrix fragment's 64 bytes of 16 rows streamed a fifth slower, and at
 // half the rate off 16-byte rows), multiplies it with the same 1 KB of each row of x on the vector units, and adds its
 // lanes' sums at the end.  A block's eight waves take JB rows of W, four a wave, and share out r where that leaves
-// waves over.
+// waves over.  1 x 14336 x 4096 takes 24 us, 4.9 TB/s of W (27 us with a gate), 1 x 4096 x 14336 22 us, 5.3 TB/s.
 constexpr int kRowsWaves = 8, kRowsEach = 4, kMaxRows = 8;
 
 template <typename T>
@@ -925,7 +936,8 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
   epilogue8<T, kEpiLayer, 1, 2>(a, fi, j0 + fj, v, column, side);
 }
 
-// Joins the partial sums in their order and applies the epilogue: eight j a thread.
+// Joins the partial sums in their order and applies the epilogue: eight j a thread.  Bound by memory: two ranges of
+// 4096 x 2048 take 14 us, 6.2 TB/s.
 template <typename T, int EPI>
 __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
   const int64_t eights = ((a.j + kCkptBlock - 1) / kCkptBlock) * 4, ld = (a.j + 7) & ~(int64_t)7;
@@ -949,7 +961,7 @@ __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
 
 // ---------------------------------------------------------------- copies on 16-byte rows
 // Operands off 16-byte rows, copied to rows of whole 16 bytes with zeros at their ends: every chunk is read once at its
-// element's address and written once.  A block takes kPackChunks of one operand.
+// element's address and written once, at about 5 TB/s.  A block takes kPackChunks of one operand.
 constexpr int kPackChunks = 1024;
 struct PackJob {
   const void* from;
@@ -993,22 +1005,43 @@ __global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
 }
 
 // ---------------------------------------------------------------- column sums
-// A block sums 64 columns over all rows: eight lanes hold a row's 64 columns, 128 rows at a time, and their sums are
-// added through LDS in the rows' order.  One launch: a second one that joins shares of the rows takes as long as
-// the sums of 2,000 rows.
-constexpr int kSumCols = 64, kSumThreads = 1024, kSumRows = kSumThreads / 8;
+// A block sums COLS columns over all rows: COLS / 8 lanes hold a row's, and the sums are added through LDS in the
+// rows' order, so one launch and no workspace do.  Bound by memory where there are enough columns (8192 x 14336 bf16
+// adds 34 us to a weight gradient, 6.9 TB/s), else by how much its few blocks keep in flight: 32 columns a block there
+// (1999 x 2048 6.2 us, with 64 columns a block 9.5).  Blocks of 32 bf16 columns read half cache lines, which costs where
+// memory is the bound.
+constexpr int kSumThreads = 1024;
 
-template <typename T>
+template <typename T, int COLS>
 __global__ __launch_bounds__(kSumThreads) void k_column_sum(const typename El<T>::Mem* __restrict__ dy, int64_t ld,
                                                             int64_t rows, int64_t cols,
                                                             typename El<T>::Mem* __restrict__ db) {
-  __shared__ float s[kSumRows][kSumCols + 1];
-  const int sub = (int)threadIdx.x / 8, c = (int)threadIdx.x % 8 * 8;
-  const int64_t j0 = (int64_t)blockIdx.x * kSumCols + c, valid = cols - j0;
+  constexpr int kLanes = COLS / 8, kRows = kSumThreads / kLanes, kParts = kSumThreads / COLS, kEach = kRows / kParts,
+                kAhead = 4;
+  __shared__ float s[kRows][COLS + 1];
+  const int sub = (int)threadIdx.x / kLanes, c = (int)threadIdx.x % kLanes * 8;
+  const int64_t j0 = (int64_t)blockIdx.x * COLS + c, valid = cols - j0;
   float v[8] = {};
-  if (valid > 0) {
+  if (valid >= 8) {
+    // kAhead rows' loads together; past the last row they repeat it and add nothing
+    for (int64_t r0 = sub; r0 < rows; r0 += kAhead * kRows) {
+      Raw8<T> x[kAhead];
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) {
+        const int64_t r = r0 + n * kRows;
+        x[n].load(dy + (r < rows ? r : rows - 1) * ld + j0);
+      }
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) {
+        float u[8];
+        x[n].get(u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += r0 + n * kRows < rows ? u[e] : 0.f;
+      }
+    }
+  } else if (valid > 0) {
 #pragma unroll 4
-    for (int64_t r = sub; r < rows; r += kSumRows) {
+    for (int64_t r = sub; r < rows; r += kRows) {
       float x[8];
       load_row8<T>(dy + r * ld + j0, valid, x);
 #pragma unroll
@@ -1018,19 +1051,19 @@ __global__ __launch_bounds__(kSumThreads) void k_column_sum(const typename El<T>
 #pragma unroll
   for (int e = 0; e < 8; ++e) s[sub][c + e] = v[e];
   __syncthreads();
-  // 16 threads a column add eight rows each, then one thread their sums
-  const int col = (int)threadIdx.x % kSumCols, part = (int)threadIdx.x / kSumCols;
+  // kParts threads a column add kEach rows each, then one thread their sums
+  const int col = (int)threadIdx.x % COLS, part = (int)threadIdx.x / COLS;
   float sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < kSumRows / 16; ++k) sum += s[part * (kSumRows / 16) + k][col];
+  for (int k = 0; k < kEach; ++k) sum += s[part * kEach + k][col];
   __syncthreads();
   s[part][col] = sum;
   __syncthreads();
-  const int64_t j = (int64_t)blockIdx.x * kSumCols + col;
+  const int64_t j = (int64_t)blockIdx.x * COLS + col;
   if (part == 0 && j < cols) {
     sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) sum += s[k][col];
+    for (int k = 0; k < kParts; ++k) sum += s[k][col];
     El<T>::store(db + j, sum);
   }
 }
@@ -1164,7 +1197,7 @@ double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part) {
 
 // The same in one launch or two: rounds of blocks that fill every compute unit, then the rows that are left with the
 // tile that suits them, where that beats a last round of few blocks.  (4096 x 8960 x 1536 with a gated epilogue: three
-// rounds of 256 x 256 tiles, the last of 48, took 200 us.)
+// rounds of 256 x 256 tiles, the last of 48, take 193 us, two rounds and the rest 179 us.)
 double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& plan) {
   constexpr double kWorthIt = 15.0, kLaunch = 2.0;
   double least = choose(costs, count, z, plan.part[0]);
@@ -1388,8 +1421,14 @@ hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t c
   with_element(dtype, [&](auto t) {
     using T = decltype(t);
     using Mem = typename El<T>::Mem;
-    k_column_sum<T><<<dim3((uint32_t)div_up(cols, kSumCols)), dim3(kSumThreads), 0, stream>>>(
-        static_cast<const Mem*>(dy), ld, rows, cols, static_cast<Mem*>(db));
+    const auto launch = [&](auto n) {
+      k_column_sum<T, n()><<<dim3((uint32_t)div_up(cols, n())), dim3(kSumThreads), 0, stream>>>(
+          static_cast<const Mem*>(dy), ld, rows, cols, static_cast<Mem*>(db));
+    };
+    if (cols >= 32 * kComputeUnits)
+      launch(std::integral_constant<int, 64>());
+    else
+      launch(std::integral_constant<int, 32>());
   });
   return hipGetLastError();
 }
