@@ -1306,6 +1306,8 @@ hipError_t launch_group(const LinArgs& a, bool direct, hipStream_t stream) {
   } else if constexpr (std::is_same<S, MiddleShape>::value || std::is_same<S, TinyShape>::value) {
     using R = typename S::Staged;
     k_linear_group<T, PT, QT, EPI, R, false><<<grid, dim3(R::kThreads), R::kLds, stream>>>(a);
+  } else {
+    return hipErrorInvalidConfiguration;
   }
   return hipGetLastError();
 }
