@@ -1163,7 +1163,12 @@ double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
   const double end = splits > 1 ? 0.0 : z.epilogue * (double)(f.i * f.j) / 65536.0;
   const double full = f.rest + steps * f.stage + end * f.resident;
   double us = (double)rounds * full;
-  if (left) us += left > kComputeUnits || rounds ? full : f.rest + steps * f.alone + end;
+  // a part of a round: fewer units run two epilogues (512 x 8960 x 1536, gated: 37 us in 280 tiles of 128 x 128, 42 us in
+  // three ranges of r of 256 x 256)
+  if (left > kComputeUnits)
+    us += f.rest + steps * f.stage + end * f.resident * (double)left / (double)slots;
+  else if (left)
+    us += rounds ? full : f.rest + steps * f.alone + end;
   // Memory delivers the operands at 5.6 TB/s after a start of 4.5 us, and to a block at 40 GB/s, half of it where the
   // block takes half of each cache line (32 x 4096 x 14336 with W read along its rows: 51 us in 128 tiles of 16 x 32,
   // 31 us in 256 blocks of 32 x 64); between tiles that it bounds, the one with the least work.
