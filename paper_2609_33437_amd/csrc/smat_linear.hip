@@ -1082,10 +1082,15 @@ void with_element(int dtype, F&& fn) {
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int kComputeUnits = 256;
 
-// Whether an operand's stages can be copied to LDS directly: 16-byte rows, and offsets of a tile below 2^31.
+// The first row stride whose tiles cannot be copied to LDS directly: copies take 32-bit offsets from a tile's first
+// byte, and those past 0x7FFFFFF0 read as zeros.  A tile has up to 256 bf16 or 128 fp32 rows of a direct operand
+// (510 ld bytes), and a stage 64 bf16 or 32 fp32 of a transposed one (126 ld bytes and a tile's 512).
+constexpr int64_t wide_ld(bool trans) { return trans ? (int64_t)1 << 24 : (int64_t)1 << 22; }
+
+// Whether an operand's stages can be copied to LDS directly: 16-byte rows, and no wide ones.
 bool operand_fits(const void* p, int64_t ld, int64_t r, bool trans, int bytes) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * bytes % 16 == 0 && (trans || r * bytes % 16 == 0) &&
-         ld < ((int64_t)1 << 20);
+         ld < wide_ld(trans);
 }
 
 // fn(element type, P transposed, Q transposed, epilogue) of an operation.
@@ -1234,15 +1239,15 @@ double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& p
 struct Operand {
   const void* p;
   int64_t ld, rows, run;
-  bool fits;
+  bool fits, trans;
 };
 // Operands 2 s and 2 s + 1 are P and Q of product s.
 void operands(const LinArgs& a, LinEpilogue epi, int bytes, Operand (&o)[4]) {
   const bool pt = epi == kEpiStore, qt = epi != kEpiLayer;
   for (int s = 0; s < 2; ++s) {
     const LinProduct& pr = a.prod[s];
-    o[2 * s] = {pr.p, pr.ldp, pt ? pr.r : a.i, pt ? a.i : pr.r, pr.r == 0 || operand_fits(pr.p, pr.ldp, pr.r, pt, bytes)};
-    o[2 * s + 1] = {pr.q, pr.ldq, qt ? pr.r : a.j, qt ? a.j : pr.r, pr.r == 0 || operand_fits(pr.q, pr.ldq, pr.r, qt, bytes)};
+    o[2 * s] = {pr.p, pr.ldp, pt ? pr.r : a.i, pt ? a.i : pr.r, pr.r == 0 || operand_fits(pr.p, pr.ldp, pr.r, pt, bytes), pt};
+    o[2 * s + 1] = {pr.q, pr.ldq, qt ? pr.r : a.j, qt ? a.j : pr.r, pr.r == 0 || operand_fits(pr.q, pr.ldq, pr.r, qt, bytes), qt};
   }
 }
 int64_t packed_ld(int64_t run, int bytes) { return div_up(run * bytes, 16) * 16 / bytes; }
@@ -1257,12 +1262,14 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   if (epi == kEpiDgrad) z.epilogue = a.up_codes ? 22.0 : a.z_codes ? 13.0 : 0.0;
   Operand o[4];
   operands(a, epi, bytes, o);
-  int32_t off = 0;  // operands whose rows do not start and end on 16 bytes
+  int32_t off = 0;  // operands that cannot be copied to LDS directly as they lie
+  bool wide = false;  // one of them is too wide for direct copies even where it is packed
   double moved = 0.0;
   for (int k = 0; k < 4; ++k) z.bytes += (double)o[k].rows * (double)o[k].run * bytes;
   for (int k = 0; k < 4; ++k)
     if (!o[k].fits) {
       off |= 1 << k;
+      wide |= packed_ld(o[k].run, bytes) >= wide_ld(o[k].trans);
       moved += 2.0 * (double)o[k].rows * (double)o[k].run * bytes;
     }
   const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
@@ -1274,7 +1281,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
     LinPlan staged{};
     const double through = dtype == 1 ? choose_parts(kStagedCosts[transposed], 2, z, staged) : choose_parts(kFp32StagedCosts, 2, z, staged);
     least = direct + 6.0 + moved / 5.0e6;
-    if (through <= least) {
+    if (wide || through <= least) {
       best = staged;
       least = through;
     } else {
