@@ -34,10 +34,12 @@ struct Array {
   int64_t span() const { return rows > 0 && run > 0 ? (rows - 1) * ld + run : 0; }
 };
 
+// A row stride that check_arrays refuses stays one in bytes.
 Array matrix(const char* what, const void* p, int64_t rows, int64_t cols, int64_t ld, int dtype, bool out = false,
              bool same = false) {
   const int64_t b = (int64_t)dtype_bytes(dtype);
-  return Array{what, p, rows, cols * b, ld * b, (size_t)b, out, same};
+  const int64_t bytes = ld < 0 ? -1 : ld > kMaxSpan ? INT64_MAX : ld * b;
+  return Array{what, p, rows, cols * b, bytes, (size_t)b, out, same};
 }
 Array codes(const char* what, const void* p, int64_t rows, int64_t cols, bool out = false) {
   const int64_t run = smat::ckpt_blocks(cols) * smat::kCkptBlock;
