@@ -10,7 +10,8 @@ epilogue (smat_linear_dgrad) and reads the input's checkpoint in the weight grad
 byte, against d + 2 f or d + 3 f of two bytes.
 
 Gradients are those of the checkpointed values: they differ from exact ones by what 8 bits lose of the
-saved activations (about one per cent of a weight gradient's norm), never in the forward pass.  Without gradients (a merged
+saved activations (about one per cent of a weight gradient's norm), never in the forward pass.  They have no
+derivatives of their own: differentiating them again raises.  Without gradients (a merged
 model answering) nothing is saved, and a few tokens take the product's form for few rows.
 
 Tensors are fp32 or bf16 on the GPU; under torch.autocast floating inputs are cast to its dtype first, as
@@ -22,6 +23,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from ._lib import SMAT_ERR_INVALID, SmatError
 from ._linear import (SMAT_ACT_NONE, SMAT_ACT_SILU, ActCheckpoint, smat_ckpt_read, smat_ckpt_write, smat_linear,
@@ -96,6 +98,7 @@ class _Linear(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         w, *saved = ctx.saved_tensors
         need_x, need_w, need_b, need_r = ctx.needs_input_grad
@@ -129,6 +132,7 @@ class _Mlp(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         w1, w2, *saved = ctx.saved_tensors
         kept = _kept(ctx, saved)
@@ -176,6 +180,7 @@ class _GatedMlp(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         wg, wu, wd, *saved = ctx.saved_tensors
         kept = _kept(ctx, saved)

@@ -1,0 +1,39 @@
+"""The differentiable layers where a call could go wrong without a sign of it."""
+import pytest
+import torch
+
+import paper_2609_33437_amd as smat
+from paper_2609_33437_amd import layers
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def rand(gen, *shape, std=1.0, dtype=torch.float32):
+    return (torch.randn(*shape, generator=gen, device=DEV) * std).to(dtype)
+
+
+def weights(gen, d=64, f=96):
+    """w1 (or the gate), w2 (or the down projection), the up projection."""
+    return rand(gen, f, d, std=0.1), rand(gen, d, f, std=0.1), rand(gen, f, d, std=0.1)
+
+
+FORMS = {
+    "linear": lambda x, w1, w2, wu, **kw: layers.linear(x, w1, **kw),
+    "mlp": lambda x, w1, w2, wu, **kw: layers.mlp(x, w1, None, w2, None, smat.SMAT_ACT_GELU, **kw),
+    "gated": lambda x, w1, w2, wu, **kw: layers.gated_mlp(x, w1, wu, w2, **kw),
+}
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("wanted", ["x", "w"])
+def test_a_second_derivative_raises(form, wanted):
+    """A penalty on a gradient must not lose its derivative silently."""
+    gen = torch.Generator(DEV).manual_seed(1)
+    x, ws = rand(gen, 6, 64).requires_grad_(True), [w.requires_grad_(True) for w in weights(gen)]
+    y = FORMS[form](x, *ws)
+    (g,) = torch.autograd.grad(y.square().sum(), x if wanted == "x" else ws[0], create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (y.sum() + g.square().sum()).backward()
+    # without a graph of the gradient all is as before
+    torch.autograd.grad(FORMS[form](x, *ws).square().sum(), [x] + ws[:1])
