@@ -11,7 +11,7 @@ byte, against d + 2 f or d + 3 f of two bytes.
 
 Gradients are those of the checkpointed values: they differ from exact ones by what 8 bits lose of the
 saved activations (about one per cent of a weight gradient's norm), never in the forward pass.  They have no
-derivatives of their own: differentiating them again raises.  Without gradients (a merged
+derivatives of their own, and there are none in forward mode: asking for either raises.  Without gradients (a merged
 model answering) nothing is saved, and a few tokens take the product's form for few rows.
 
 Tensors are fp32 or bf16 on the GPU; under torch.autocast floating inputs are cast to its dtype first, as
@@ -23,6 +23,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from ._lib import SMAT_ERR_INVALID, SmatError
@@ -50,7 +51,13 @@ def _cast(*tensors):
 
 
 def _saves(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    """Whether autograd records the call.  Where it does not, tangents, which torch carries through frozen
+    weights and no_grad too, are refused (the recorded functions raise on them themselves)."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        return True
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise SmatError(SMAT_ERR_INVALID, "the layers have no forward-mode derivatives")
+    return False
 
 
 def _checkpoint(x: torch.Tensor) -> ActCheckpoint:

@@ -1,6 +1,7 @@
 """The differentiable layers where a call could go wrong without a sign of it."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import paper_2609_33437_amd as smat
 from paper_2609_33437_amd import layers
@@ -37,3 +38,23 @@ def test_a_second_derivative_raises(form, wanted):
         (y.sum() + g.square().sum()).backward()
     # without a graph of the gradient all is as before
     torch.autograd.grad(FORMS[form](x, *ws).square().sum(), [x] + ws[:1])
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dual", ["x", "w", "residual"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_tangents_are_refused(form, dual, grad):
+    """Frozen weights, no_grad and recorded calls: a forward-mode derivative is never left out of the result."""
+    gen = torch.Generator(DEV).manual_seed(2)
+    x, ws = rand(gen, 6, 64), weights(gen)
+    r = rand(gen, 6, 96 if form == "linear" else 64)
+    with forward_ad.dual_level():
+        mark = lambda t: forward_ad.make_dual(t, torch.ones_like(t))        # noqa: E731
+        x, r = mark(x) if dual == "x" else x, mark(r) if dual == "residual" else r
+        ws = (mark(ws[0]), *ws[1:]) if dual == "w" else ws
+        with pytest.raises(smat.SmatError, match="forward-mode"):
+            FORMS[form](x, *ws, residual=r)
+        with torch.set_grad_enabled(grad), pytest.raises((smat.SmatError, NotImplementedError, RuntimeError)):
+            FORMS[form](x, *(w.requires_grad_(True) if forward_ad.unpack_dual(w).tangent is None else w for w in ws), residual=r)
+    with torch.no_grad():       # the same tensors without tangents
+        assert torch.isfinite(FORMS[form](rand(gen, 6, 64), *weights(gen))).all()
