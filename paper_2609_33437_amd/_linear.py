@@ -3,7 +3,8 @@ marshalling only; see include/smat.h for what each call computes).
 
 Matrices are 2-D GPU tensors with contiguous rows (any row stride); outputs are the caller's.  A call that
 needs device memory for partial sums takes it from `workspace` (a contiguous uint8 GPU tensor) or,
-without one, from torch's allocator on the call's stream.
+without one, from torch's allocator on the call's stream.  Tensors, stream and the current device are of one
+GPU; a call refuses others.
 """
 from __future__ import annotations
 
@@ -13,7 +14,7 @@ from typing import Optional
 
 from . import _lib
 from ._lib import (SMAT_ACT_GELU, SMAT_ACT_GELU_TANH, SMAT_ACT_NONE, SMAT_ACT_SILU, SMAT_ERR_DTYPE, SMAT_ERR_INVALID,
-                   SmatError, _check, _stream_handle, _torch, dtype_code, lib, smat_linear_args, smat_linear_dgrad_args,
+                   SmatError, _check, _torch, dtype_code, lib, smat_linear_args, smat_linear_dgrad_args,
                    smat_linear_wgrad_args)
 
 CKPT_BLOCK = 32     # elements along a row that share a power of two
@@ -102,10 +103,24 @@ def _ckpt(c, rows: int, cols: int, device: int, what: str):
     return c.codes.data_ptr(), c.exps.data_ptr()
 
 
+def _stream_on(device: int, stream) -> int:
+    """Handle of the given stream, or of the current one, where work on that GPU's tensors can be launched."""
+    C = _torch()._C
+    current = C._cuda_getDevice()
+    if current != device:
+        raise SmatError(SMAT_ERR_INVALID, f"the tensors are on GPU {device} and the current device is {current}: "
+                                          "call under torch.cuda.device(tensor.device)")
+    if stream is None:
+        return C._cuda_getCurrentRawStream(device)
+    if getattr(stream, "device_index", device) != device:
+        raise SmatError(SMAT_ERR_INVALID, f"the stream is of GPU {stream.device_index}, the tensors are on GPU {device}")
+    return stream.cuda_stream
+
+
 def _call(fn, size_fn, args, workspace, device: int, stream) -> None:
     need = c_size_t()
     _check(size_fn(byref(args), byref(need)))
-    ptr, have, handle = None, 0, _stream_handle(stream)
+    ptr, have, handle = None, 0, _stream_on(device, stream)
     if need.value:
         if workspace is None:
             torch = _torch()
@@ -126,8 +141,9 @@ def smat_ckpt_write(x, ckpt: ActCheckpoint, stream=None) -> None:
     code = _first(x, "x")
     rows, cols = x.shape
     px, ldx = _matrix(x, rows, cols, x, "x")
-    codes, exps = _ckpt(ckpt, rows, cols, x.get_device(), "ckpt")
-    _check(lib().smat_ckpt_write(px, ldx, code, rows, cols, codes, exps, _stream_handle(stream)))
+    device = x.get_device()
+    codes, exps = _ckpt(ckpt, rows, cols, device, "ckpt")
+    _check(lib().smat_ckpt_write(px, ldx, code, rows, cols, codes, exps, _stream_on(device, stream)))
 
 
 def smat_ckpt_read(ckpt: ActCheckpoint, out, act: int = SMAT_ACT_NONE, up: Optional[ActCheckpoint] = None,
@@ -140,7 +156,7 @@ def smat_ckpt_read(ckpt: ActCheckpoint, out, act: int = SMAT_ACT_NONE, up: Optio
     codes, exps = _ckpt(ckpt, rows, cols, device, "ckpt")
     up_codes, up_exps = _ckpt(up, rows, cols, device, "up") if up is not None else (None, None)
     _check(lib().smat_ckpt_read(codes, exps, up_codes, up_exps, int(act), code, rows, cols, pout, ldout,
-                                _stream_handle(stream)))
+                                _stream_on(device, stream)))
 
 
 # ------------------------------------------------------------------ products

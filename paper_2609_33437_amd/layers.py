@@ -50,6 +50,11 @@ def _cast(*tensors):
     return tuple(t if t is None or t.dtype == dtype else t.to(dtype) for t in tensors)
 
 
+def _device(x: torch.Tensor):
+    """x's GPU as the current one, which a model split over GPUs does not set.  (Autograd sets it for the backward.)"""
+    return torch.cuda.device(x.get_device())
+
+
 def _saves(*tensors) -> bool:
     """Whether autograd records the call.  Where it does not, tangents, which torch carries through frozen
     weights and no_grad too, are refused (the recorded functions raise on them themselves)."""
@@ -220,11 +225,12 @@ def linear(x, weight, bias: Optional[torch.Tensor] = None, residual: Optional[to
     x, weight, bias, residual = _cast(x, weight, bias, residual)
     shape, x = x.shape[:-1] + weight.shape[:1], _rows(x)
     r = None if residual is None else _rows(residual)
-    if _saves(x, weight, bias, r):
-        return _Linear.apply(x, weight, bias, r).view(shape)
-    out = torch.empty(x.shape[0], weight.shape[0], dtype=x.dtype, device=x.device)
-    smat_linear(x, weight, out, bias=bias, residual=r)
-    return out.view(shape)
+    with _device(x):
+        if _saves(x, weight, bias, r):
+            return _Linear.apply(x, weight, bias, r).view(shape)
+        out = torch.empty(x.shape[0], weight.shape[0], dtype=x.dtype, device=x.device)
+        smat_linear(x, weight, out, bias=bias, residual=r)
+        return out.view(shape)
 
 
 def mlp(x, w1, b1, w2, b2, act: int, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -234,13 +240,14 @@ def mlp(x, w1, b1, w2, b2, act: int, residual: Optional[torch.Tensor] = None) ->
     x, w1, b1, w2, b2, residual = _cast(x, w1, b1, w2, b2, residual)
     shape, x = x.shape[:-1] + w2.shape[:1], _rows(x)
     r = None if residual is None else _rows(residual)
-    if _saves(x, w1, b1, w2, b2, r):
-        return _Mlp.apply(x, w1, b1, w2, b2, r, int(act)).view(shape)
-    h = torch.empty(x.shape[0], w1.shape[0], dtype=x.dtype, device=x.device)
-    smat_linear(x, w1, h, bias=b1, act=act)
-    out = torch.empty(x.shape[0], w2.shape[0], dtype=x.dtype, device=x.device)
-    smat_linear(h, w2, out, bias=b2, residual=r)
-    return out.view(shape)
+    with _device(x):
+        if _saves(x, w1, b1, w2, b2, r):
+            return _Mlp.apply(x, w1, b1, w2, b2, r, int(act)).view(shape)
+        h = torch.empty(x.shape[0], w1.shape[0], dtype=x.dtype, device=x.device)
+        smat_linear(x, w1, h, bias=b1, act=act)
+        out = torch.empty(x.shape[0], w2.shape[0], dtype=x.dtype, device=x.device)
+        smat_linear(h, w2, out, bias=b2, residual=r)
+        return out.view(shape)
 
 
 def gated_mlp(x, w_gate, w_up, w_down, act: int = SMAT_ACT_SILU,
@@ -249,11 +256,12 @@ def gated_mlp(x, w_gate, w_up, w_down, act: int = SMAT_ACT_SILU,
     x, w_gate, w_up, w_down, residual = _cast(x, w_gate, w_up, w_down, residual)
     shape, x = x.shape[:-1] + w_down.shape[:1], _rows(x)
     r = None if residual is None else _rows(residual)
-    if _saves(x, w_gate, w_up, w_down, r):
-        return _GatedMlp.apply(x, w_gate, w_up, w_down, r, int(act)).view(shape)
-    h = torch.empty(x.shape[0], w_gate.shape[0], dtype=x.dtype, device=x.device)
-    smat_linear(x, w_up, h)
-    smat_linear(x, w_gate, h, act=act, mul=h)
-    out = torch.empty(x.shape[0], w_down.shape[0], dtype=x.dtype, device=x.device)
-    smat_linear(h, w_down, out, residual=r)
-    return out.view(shape)
+    with _device(x):
+        if _saves(x, w_gate, w_up, w_down, r):
+            return _GatedMlp.apply(x, w_gate, w_up, w_down, r, int(act)).view(shape)
+        h = torch.empty(x.shape[0], w_gate.shape[0], dtype=x.dtype, device=x.device)
+        smat_linear(x, w_up, h)
+        smat_linear(x, w_gate, h, act=act, mul=h)
+        out = torch.empty(x.shape[0], w_down.shape[0], dtype=x.dtype, device=x.device)
+        smat_linear(h, w_down, out, residual=r)
+        return out.view(shape)

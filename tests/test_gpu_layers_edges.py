@@ -58,3 +58,39 @@ def test_tangents_are_refused(form, dual, grad):
             FORMS[form](x, *(w.requires_grad_(True) if forward_ad.unpack_dual(w).tangent is None else w for w in ws), residual=r)
     with torch.no_grad():       # the same tensors without tangents
         assert torch.isfinite(FORMS[form](rand(gen, 6, 64), *weights(gen))).all()
+
+
+def test_another_current_device(monkeypatch):
+    """With another GPU as the current one the calls refuse the tensors, whose streams they would not use; the layers
+    enter the tensors' GPU themselves."""
+    gen = torch.Generator(DEV).manual_seed(3)
+    x, ws = rand(gen, 6, 64), weights(gen)
+    here = x.get_device()
+    current = [here + 1]
+    out, z = torch.empty(6, 96, device=DEV), smat.ActCheckpoint.empty(6, 64)
+
+    class entered:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    stream = torch.cuda.Stream()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0])
+    for call in (lambda: smat.smat_linear(x, ws[0], out), lambda: smat.smat_linear_dgrad(out, ws[0], torch.empty_like(x)),
+                 lambda: smat.smat_linear_wgrad(out, x, torch.empty_like(ws[0])), lambda: smat.smat_ckpt_write(x, z),
+                 lambda: smat.smat_ckpt_read(z, x), lambda: smat.smat_linear(x, ws[0], out, stream=stream)):
+        with pytest.raises(smat.SmatError, match="current device"):
+            call()
+    monkeypatch.setattr(torch.cuda, "device", entered)
+    for requires in (False, True):
+        for form, fn in FORMS.items():
+            y = fn(x, *(w.requires_grad_(requires) for w in ws))
+            assert torch.isfinite(y).all() and current[0] == here + 1
+    current[0] = here
+    with pytest.raises(smat.SmatError, match="stream"):
+        smat.smat_linear(x, ws[0], out, stream=type("Stream", (), dict(device_index=here + 1, cuda_stream=0))())
