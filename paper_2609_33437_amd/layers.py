@@ -15,7 +15,8 @@ derivatives of their own, and there are none in forward mode: asking for either 
 model answering) nothing is saved, and a few tokens take the product's form for few rows.
 
 Tensors are fp32 or bf16 on the GPU; under torch.autocast floating inputs are cast to its dtype first, as
-torch's own linear layers do.  A call's tensors share one dtype.  Row strides are kept where the last dimension
+torch's own linear layers do, except a residual: one of another dtype is added to the result in torch's
+promoted dtype.  Otherwise a call's tensors share one dtype.  Row strides are kept where the last dimension
 is contiguous; other layouts are copied.
 """
 from __future__ import annotations
@@ -48,6 +49,21 @@ def _cast(*tensors):
         return tensors
     dtype = torch.get_autocast_dtype("cuda")
     return tuple(t if t is None or t.dtype == dtype else t.to(dtype) for t in tensors)
+
+
+def _residual(residual: Optional[torch.Tensor], x: torch.Tensor):
+    """(the residual as the product's epilogue adds it, or as torch adds it to the product's result).  Under autocast one of
+    another dtype, an fp32 residual stream beside bf16 products, is not cast: torch adds it in its own dtype, as it does
+    to the result of its own layers."""
+    if residual is None:
+        return None, None
+    if residual.dtype != x.dtype and torch.is_autocast_enabled("cuda"):
+        return None, residual
+    return _rows(residual), None
+
+
+def _sum(y: torch.Tensor, after: Optional[torch.Tensor]) -> torch.Tensor:
+    return y if after is None else after + y
 
 
 def _device(x: torch.Tensor):
@@ -222,46 +238,46 @@ class _GatedMlp(torch.autograd.Function):
 # ------------------------------------------------------------------ public functions
 def linear(x, weight, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x weight^T + bias + residual for x [.., k]; the weight gradient reads x from an 8-bit checkpoint."""
-    x, weight, bias, residual = _cast(x, weight, bias, residual)
+    x, weight, bias = _cast(x, weight, bias)
     shape, x = x.shape[:-1] + weight.shape[:1], _rows(x)
-    r = None if residual is None else _rows(residual)
+    r, after = _residual(residual, x)
     with _device(x):
         if _saves(x, weight, bias, r):
-            return _Linear.apply(x, weight, bias, r).view(shape)
+            return _sum(_Linear.apply(x, weight, bias, r).view(shape), after)
         out = torch.empty(x.shape[0], weight.shape[0], dtype=x.dtype, device=x.device)
         smat_linear(x, weight, out, bias=bias, residual=r)
-        return out.view(shape)
+        return _sum(out.view(shape), after)
 
 
 def mlp(x, w1, b1, w2, b2, act: int, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(x w1^T + b1) w2^T + b2 + residual for x [.., d] (biases and residual may be None)."""
     if act == SMAT_ACT_NONE:
         raise SmatError(SMAT_ERR_INVALID, "an MLP needs an activation")
-    x, w1, b1, w2, b2, residual = _cast(x, w1, b1, w2, b2, residual)
+    x, w1, b1, w2, b2 = _cast(x, w1, b1, w2, b2)
     shape, x = x.shape[:-1] + w2.shape[:1], _rows(x)
-    r = None if residual is None else _rows(residual)
+    r, after = _residual(residual, x)
     with _device(x):
         if _saves(x, w1, b1, w2, b2, r):
-            return _Mlp.apply(x, w1, b1, w2, b2, r, int(act)).view(shape)
+            return _sum(_Mlp.apply(x, w1, b1, w2, b2, r, int(act)).view(shape), after)
         h = torch.empty(x.shape[0], w1.shape[0], dtype=x.dtype, device=x.device)
         smat_linear(x, w1, h, bias=b1, act=act)
         out = torch.empty(x.shape[0], w2.shape[0], dtype=x.dtype, device=x.device)
         smat_linear(h, w2, out, bias=b2, residual=r)
-        return out.view(shape)
+        return _sum(out.view(shape), after)
 
 
 def gated_mlp(x, w_gate, w_up, w_down, act: int = SMAT_ACT_SILU,
               residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """(act(x w_gate^T) (.) (x w_up^T)) w_down^T + residual for x [.., d] (SwiGLU with the default act)."""
-    x, w_gate, w_up, w_down, residual = _cast(x, w_gate, w_up, w_down, residual)
+    x, w_gate, w_up, w_down = _cast(x, w_gate, w_up, w_down)
     shape, x = x.shape[:-1] + w_down.shape[:1], _rows(x)
-    r = None if residual is None else _rows(residual)
+    r, after = _residual(residual, x)
     with _device(x):
         if _saves(x, w_gate, w_up, w_down, r):
-            return _GatedMlp.apply(x, w_gate, w_up, w_down, r, int(act)).view(shape)
+            return _sum(_GatedMlp.apply(x, w_gate, w_up, w_down, r, int(act)).view(shape), after)
         h = torch.empty(x.shape[0], w_gate.shape[0], dtype=x.dtype, device=x.device)
         smat_linear(x, w_up, h)
         smat_linear(x, w_gate, h, act=act, mul=h)
         out = torch.empty(x.shape[0], w_down.shape[0], dtype=x.dtype, device=x.device)
         smat_linear(h, w_down, out, residual=r)
-        return out.view(shape)
+        return _sum(out.view(shape), after)

@@ -94,3 +94,25 @@ def test_another_current_device(monkeypatch):
     current[0] = here
     with pytest.raises(smat.SmatError, match="stream"):
         smat.smat_linear(x, ws[0], out, stream=type("Stream", (), dict(device_index=here + 1, cuda_stream=0))())
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_an_fp32_residual_under_autocast_stays_fp32(form):
+    """As x + layer(x) of torch's layers: the residual stream is not rounded to the products' dtype."""
+    gen = torch.Generator(DEV).manual_seed(4)
+    x, ws = rand(gen, 2, 3, 64).requires_grad_(True), [w.requires_grad_(True) for w in weights(gen)]
+    r = (1000.0 + rand(gen, 2, 3, 96 if form == "linear" else 64)).requires_grad_(True)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        bare = FORMS[form](x, *ws)
+        y = FORMS[form](x, *ws, residual=r)
+        low = FORMS[form](x, *ws, residual=r.bfloat16())
+        with torch.no_grad():
+            plain = FORMS[form](x, *ws, residual=r)
+    assert bare.dtype == low.dtype == torch.bfloat16 and y.dtype == torch.float32
+    assert torch.equal(y, r + bare) and torch.equal(plain, y)
+    c = rand(gen, *y.shape)
+    got = torch.autograd.grad(y, (r, x), c)
+    assert torch.equal(got[0], c) and torch.equal(got[1], torch.autograd.grad(bare, x, c.bfloat16())[0])
+    # without autocast dtypes are not mixed
+    with pytest.raises(smat.SmatError):
+        FORMS[form](x, *ws, residual=r.bfloat16())
