@@ -16,7 +16,8 @@ model answering) nothing is saved, and a few tokens take the product's form for 
 
 Tensors are fp32 or bf16 on the GPU; under torch.autocast floating inputs are cast to its dtype first, as
 torch's own linear layers do, except a residual: one of another dtype is added to the result in torch's
-promoted dtype.  Otherwise a call's tensors share one dtype.  Row strides are kept where the last dimension
+promoted dtype.  Otherwise a call's tensors share one dtype.  A residual has the output's
+shape, or is the output's matrix of rows.  Row strides are kept where the last dimension
 is contiguous; other layouts are copied.
 """
 from __future__ import annotations
@@ -51,14 +52,16 @@ def _cast(*tensors):
     return tuple(t if t is None or t.dtype == dtype else t.to(dtype) for t in tensors)
 
 
-def _residual(residual: Optional[torch.Tensor], x: torch.Tensor):
+def _residual(residual: Optional[torch.Tensor], x: torch.Tensor, shape):
     """(the residual as the product's epilogue adds it, or as torch adds it to the product's result).  Under autocast one of
     another dtype, an fp32 residual stream beside bf16 products, is not cast: torch adds it in its own dtype, as it does
     to the result of its own layers."""
     if residual is None:
         return None, None
+    if residual.shape != shape and residual.shape != (x.shape[0], shape[-1]):
+        raise SmatError(SMAT_ERR_INVALID, f"residual has shape {tuple(residual.shape)}, the output {tuple(shape)}")
     if residual.dtype != x.dtype and torch.is_autocast_enabled("cuda"):
-        return None, residual
+        return None, residual.reshape(shape)
     return _rows(residual), None
 
 
@@ -240,7 +243,7 @@ def linear(x, weight, bias: Optional[torch.Tensor] = None, residual: Optional[to
     """x weight^T + bias + residual for x [.., k]; the weight gradient reads x from an 8-bit checkpoint."""
     x, weight, bias = _cast(x, weight, bias)
     shape, x = x.shape[:-1] + weight.shape[:1], _rows(x)
-    r, after = _residual(residual, x)
+    r, after = _residual(residual, x, shape)
     with _device(x):
         if _saves(x, weight, bias, r):
             return _sum(_Linear.apply(x, weight, bias, r).view(shape), after)
@@ -255,7 +258,7 @@ def mlp(x, w1, b1, w2, b2, act: int, residual: Optional[torch.Tensor] = None) ->
         raise SmatError(SMAT_ERR_INVALID, "an MLP needs an activation")
     x, w1, b1, w2, b2 = _cast(x, w1, b1, w2, b2)
     shape, x = x.shape[:-1] + w2.shape[:1], _rows(x)
-    r, after = _residual(residual, x)
+    r, after = _residual(residual, x, shape)
     with _device(x):
         if _saves(x, w1, b1, w2, b2, r):
             return _sum(_Mlp.apply(x, w1, b1, w2, b2, r, int(act)).view(shape), after)
@@ -271,7 +274,7 @@ def gated_mlp(x, w_gate, w_up, w_down, act: int = SMAT_ACT_SILU,
     """(act(x w_gate^T) (.) (x w_up^T)) w_down^T + residual for x [.., d] (SwiGLU with the default act)."""
     x, w_gate, w_up, w_down = _cast(x, w_gate, w_up, w_down)
     shape, x = x.shape[:-1] + w_down.shape[:1], _rows(x)
-    r, after = _residual(residual, x)
+    r, after = _residual(residual, x, shape)
     with _device(x):
         if _saves(x, w_gate, w_up, w_down, r):
             return _sum(_GatedMlp.apply(x, w_gate, w_up, w_down, r, int(act)).view(shape), after)

@@ -116,3 +116,20 @@ def test_an_fp32_residual_under_autocast_stays_fp32(form):
     # without autocast dtypes are not mixed
     with pytest.raises(smat.SmatError):
         FORMS[form](x, *ws, residual=r.bfloat16())
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("autocast", [False, True])
+def test_residuals_of_other_shapes_are_refused(form, autocast):
+    """As many rows in another order ([sequence, batch] for [batch, sequence]) would be added to the wrong tokens."""
+    gen = torch.Generator(DEV).manual_seed(5)
+    x, ws = rand(gen, 2, 3, 64), weights(gen)
+    n = 96 if form == "linear" else 64
+    with torch.autocast("cuda", dtype=torch.bfloat16, enabled=autocast):
+        for shape in ((3, 2, n), (1, 6, n), (1, 3, n), (n,), (2, 3, 1), (6, n, 1), (5, n)):
+            with pytest.raises(smat.SmatError):
+                FORMS[form](x, *ws, residual=rand(gen, *shape))
+        r = rand(gen, 2, 3, n)
+        assert torch.equal(FORMS[form](x, *ws, residual=r), FORMS[form](x, *ws, residual=r.view(6, n)))
+        one = rand(gen, n)      # a vector's residual is a vector
+        assert FORMS[form](x[0, 0], *ws, residual=one).shape == (n,)
