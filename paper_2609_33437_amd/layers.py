@@ -18,7 +18,7 @@ Tensors are fp32 or bf16 on the GPU; under torch.autocast floating inputs are ca
 torch's own linear layers do, except a residual: one of another dtype is added to the result in torch's
 promoted dtype.  Otherwise a call's tensors share one dtype.  A residual has the output's
 shape, or is the output's matrix of rows.  Row strides are kept where the last dimension
-is contiguous; other layouts are copied.
+is contiguous; other layouts, those of weights and biases too, are copied in every call.
 """
 from __future__ import annotations
 
@@ -39,6 +39,16 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
     if m.shape[1] > 1 and m.stride(1) != 1 or m.shape[0] > 1 and m.stride(0) < m.shape[1]:
         m = m.contiguous()
     return m
+
+
+def _weight(w: torch.Tensor) -> torch.Tensor:
+    if w.dim() != 2:
+        raise SmatError(SMAT_ERR_INVALID, f"a weight is a matrix, got shape {tuple(w.shape)}")
+    return _rows(w)
+
+
+def _bias(b: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    return None if b is None else b.contiguous()
 
 
 def _cast(*tensors):
@@ -242,6 +252,7 @@ class _GatedMlp(torch.autograd.Function):
 def linear(x, weight, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x weight^T + bias + residual for x [.., k]; the weight gradient reads x from an 8-bit checkpoint."""
     x, weight, bias = _cast(x, weight, bias)
+    weight, bias = _weight(weight), _bias(bias)
     shape, x = x.shape[:-1] + weight.shape[:1], _rows(x)
     r, after = _residual(residual, x, shape)
     with _device(x):
@@ -257,6 +268,7 @@ def mlp(x, w1, b1, w2, b2, act: int, residual: Optional[torch.Tensor] = None) ->
     if act == SMAT_ACT_NONE:
         raise SmatError(SMAT_ERR_INVALID, "an MLP needs an activation")
     x, w1, b1, w2, b2 = _cast(x, w1, b1, w2, b2)
+    w1, b1, w2, b2 = _weight(w1), _bias(b1), _weight(w2), _bias(b2)
     shape, x = x.shape[:-1] + w2.shape[:1], _rows(x)
     r, after = _residual(residual, x, shape)
     with _device(x):
@@ -273,6 +285,7 @@ def gated_mlp(x, w_gate, w_up, w_down, act: int = SMAT_ACT_SILU,
               residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """(act(x w_gate^T) (.) (x w_up^T)) w_down^T + residual for x [.., d] (SwiGLU with the default act)."""
     x, w_gate, w_up, w_down = _cast(x, w_gate, w_up, w_down)
+    w_gate, w_up, w_down = _weight(w_gate), _weight(w_up), _weight(w_down)
     shape, x = x.shape[:-1] + w_down.shape[:1], _rows(x)
     r, after = _residual(residual, x, shape)
     with _device(x):

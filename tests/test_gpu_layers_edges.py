@@ -133,3 +133,29 @@ def test_residuals_of_other_shapes_are_refused(form, autocast):
         assert torch.equal(FORMS[form](x, *ws, residual=r), FORMS[form](x, *ws, residual=r.view(6, n)))
         one = rand(gen, n)      # a vector's residual is a vector
         assert FORMS[form](x[0, 0], *ws, residual=one).shape == (n,)
+
+
+def test_weights_and_biases_of_any_layout():
+    """Transposed and strided weights, a strided bias and one value for all: results and gradients of contiguous copies."""
+    gen = torch.Generator(DEV).manual_seed(6)
+    d, f = 64, 96
+    x = rand(gen, 5, d).requires_grad_(True)
+    leaves = [rand(gen, d, f, std=0.1), rand(gen, 2 * f), rand(gen, d, 2 * f, std=0.1), rand(gen, 1), rand(gen, f, d, std=0.1)]
+    leaves = [t.requires_grad_(True) for t in leaves]
+    w1, b1, w2, b2, wu = leaves[0].t(), leaves[1][::2], leaves[2][:, ::2], leaves[3].expand(d), leaves[4]
+    c = [t.contiguous() for t in (w1, b1, w2, b2, wu)]
+    act = smat.SMAT_ACT_SILU
+    for views, copies in ((layers.linear(x, w1, b1), layers.linear(x, c[0], c[1])),
+                          (layers.mlp(x, w1, b1, w2, b2, act), layers.mlp(x, c[0], c[1], c[2], c[3], act)),
+                          (layers.gated_mlp(x, w1, wu, w2), layers.gated_mlp(x, c[0], c[4], c[2]))):
+        assert torch.equal(views, copies)
+        dy = rand(gen, *views.shape)
+        got = torch.autograd.grad(views, [x] + leaves, dy, allow_unused=True)
+        want = torch.autograd.grad(copies, [x] + leaves, dy, allow_unused=True, retain_graph=True)
+        for g, w in zip(got, want):
+            assert (g is None) == (w is None) and (g is None or torch.equal(g, w))
+    with torch.no_grad():
+        assert torch.equal(layers.linear(x, w1, b1), layers.linear(x, c[0], c[1]))
+    for bad in (rand(gen, d), rand(gen, 2, f, d), torch.tensor(1.0, device=DEV)):
+        with pytest.raises(smat.SmatError):
+            layers.linear(x, bad)
