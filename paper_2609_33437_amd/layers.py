@@ -35,7 +35,9 @@ from ._linear import (SMAT_ACT_NONE, SMAT_ACT_SILU, ActCheckpoint, smat_ckpt_rea
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
     """x [.., k] as a matrix of contiguous rows."""
-    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+    if x.dim() == 0:
+        raise SmatError(SMAT_ERR_INVALID, "the layers take tensors with a last dimension")
+    m = x if x.dim() == 2 else x.reshape(x.shape[:-1].numel(), x.shape[-1])
     if m.shape[1] > 1 and m.stride(1) != 1 or m.shape[0] > 1 and m.stride(0) < m.shape[1]:
         m = m.contiguous()
     return m

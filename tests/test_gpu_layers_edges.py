@@ -159,3 +159,29 @@ def test_weights_and_biases_of_any_layout():
     for bad in (rand(gen, d), rand(gen, 2, f, d), torch.tensor(1.0, device=DEV)):
         with pytest.raises(smat.SmatError):
             layers.linear(x, bad)
+
+
+@pytest.mark.parametrize("lead", [(2, 3), (6,), (), (0, 3), (2, 0)])
+@pytest.mark.parametrize("d,f,n", [(0, 96, 64), (64, 0, 64), (64, 96, 0), (0, 0, 0), (1, 1, 1)])
+def test_dimensions_of_zero(lead, d, f, n):
+    """Empty sums, empty results and empty batches in every position, forward and backward, as torch's layers have them."""
+    gen = torch.Generator(DEV).manual_seed(7)
+    lin = torch.nn.functional.linear
+    t = dict(x=rand(gen, *lead, d), w1=rand(gen, f, d, std=0.1), b1=rand(gen, f), w2=rand(gen, n, f, std=0.1), b2=rand(gen, n),
+             wu=rand(gen, f, d, std=0.1), r=rand(gen, *lead, n))
+    x, w1, b1, w2, b2, wu, r = (v.requires_grad_(True) for v in t.values())
+    silu = torch.nn.functional.silu
+    for got, want in ((layers.linear(x, w1, b1), lin(x, w1, b1)),
+                      (layers.mlp(x, w1, b1, w2, b2, smat.SMAT_ACT_SILU, residual=r), lin(silu(lin(x, w1, b1)), w2, b2) + r),
+                      (layers.gated_mlp(x, w1, wu, w2, residual=r), lin(silu(lin(x, w1)) * lin(x, wu), w2) + r)):
+        assert got.shape == want.shape
+        assert torch.allclose(got, want, rtol=1e-4, atol=1e-4)
+        g = torch.autograd.grad(got.sum(), (x, w1, b1, w2, wu), allow_unused=True)
+        e = torch.autograd.grad(want.sum(), (x, w1, b1, w2, wu), allow_unused=True)
+        for a, b in zip(g, e):
+            assert (a is None) == (b is None)
+            if a is not None:
+                assert a.shape == b.shape and torch.isfinite(a).all()
+                assert (a - b).norm() <= 0.05 * b.norm()      # 8 bits of the saved activations, small sums
+    with pytest.raises(smat.SmatError):
+        layers.linear(torch.tensor(1.0, device=DEV), w1)
