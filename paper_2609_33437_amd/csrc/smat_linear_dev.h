@@ -101,12 +101,13 @@ template <typename T>
 __device__ __forceinline__ float logistic(float x) {
   return act_rcp<T>(1.f + act_exp<T>(-x));
 }
-// The logistic function and 1 minus it, without the subtraction's cancellation.
+// The logistic function and 1 minus it, without the subtraction's cancellation.  Where exp(-x) overflows the first is 0, as
+// logistic() has it, and the second need only be finite: it stands beside a factor of the first.
 template <typename T>
 __device__ __forceinline__ void logistic_both(float x, float& g, float& h) {
-  const float e = fminf(act_exp<T>(-x), 1e38f);
+  const float e = act_exp<T>(-x);
   g = act_rcp<T>(1.f + e);
-  h = e * g;
+  h = fminf(e, 1e38f) * g;
 }
 // The standard normal's distribution function at z, and exp(-z^2 / 2).  (The coefficients carry the half.)
 template <typename T>
