@@ -32,7 +32,7 @@ template <typename T, bool FLAT, typename Index>
 __global__ __launch_bounds__(kCkptThreads) void k_ckpt_write(const typename El<T>::Mem* __restrict__ x, int64_t ld,
                                                              int64_t cols, Index across, int64_t total,
                                                              int8_t* __restrict__ codes, uint8_t* __restrict__ exps) {
-  const int64_t t = (int64_t)blockIdx.x * kCkptThreads + threadIdx.x;
+  const int64_t t = wide_block() * kCkptThreads + threadIdx.x;
   if (t >= total) return;
   int64_t at, valid;
   eight_place<FLAT, Index>((Index)t, across, ld, cols, at, valid);
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kCkptThreads) void k_ckpt_read(const int8_t* __rest
                                                             const uint8_t* __restrict__ up_exps, int act, int64_t cols,
                                                             Index across, int64_t total,
                                                             typename El<T>::Mem* __restrict__ out, int64_t ldout) {
-  const int64_t t = (int64_t)blockIdx.x * kCkptThreads + threadIdx.x;
+  const int64_t t = wide_block() * kCkptThreads + threadIdx.x;
   if (t >= total) return;
   const u32x2 z = *reinterpret_cast<const u32x2*>(codes + t * 8);
   const uint32_t z_byte = exps[t / 4];
@@ -91,7 +91,7 @@ void with_element(int dtype, F&& fn) {
   else
     fn(float());
 }
-dim3 ckpt_grid(int64_t total) { return dim3((uint32_t)((total + kCkptThreads - 1) / kCkptThreads)); }
+dim3 ckpt_grid(int64_t total) { return wide_grid((total + kCkptThreads - 1) / kCkptThreads); }
 
 // fn(element type, whether the rows are whole blocks end to end, type of an eight's number) of a call.
 template <typename F>

@@ -17,6 +17,15 @@ namespace smat {
 constexpr int kCkptBlock = 32;  // elements along a row that share a checkpoint's power of two
 inline int64_t ckpt_blocks(int64_t cols) { return (cols + kCkptBlock - 1) / kCkptBlock; }
 
+// A launch whose grid has 2^32 threads or more in a dimension does less than it was asked, without an error.
+constexpr int64_t kMaxThreads = INT64_C(0xFFFFFFFF);
+// Grids of kernels that may need more: rows of 2^20 blocks, numbered by wide_block() in the kernel.
+constexpr int kWideShift = 20;
+inline dim3 wide_grid(int64_t blocks) {
+  constexpr int64_t kRow = (int64_t)1 << kWideShift;
+  return blocks <= kRow ? dim3((uint32_t)blocks) : dim3((uint32_t)kRow, (uint32_t)((blocks + kRow - 1) >> kWideShift));
+}
+
 enum LinEpilogue : int { kEpiStore = 0, kEpiLayer = 1, kEpiDgrad = 2 };
 
 struct LinProduct {

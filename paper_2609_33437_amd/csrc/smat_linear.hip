@@ -1022,7 +1022,7 @@ __global__ __launch_bounds__(kSumThreads) void k_column_sum(const typename El<T>
                 kAhead = 4;
   __shared__ float s[kRows][COLS + 1];
   const int sub = (int)threadIdx.x / kLanes, c = (int)threadIdx.x % kLanes * 8;
-  const int64_t j0 = (int64_t)blockIdx.x * COLS + c, valid = cols - j0;
+  const int64_t j0 = wide_block() * COLS + c, valid = cols - j0;
   float v[8] = {};
   if (valid >= 8) {
     // kAhead rows' loads together; past the last row they repeat it and add nothing
@@ -1061,7 +1061,7 @@ __global__ __launch_bounds__(kSumThreads) void k_column_sum(const typename El<T>
   __syncthreads();
   s[part][col] = sum;
   __syncthreads();
-  const int64_t j = (int64_t)blockIdx.x * COLS + col;
+  const int64_t j = wide_block() * COLS + col;
   if (part == 0 && j < cols) {
     sum = 0.f;
 #pragma unroll
@@ -1120,17 +1120,17 @@ using TinyShape = GroupShape<16, 32, 1, 1, 4, 3>;    // 16 x 32, r in four, two 
 // takes together (its groups), and measured microseconds: of a stage with as many blocks on each unit, of one with one
 // block a unit, and of a block's start and end.
 struct FormCost {
-  int32_t form, i, j, resident, groups;
+  int32_t form, i, j, threads, resident, groups;
   double stage, alone, rest;
 };
 template <typename S>
 constexpr FormCost cost(int32_t form, double stage, double alone, double rest) {
-  return {form, S::kI, S::kJ, S::kResident, S::G, stage, alone, rest};
+  return {form, S::kI, S::kJ, S::kThreads, S::kResident, S::G, stage, alone, rest};
 }
 // bf16 with stages copied to LDS directly, by how many operands are transposed; the same by way of registers, where
 // the other tiles are slower than these at every size tried (64 x 64, one wave a SIMD, twice as long); fp32 both ways,
 // whose matrix instructions take 16 times as long.
-constexpr FormCost direct_fast(double stage) { return {kFast, kFastB, kFastB, 1, 1, stage, stage, 10.0}; }
+constexpr FormCost direct_fast(double stage) { return {kFast, kFastB, kFastB, kFastThreads, 1, 1, stage, stage, 10.0}; }
 const FormCost kDirectCosts[3][6] = {
     {direct_fast(1.40), cost<MiddleShape>(kMiddle, 0.90, 0.66, 6.0), cost<SmallShape>(kSmall, 0.92, 0.92, 5.2),
      cost<NarrowShape>(kNarrow, 0.55, 0.55, 5.0), cost<TinyShape>(kTiny, 0.45, 0.28, 4.2),
@@ -1162,9 +1162,12 @@ struct Sizes {
   int64_t line;  // columns of a transposed Q in a cache line, or 0
 };
 
-// Microseconds of `splits` ranges of r with tile f.
+// Microseconds of `splits` ranges of r with tile f, or kNever where its grid cannot be launched.
+constexpr double kNever = 1e30;
 double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
-  const int64_t blocks = div_up(z.i, f.i) * div_up(z.j, f.j) * splits, slots = (int64_t)kComputeUnits * f.resident;
+  const int64_t tiles = div_up(z.i, f.i) * div_up(z.j, f.j), blocks = tiles * splits;
+  const int64_t slots = (int64_t)kComputeUnits * f.resident;
+  if (tiles > kMaxThreads / f.threads) return kNever;
   const int64_t rounds = blocks / slots, left = blocks % slots;
   const double steps = (double)div_up(z.stages, splits * f.groups);
   const double end = splits > 1 ? 0.0 : z.epilogue * (double)(f.i * f.j) / 65536.0;
@@ -1189,7 +1192,8 @@ double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
 
 // The least-time tile and number of ranges of r by those costs.  Ranges beyond one block a place only cost.
 double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part) {
-  double least = 1e30;
+  double least = kNever;
+  part = {z.i, 0, 1};
   for (int c = 0; c < count; ++c) {
     const FormCost& f = costs[c];
     const int64_t tiles = div_up(z.i, f.i) * div_up(z.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
@@ -1288,8 +1292,8 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       best.pack = off;
     }
   }
-  // few rows: the kernel that takes operands of any alignment without a copy
-  if (epi == kEpiLayer && a.i <= kMaxRows) {
+  // few rows: the kernel that takes operands of any alignment without a copy (16 threads a column where there are many)
+  if (epi == kEpiLayer && a.i <= kMaxRows && a.j <= kMaxThreads / 16 - 32) {
     const double rate = kRowsRate[a.i > 4 ? 3 : a.i > 2 ? 2 : a.i - 1];
     if (kRowsStart + z.bytes / rate <= least) {
       best = LinPlan{};
@@ -1396,6 +1400,7 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
         (k % 2 ? pr.q : pr.p) = to;
         (k % 2 ? pr.ldq : pr.ldp) = ld;
       }
+    if (jobs.blocks > kMaxThreads / 256) return hipErrorInvalidConfiguration;
     with_element(dtype, [&](auto t) { k_pack<decltype(t)><<<dim3(jobs.blocks), dim3(256), 0, stream>>>(jobs); });
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
@@ -1405,6 +1410,8 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
     LinArgs a = rows_of(whole, from, part.rows, bytes, epi == kEpiStore);
     a.splits = part.splits;
     from += part.rows;
+    const int64_t eights = a.i * ckpt_blocks(a.j) * 4;  // of the join
+    if (part.form == 0 || (a.splits > 1 && eights > kMaxThreads - 256)) return hipErrorInvalidConfiguration;
     with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {
       using T = decltype(t);
       if constexpr (std::is_same<T, Bf16>::value) {
@@ -1425,7 +1432,7 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
       }
       if (part.form == kTiny) e = launch_group<TinyShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
       if (e != hipSuccess || a.splits <= 1) return;
-      k_linear_join<T, ep()><<<dim3((uint32_t)div_up(a.i * ckpt_blocks(a.j) * 4, 256)), dim3(256), 0, stream>>>(a);
+      k_linear_join<T, ep()><<<dim3((uint32_t)div_up(eights, 256)), dim3(256), 0, stream>>>(a);
       e = hipGetLastError();
     });
   }
@@ -1438,7 +1445,7 @@ hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t c
     using T = decltype(t);
     using Mem = typename El<T>::Mem;
     const auto launch = [&](auto n) {
-      k_column_sum<T, n()><<<dim3((uint32_t)div_up(cols, n())), dim3(kSumThreads), 0, stream>>>(
+      k_column_sum<T, n()><<<wide_grid(div_up(cols, n())), dim3(kSumThreads), 0, stream>>>(
           static_cast<const Mem*>(dy), ld, rows, cols, static_cast<Mem*>(db));
     };
     if (cols >= 32 * kComputeUnits)

@@ -13,6 +13,8 @@ namespace smat {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+__device__ __forceinline__ int64_t wide_block() { return ((int64_t)blockIdx.y << kWideShift) + blockIdx.x; }
+
 // ---------------------------------------------------------------- element types
 template <typename T>
 struct El;
