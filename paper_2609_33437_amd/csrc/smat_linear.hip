@@ -246,7 +246,7 @@ __device__ __forceinline__ void copy_to_lds(i32x4 rsrc, uint32_t offset, uint32_
   asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(lds), "v"(offset), "s"(rsrc), "n"(PLUS)
-               : "memory", "scc", "m0");
+               : "memory", "scc");
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer
 
