@@ -7,7 +7,7 @@ import paper_2609_33437_amd as smat
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
-PIECE = 1 << 26
+PIECE = 1 << 22
 
 
 def ternary(gen, rows, cols):
