@@ -165,7 +165,7 @@ def smat_linear(x, w, out, bias=None, act: int = SMAT_ACT_NONE, mul=None, residu
     """out = act(x w^T + bias) (.) mul + residual; z_ckpt receives the checkpoint of x w^T + bias."""
     code = _first(x, "x")
     m, k = x.shape
-    n = w.shape[0]
+    n = w.shape[0] if w.dim() == 2 else -1
     a = smat_linear_args(dtype=code, act=int(act), m=m, n=n, k=k)
     a.x, a.ldx = _matrix(x, m, k, x, "x")
     a.w, a.ldw = _matrix(w, n, k, x, "w")

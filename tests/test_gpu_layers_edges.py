@@ -185,3 +185,16 @@ def test_dimensions_of_zero(lead, d, f, n):
                 assert (a - b).norm() <= 0.05 * b.norm()      # 8 bits of the saved activations, small sums
     with pytest.raises(smat.SmatError):
         layers.linear(torch.tensor(1.0, device=DEV), w1)
+
+
+def test_arguments_that_are_no_matrices():
+    """The calls refuse tensors of every other number of dimensions themselves."""
+    good = dict(x=torch.ones(4, 8, device=DEV), w=torch.ones(6, 8, device=DEV), out=torch.ones(4, 6, device=DEV))
+    dgrad = dict(dy=torch.ones(4, 6, device=DEV), w=torch.ones(6, 8, device=DEV), out=torch.ones(4, 8, device=DEV))
+    wgrad = dict(dy=torch.ones(4, 6, device=DEV), x=torch.ones(4, 8, device=DEV), dw=torch.ones(6, 8, device=DEV))
+    for fn, args in ((smat.smat_linear, good), (smat.smat_linear_dgrad, dgrad), (smat.smat_linear_wgrad, wgrad)):
+        fn(**args)
+        for name in args:
+            for bad in (torch.tensor(1.0, device=DEV), torch.ones(8, device=DEV), torch.ones(2, 4, 8, device=DEV)):
+                with pytest.raises(smat.SmatError):
+                    fn(**{**args, name: bad})
