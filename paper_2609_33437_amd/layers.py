@@ -35,6 +35,8 @@ from ._linear import (SMAT_ACT_NONE, SMAT_ACT_SILU, ActCheckpoint, smat_ckpt_rea
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
     """x [.., k] as a matrix of contiguous rows."""
+    if x.dim() == 2 and x.is_contiguous():
+        return x
     if x.dim() == 0:
         raise SmatError(SMAT_ERR_INVALID, "the layers take tensors with a last dimension")
     m = x if x.dim() == 2 else x.reshape(x.shape[:-1].numel(), x.shape[-1])
@@ -81,9 +83,10 @@ def _sum(y: torch.Tensor, after: Optional[torch.Tensor]) -> torch.Tensor:
     return y if after is None else after + y
 
 
-def _device(x: torch.Tensor):
-    """x's GPU as the current one, which a model split over GPUs does not set.  (Autograd sets it for the backward.)"""
-    return torch.cuda.device(x.get_device())
+def _elsewhere(x: torch.Tensor) -> bool:
+    """Whether x's GPU is not the current one, which a model split over GPUs does not set.  The public functions enter it
+    then; autograd does for the backward."""
+    return x.is_cuda and x.get_device() != torch._C._cuda_getDevice()
 
 
 def _saves(*tensors) -> bool:
@@ -91,7 +94,8 @@ def _saves(*tensors) -> bool:
     weights and no_grad too, are refused (the recorded functions raise on them themselves)."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         return True
-    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(      # -1: no tangents are about
+            t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
         raise SmatError(SMAT_ERR_INVALID, "the layers have no forward-mode derivatives")
     return False
 
@@ -253,49 +257,55 @@ class _GatedMlp(torch.autograd.Function):
 # ------------------------------------------------------------------ public functions
 def linear(x, weight, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x weight^T + bias + residual for x [.., k]; the weight gradient reads x from an 8-bit checkpoint."""
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return linear(x, weight, bias, residual)
     x, weight, bias = _cast(x, weight, bias)
     weight, bias = _weight(weight), _bias(bias)
     shape, x = x.shape[:-1] + weight.shape[:1], _rows(x)
     r, after = _residual(residual, x, shape)
-    with _device(x):
-        if _saves(x, weight, bias, r):
-            return _sum(_Linear.apply(x, weight, bias, r).view(shape), after)
-        out = torch.empty(x.shape[0], weight.shape[0], dtype=x.dtype, device=x.device)
-        smat_linear(x, weight, out, bias=bias, residual=r)
-        return _sum(out.view(shape), after)
+    if _saves(x, weight, bias, r):
+        return _sum(_Linear.apply(x, weight, bias, r).view(shape), after)
+    out = torch.empty(x.shape[0], weight.shape[0], dtype=x.dtype, device=x.device)
+    smat_linear(x, weight, out, bias=bias, residual=r)
+    return _sum(out.view(shape), after)
 
 
 def mlp(x, w1, b1, w2, b2, act: int, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(x w1^T + b1) w2^T + b2 + residual for x [.., d] (biases and residual may be None)."""
     if act == SMAT_ACT_NONE:
         raise SmatError(SMAT_ERR_INVALID, "an MLP needs an activation")
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return mlp(x, w1, b1, w2, b2, act, residual)
     x, w1, b1, w2, b2 = _cast(x, w1, b1, w2, b2)
     w1, b1, w2, b2 = _weight(w1), _bias(b1), _weight(w2), _bias(b2)
     shape, x = x.shape[:-1] + w2.shape[:1], _rows(x)
     r, after = _residual(residual, x, shape)
-    with _device(x):
-        if _saves(x, w1, b1, w2, b2, r):
-            return _sum(_Mlp.apply(x, w1, b1, w2, b2, r, int(act)).view(shape), after)
-        h = torch.empty(x.shape[0], w1.shape[0], dtype=x.dtype, device=x.device)
-        smat_linear(x, w1, h, bias=b1, act=act)
-        out = torch.empty(x.shape[0], w2.shape[0], dtype=x.dtype, device=x.device)
-        smat_linear(h, w2, out, bias=b2, residual=r)
-        return _sum(out.view(shape), after)
+    if _saves(x, w1, b1, w2, b2, r):
+        return _sum(_Mlp.apply(x, w1, b1, w2, b2, r, int(act)).view(shape), after)
+    h = torch.empty(x.shape[0], w1.shape[0], dtype=x.dtype, device=x.device)
+    smat_linear(x, w1, h, bias=b1, act=act)
+    out = torch.empty(x.shape[0], w2.shape[0], dtype=x.dtype, device=x.device)
+    smat_linear(h, w2, out, bias=b2, residual=r)
+    return _sum(out.view(shape), after)
 
 
 def gated_mlp(x, w_gate, w_up, w_down, act: int = SMAT_ACT_SILU,
               residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """(act(x w_gate^T) (.) (x w_up^T)) w_down^T + residual for x [.., d] (SwiGLU with the default act)."""
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return gated_mlp(x, w_gate, w_up, w_down, act, residual)
     x, w_gate, w_up, w_down = _cast(x, w_gate, w_up, w_down)
     w_gate, w_up, w_down = _weight(w_gate), _weight(w_up), _weight(w_down)
     shape, x = x.shape[:-1] + w_down.shape[:1], _rows(x)
     r, after = _residual(residual, x, shape)
-    with _device(x):
-        if _saves(x, w_gate, w_up, w_down, r):
-            return _sum(_GatedMlp.apply(x, w_gate, w_up, w_down, r, int(act)).view(shape), after)
-        h = torch.empty(x.shape[0], w_gate.shape[0], dtype=x.dtype, device=x.device)
-        smat_linear(x, w_up, h)
-        smat_linear(x, w_gate, h, act=act, mul=h)
-        out = torch.empty(x.shape[0], w_down.shape[0], dtype=x.dtype, device=x.device)
-        smat_linear(h, w_down, out, residual=r)
-        return _sum(out.view(shape), after)
+    if _saves(x, w_gate, w_up, w_down, r):
+        return _sum(_GatedMlp.apply(x, w_gate, w_up, w_down, r, int(act)).view(shape), after)
+    h = torch.empty(x.shape[0], w_gate.shape[0], dtype=x.dtype, device=x.device)
+    smat_linear(x, w_up, h)
+    smat_linear(x, w_gate, h, act=act, mul=h)
+    out = torch.empty(x.shape[0], w_down.shape[0], dtype=x.dtype, device=x.device)
+    smat_linear(h, w_down, out, residual=r)
+    return _sum(out.view(shape), after)
