@@ -539,7 +539,7 @@ smat_status smat_stream_copy(const void* src, void* dst, uint64_t bytes, hipStre
  * gradients, and the activations that a training step saves between them, held in 8 bits.
  *
  * Matrices are row-major with a row stride ld in elements (ld >= columns) and contiguous rows, at any
- * element's alignment; dimensions are at most 2^31 - 1 and rows * ld below 2^60.  A call's matrices have one dtype (SMAT_F32 or
+ * element's alignment; dimensions are at most 2^31 - 1 and rows * ld at most 2^60 bytes.  A call's matrices have one dtype (SMAT_F32 or
  * SMAT_BF16); products and epilogues are computed in fp32 (bf16 products are exact there) and each output is
  * rounded once.  A dimension of 0 is valid: no output, or, where the summed dimension is 0, an empty sum.
  * Outputs must not overlap inputs or each other, except that `out` may be `mul` or `residual`
@@ -642,7 +642,8 @@ typedef struct smat_linear_wgrad_args {
   void* db;                /* [n], or NULL */
 } smat_linear_wgrad_args;
 
-/* smat_linear_wgrad -- the gradients of a layer's weight and bias; the same bits in every run.  Errors:
+/* smat_linear_wgrad -- the gradients of a layer's weight and bias; the same bits in every run.  A checkpoint of x is
+ * read back into the workspace first, at x's size in the call's dtype.  Errors:
  * SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
 smat_status smat_linear_wgrad_workspace_bytes(const smat_linear_wgrad_args* args, size_t* bytes);
 smat_status smat_linear_wgrad(const smat_linear_wgrad_args* args, void* workspace, size_t workspace_bytes,

@@ -21,7 +21,9 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 //
 // Chunks are exchanged within their row (an exclusive or) so that the lanes that read together reach
 // different banks: by the row's number in P, and in Q, whose lanes read rows q_row, by the bits of the row
-// that differ between them.
+// that differ between them.  Direct operands have no conflicts so.  Transposed ones keep some: a quarter to a third of the
+// active LDS cycles with 128 columns a stage, where the exchange has all its bits, and 0.61 of them with 64 (a weight gradient
+// of 1999; 2048 x 257), whose rows have half as many chunks; with 32 Q's chunks are not exchanged at all.
 __device__ __forceinline__ constexpr int q_row(int r, int t) { return (r >> 2) * 8 + t * 4 + (r & 3); }
 template <bool Q>
 __device__ __forceinline__ int direct_swizzle(int row) {
@@ -1009,9 +1011,9 @@ __global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
 // ---------------------------------------------------------------- column sums
 // A block sums COLS columns over all rows: COLS / 8 lanes hold a row's, and the sums are added through LDS in the
 // rows' order, so one launch and no workspace do.  Bound by memory where there are enough columns (8192 x 14336 bf16
-// adds 34 us to a weight gradient, 6.9 TB/s), else by how much its few blocks keep in flight: 32 columns a block there
-// (1999 x 2048 6.2 us, with 64 columns a block 9.5).  Blocks of 32 bf16 columns read half cache lines, which costs where
-// memory is the bound.
+// takes 49 us with dy in HBM, 4.8 TB/s, 40 us with the same dy in every call, and adds 44 us to a weight gradient), else by
+// how much its few blocks keep in flight: 32 columns a block there (1999 x 2048 6.2 us, with 64 columns a block 9.5).  Blocks
+// of 32 bf16 columns read half cache lines, which costs where memory is the bound.
 constexpr int kSumThreads = 1024;
 
 template <typename T, int COLS>
@@ -1148,7 +1150,8 @@ const FormCost kFp32Costs[] = {cost<MiddleShape>(kMiddle, 3.95, 2.1, 7.0), cost<
                                cost<TinyShape>(kTiny, 0.6, 0.32, 4.5)};
 const FormCost kFp32StagedCosts[] = {cost<MiddleShape>(kMiddle, 4.65, 2.5, 7.0), cost<TinyShape::Staged>(kTiny, 1.2, 0.75, 5.0)};
 
-// The kernel for few rows of x: its start, and the bytes a microsecond that it reads with 1, 2, 4 and 8 rows.  Against
+// The kernel for few rows of x: its start, and the bytes a microsecond that it reads with 1, 2, 4 and 8 rows of bf16 (fp32
+// is chosen by the same: 14336 x 4096 takes 45 us with 1 or 2 rows, 52 with 5 or 8, 5.2 and 4.5 TB/s).  Against
 // 16 x 32 tiles with 5 rows: 14336 x 4096 31.5 us (23.6), 4096 x 4096 10.2 (9.8), 2048 x 2048 5.6 (6.2), 960 x 4096 7.0
 // (7.7); with 3 rows 25.6 (23.4), 8.8 (9.8), 4.8 (6.2) and 5.0 (7.7).
 constexpr double kRowsStart = 3.5, kRowsRate[4] = {5.8e6, 5.6e6, 4.9e6, 3.8e6};

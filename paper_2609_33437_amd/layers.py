@@ -5,8 +5,8 @@ The forward passes run as products with their bias, activation, gate and residua
 a value (ActCheckpoint): a layer's input, and the pre-activations, written by the product's own
 epilogue.  The hidden activation of an MLP is not saved at all; the backward recomputes it from the
 pre-activations (smat_ckpt_read), takes the data gradient through the activation in the product's
-epilogue (smat_linear_dgrad) and reads the input's checkpoint in the weight gradient
-(smat_linear_wgrad).  A token's MLP of width d and ffn f keeps d + f (act) or d + 2 f (gated) values of about a
+epilogue (smat_linear_dgrad) and takes the weight gradient from the input's checkpoint, which the call reads
+back into its workspace (smat_linear_wgrad; once for each weight, the gate's and the up projection's).  A token's MLP of width d and ffn f keeps d + f (act) or d + 2 f (gated) values of about a
 byte, against d + 2 f or d + 3 f of two bytes.
 
 Gradients are those of the checkpointed values: they differ from exact ones by what 8 bits lose of the
