@@ -649,6 +649,152 @@ smat_status smat_linear_wgrad_workspace_bytes(const smat_linear_wgrad_args* args
 smat_status smat_linear_wgrad(const smat_linear_wgrad_args* args, void* workspace, size_t workspace_bytes,
                               hipStream_t stream);
 
+/* ---------------------------------------------------------------- norms, token embedding, output layer with its loss
+ * What a decoder has beside attention and the linear layers above.  Conventions as there: row-major matrices with a row
+ * stride, at any element's alignment; fp32 arithmetic, each output rounded once; outputs overlap neither inputs nor
+ * each other nor the workspace; the calls can be captured into a graph, and their results are the same bits in every run. */
+
+typedef enum smat_norm_kind {
+  SMAT_NORM_LAYER = 0, /* y = (x - mean) rstd w + b, mean = mean x, rstd = 1 / sqrt(mean (x - mean)^2 + eps) */
+  SMAT_NORM_RMS = 1    /* y = x rstd w + b, rstd = 1 / sqrt(mean x^2 + eps) */
+} smat_norm_kind;
+
+/* Arguments of smat_norm, over the n columns of each of m rows. */
+typedef struct smat_norm_args {
+  int32_t dtype, wdtype;   /* smat_dtype of x and y, and of weight and bias */
+  int32_t kind;            /* smat_norm_kind */
+  float eps;               /* finite, >= 0 */
+  int64_t m, n;
+  const void* x;           /* [m, n] */
+  int64_t ldx;
+  const void* weight;      /* [n], or NULL: ones */
+  const void* bias;        /* [n], or NULL: zeros */
+  void* y;                 /* [m, n] */
+  int64_t ldy;
+  float* mean;             /* [m], or NULL (0 for SMAT_NORM_RMS) */
+  float* rstd;             /* [m], or NULL */
+} smat_norm_args;
+
+/* smat_norm -- the rows of x normalised.  With n = 0 nothing is written.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE,
+ * SMAT_ERR_HIP. */
+smat_status smat_norm(const smat_norm_args* args, hipStream_t stream);
+
+/* Arguments of smat_norm_grad: with xh = (x - mean) rstd and g = dy w,
+ *   dx = rstd (g - xh mean(g xh) - mean(g))       SMAT_NORM_LAYER
+ *   dx = rstd (g - xh mean(g xh))                 SMAT_NORM_RMS
+ *   dweight = the column sums of dy xh, dbias = the column sums of dy */
+typedef struct smat_norm_grad_args {
+  int32_t dtype, wdtype;   /* smat_dtype of dy, x and dx, and of weight, dweight and dbias */
+  int32_t kind, reserved;  /* smat_norm_kind; reserved must be 0 */
+  int64_t m, n;
+  const void* dy;          /* [m, n] */
+  int64_t lddy;
+  const void* x;           /* [m, n] */
+  int64_t ldx;
+  const void* weight;      /* [n], or NULL: ones */
+  const float* mean;       /* [m], as smat_norm wrote it; not read for SMAT_NORM_RMS */
+  const float* rstd;       /* [m], as smat_norm wrote it */
+  void* dx;                /* [m, n], or NULL: not wanted */
+  int64_t lddx;
+  void* dweight;           /* [n], or NULL */
+  void* dbias;             /* [n], or NULL */
+} smat_norm_grad_args;
+
+/* smat_norm_grad -- the gradients of a norm.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+smat_status smat_norm_grad_workspace_bytes(const smat_norm_grad_args* args, size_t* bytes);
+smat_status smat_norm_grad(const smat_norm_grad_args* args, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Arguments of smat_embed: row i of out = scale * row ids[i] of table. */
+typedef struct smat_embed_args {
+  int32_t dtype, table_dtype; /* smat_dtype of out, and of table */
+  float scale;                /* finite */
+  int32_t reserved;           /* must be 0 */
+  int64_t m, rows, d;
+  const void* table;          /* [rows, d] */
+  int64_t ldtable;
+  const int64_t* ids;         /* [m]; an id outside [0, rows) gives a row of NaN */
+  void* out;                  /* [m, d] */
+  int64_t ldout;
+} smat_embed_args;
+
+/* smat_embed -- rows of a table by id.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+smat_status smat_embed(const smat_embed_args* args, hipStream_t stream);
+
+/* Arguments of smat_embed_grad: row v of dtable = scale * the sum of the rows dy[i] with ids[i] = v, zeros where there are
+ * none; with accumulate that is added to dtable, whose other rows keep their bits.  Ids equal to `padding` and ids outside
+ * [0, rows) take part in no row. */
+typedef struct smat_embed_grad_args {
+  int32_t dtype, table_dtype; /* smat_dtype of dy, and of dtable */
+  float scale;                /* finite */
+  int32_t accumulate;         /* 0 or 1 */
+  int64_t m, rows, d;
+  int64_t padding;            /* an id without a gradient; negative: none */
+  const void* dy;             /* [m, d] */
+  int64_t lddy;
+  const int64_t* ids;         /* [m] */
+  void* dtable;               /* [rows, d] */
+  int64_t ldtable;
+} smat_embed_grad_args;
+
+/* smat_embed_grad -- the gradient of a table.  Tokens are sorted by id and a row's summed in fp32 in their order, in runs of
+ * at least 32 whose sums are then added.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+smat_status smat_embed_grad_workspace_bytes(const smat_embed_grad_args* args, size_t* bytes);
+smat_status smat_embed_grad(const smat_embed_grad_args* args, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Arguments of smat_linear_xent: the cross entropy of the logits z = x W^T against targets, without storing z.
+ *   lse[i] = log sum_j exp z[i][j], loss[i] = lse[i] - z[i][targets[i]]
+ * A target of ignore_index marks a row without one: its loss is 0.  Another target outside [0, n) gives a loss of NaN. */
+typedef struct smat_linear_xent_args {
+  int32_t dtype, reserved; /* smat_dtype of x and w; reserved must be 0 */
+  int64_t m, n, k;         /* rows, classes (> 0), width */
+  const void* x;           /* [m, k] */
+  int64_t ldx;
+  const void* w;           /* [n, k] */
+  int64_t ldw;
+  const int64_t* targets;  /* [m] */
+  int64_t ignore_index;
+  float* loss;             /* [m] */
+  float* lse;              /* [m] */
+  float* totals;           /* [3], or NULL: the sum of the losses, the number of rows with a target, and their quotient
+                              (NaN where there is none) */
+} smat_linear_xent_args;
+
+/* smat_linear_xent -- an output layer with its loss, from single tokens (m = 1) up.  Errors: SMAT_ERR_INVALID,
+ * SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+smat_status smat_linear_xent_workspace_bytes(const smat_linear_xent_args* args, size_t* bytes);
+smat_status smat_linear_xent(const smat_linear_xent_args* args, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/* Arguments of smat_linear_xent_grad: the gradients of s * sum_i row_scale[i] loss[i],
+ *   dz[i][j] = (exp(z[i][j] - lse[i]) - [j = targets[i]]) row_scale[i]      0 in rows without a target
+ *   dx = s dz W,  dW = s dz^T x,  s = scale[0] / totals[1]
+ * The vocabulary is taken in pieces: z is computed again and dz, rounded to dtype, held for one piece (in the workspace), so
+ * nothing of the size m * n is stored.  s multiplies the fp32 sums; it is 0 where totals[1] is. */
+typedef struct smat_linear_xent_grad_args {
+  int32_t dtype, reserved; /* smat_dtype of x, w, dx and dw; reserved must be 0 */
+  int64_t m, n, k;
+  const void* x;           /* [m, k] */
+  int64_t ldx;
+  const void* w;           /* [n, k] */
+  int64_t ldw;
+  const int64_t* targets;  /* [m] */
+  int64_t ignore_index;
+  const float* lse;        /* [m], as smat_linear_xent wrote it */
+  const float* row_scale;  /* [m], or NULL: ones */
+  const float* scale;      /* [1] in device memory, or NULL: 1 */
+  const float* totals;     /* [3], as smat_linear_xent wrote it, or NULL: no division (the gradient of a sum) */
+  void* dx;                /* [m, k], or NULL: not wanted */
+  int64_t lddx;
+  void* dw;                /* [n, k], or NULL */
+  int64_t lddw;
+} smat_linear_xent_grad_args;
+
+/* smat_linear_xent_grad -- the gradients of an output layer from its loss.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE,
+ * SMAT_ERR_HIP. */
+smat_status smat_linear_xent_grad_workspace_bytes(const smat_linear_xent_grad_args* args, size_t* bytes);
+smat_status smat_linear_xent_grad(const smat_linear_xent_grad_args* args, void* workspace, size_t workspace_bytes,
+                                  hipStream_t stream);
+
 /* smat_last_error -- message of the last failure on the calling thread ("" if none). */
 const char* smat_last_error(void);
 

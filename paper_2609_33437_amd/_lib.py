@@ -21,6 +21,7 @@ SMAT_F32, SMAT_BF16 = 0, 1
 SMAT_NOISE_GAUSSIAN, SMAT_NOISE_UNIFORM, SMAT_NOISE_LAPLACE = 0, 1, 2
 SMAT_EXPERT, SMAT_SIMULATED = 0, 1
 SMAT_ACT_NONE, SMAT_ACT_GELU, SMAT_ACT_GELU_TANH, SMAT_ACT_SILU = 0, 1, 2, 3
+SMAT_NORM_LAYER, SMAT_NORM_RMS = 0, 1
 
 STATUS_NAMES = {0: "SMAT_OK", 1: "SMAT_ERR_INVALID", 2: "SMAT_ERR_DTYPE", 3: "SMAT_ERR_STATE", 4: "SMAT_ERR_HIP"}
 
@@ -36,6 +37,9 @@ EXPORTS = (
     "smat_scale_draw", "smat_simulate_multi_static",
     "smat_ckpt_write", "smat_ckpt_read", "smat_linear", "smat_linear_workspace_bytes", "smat_linear_dgrad",
     "smat_linear_dgrad_workspace_bytes", "smat_linear_wgrad", "smat_linear_wgrad_workspace_bytes",
+    "smat_norm", "smat_norm_grad", "smat_norm_grad_workspace_bytes", "smat_embed", "smat_embed_grad",
+    "smat_embed_grad_workspace_bytes", "smat_linear_xent", "smat_linear_xent_workspace_bytes", "smat_linear_xent_grad",
+    "smat_linear_xent_grad_workspace_bytes",
 )
 
 
@@ -106,6 +110,44 @@ class smat_linear_wgrad_args(ctypes.Structure):
                 ("x_codes", c_void_p), ("x_exps", c_void_p), ("dw", c_void_p), ("lddw", c_int64), ("db", c_void_p)]
 
 
+class smat_norm_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("wdtype", c_int32), ("kind", c_int32), ("eps", c_float), ("m", c_int64), ("n", c_int64),
+                ("x", c_void_p), ("ldx", c_int64), ("weight", c_void_p), ("bias", c_void_p), ("y", c_void_p), ("ldy", c_int64),
+                ("mean", c_void_p), ("rstd", c_void_p)]
+
+
+class smat_norm_grad_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("wdtype", c_int32), ("kind", c_int32), ("reserved", c_int32), ("m", c_int64),
+                ("n", c_int64), ("dy", c_void_p), ("lddy", c_int64), ("x", c_void_p), ("ldx", c_int64), ("weight", c_void_p),
+                ("mean", c_void_p), ("rstd", c_void_p), ("dx", c_void_p), ("lddx", c_int64), ("dweight", c_void_p),
+                ("dbias", c_void_p)]
+
+
+class smat_embed_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("table_dtype", c_int32), ("scale", c_float), ("reserved", c_int32), ("m", c_int64),
+                ("rows", c_int64), ("d", c_int64), ("table", c_void_p), ("ldtable", c_int64), ("ids", c_void_p),
+                ("out", c_void_p), ("ldout", c_int64)]
+
+
+class smat_embed_grad_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("table_dtype", c_int32), ("scale", c_float), ("accumulate", c_int32), ("m", c_int64),
+                ("rows", c_int64), ("d", c_int64), ("padding", c_int64), ("dy", c_void_p), ("lddy", c_int64),
+                ("ids", c_void_p), ("dtable", c_void_p), ("ldtable", c_int64)]
+
+
+class smat_linear_xent_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("reserved", c_int32), ("m", c_int64), ("n", c_int64), ("k", c_int64),
+                ("x", c_void_p), ("ldx", c_int64), ("w", c_void_p), ("ldw", c_int64), ("targets", c_void_p),
+                ("ignore_index", c_int64), ("loss", c_void_p), ("lse", c_void_p), ("totals", c_void_p)]
+
+
+class smat_linear_xent_grad_args(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("reserved", c_int32), ("m", c_int64), ("n", c_int64), ("k", c_int64),
+                ("x", c_void_p), ("ldx", c_int64), ("w", c_void_p), ("ldw", c_int64), ("targets", c_void_p),
+                ("ignore_index", c_int64), ("lse", c_void_p), ("row_scale", c_void_p), ("scale", c_void_p),
+                ("totals", c_void_p), ("dx", c_void_p), ("lddx", c_int64), ("dw", c_void_p), ("lddw", c_int64)]
+
+
 class SmatError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
@@ -165,6 +207,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "smat_linear_dgrad_workspace_bytes": [POINTER(smat_linear_dgrad_args), POINTER(c_size_t)],
         "smat_linear_wgrad": [POINTER(smat_linear_wgrad_args), P, c_size_t, P],
         "smat_linear_wgrad_workspace_bytes": [POINTER(smat_linear_wgrad_args), POINTER(c_size_t)],
+        "smat_norm": [POINTER(smat_norm_args), P],
+        "smat_norm_grad": [POINTER(smat_norm_grad_args), P, c_size_t, P],
+        "smat_norm_grad_workspace_bytes": [POINTER(smat_norm_grad_args), POINTER(c_size_t)],
+        "smat_embed": [POINTER(smat_embed_args), P],
+        "smat_embed_grad": [POINTER(smat_embed_grad_args), P, c_size_t, P],
+        "smat_embed_grad_workspace_bytes": [POINTER(smat_embed_grad_args), POINTER(c_size_t)],
+        "smat_linear_xent": [POINTER(smat_linear_xent_args), P, c_size_t, P],
+        "smat_linear_xent_workspace_bytes": [POINTER(smat_linear_xent_args), POINTER(c_size_t)],
+        "smat_linear_xent_grad": [POINTER(smat_linear_xent_grad_args), P, c_size_t, P],
+        "smat_linear_xent_grad_workspace_bytes": [POINTER(smat_linear_xent_grad_args), POINTER(c_size_t)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)

@@ -15,7 +15,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsmat.so")
 SOURCES = ["smat_kernels.hip", "smat_optim.hip", "smat_merge.hip", "smat_copy.hip", "smat_ckpt.hip",
-           "smat_linear.hip", "smat_api.hip", "smat_linear_api.hip"]
+           "smat_linear.hip", "smat_norm.hip", "smat_embed.hip", "smat_xent.hip", "smat_api.hip", "smat_linear_api.hip",
+           "smat_decoder_api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -7,6 +7,8 @@
 //   layer            P = x [m, k] direct        Q = W [n, k] direct        i = m, j = n, r = k
 //   data gradient    P = dy [m, k] direct       Q = W [k, n] transposed    i = m, j = n, r = k
 //   weight gradient  P = dy [m, n] transposed   Q = x [m, k] transposed    i = n, j = k, r = m
+// The output layer's loss takes the layer's form for its logits, whose rows its epilogues reduce (kEpiXent) or turn into
+// gradients (kEpiXentGrad), and the other two for dx (kEpiSum) and dW (kEpiScaled) of pieces of the vocabulary.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -26,7 +28,9 @@ inline dim3 wide_grid(int64_t blocks) {
   return blocks <= kRow ? dim3((uint32_t)blocks) : dim3((uint32_t)kRow, (uint32_t)((blocks + kRow - 1) >> kWideShift));
 }
 
-enum LinEpilogue : int { kEpiStore = 0, kEpiLayer = 1, kEpiDgrad = 2 };
+enum LinEpilogue : int { kEpiStore = 0, kEpiLayer = 1, kEpiDgrad = 2, kEpiXent = 3, kEpiXentGrad = 4, kEpiSum = 5, kEpiScaled = 6 };
+constexpr bool p_transposed(int epi) { return epi == kEpiStore || epi == kEpiScaled; }
+constexpr bool q_transposed(int epi) { return !(epi == kEpiLayer || epi == kEpiXent || epi == kEpiXentGrad); }
 
 struct LinProduct {
   const void* p;
@@ -55,6 +59,20 @@ struct LinArgs {
   void* out_up;
   int64_t ldup;
   int32_t act;
+  // cross entropy of logits v, columns col0 .. col0 + j of `classes` ones: the largest value and the sum of exponentials of
+  // each 32 columns of a row, and the target's logit; or out = (exp(v - lse) - [column is the target]) row_scale
+  const int64_t* targets;
+  int64_t ignore, classes, col0;
+  float* stats;  // [i][ceil(j / 32)][2]
+  float* target_z;
+  const float* lse;
+  const float* row_scale;  // NULL: 1
+  // out = s (v + sum_in), or sum_out = v + sum_in (NULL: 0), with s = scale[0] / totals[1] (NULL: 1)
+  const float* sum_in;
+  float* sum_out;
+  int64_t ldsum;
+  const float* scale;
+  const float* totals;
   // sums of `splits` ranges of r, joined by a second kernel: [splits][i][j rounded up to 8] fp32
   int32_t splits;
   float* partial;

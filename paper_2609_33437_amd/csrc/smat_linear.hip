@@ -844,7 +844,7 @@ __device__ __forceinline__ float dot_chunk(const u32x4& w, const u32x4& x, float
   return sum;
 }
 
-template <typename T, int M, int JB>
+template <typename T, int EPI, int M, int JB>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
   using Mem = typename El<T>::Mem;
   constexpr int kChunk = 16 / El<T>::kBytes, kGroups = kRowsWaves * kRowsEach / JB, kValues = kRowsEach * M;
@@ -856,11 +856,11 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
   // this thread's part of the epilogue, its loads under way from the start
   constexpr int kFinish = M * JB / 8;
   const int fi = (int)threadIdx.x / (JB / 8), fj = (int)threadIdx.x % (JB / 8) * 8;
-  Side<T, kEpiLayer> side;
-  ColumnSide<T, kEpiLayer> column;
+  Side<T, EPI> side;
+  ColumnSide<T, EPI> column;
   if (threadIdx.x < kFinish) {
-    column_load<T, kEpiLayer>(a, j0 + fj, column);
-    side_load<T, kEpiLayer>(a, fi, j0 + fj, side);
+    column_load<T, EPI>(a, j0 + fj, column);
+    side_load<T, EPI>(a, fi, j0 + fj, side);
   }
   // rows past the last of W and x repeat it; what they give is not kept
   const Mem *w[kRowsEach], *x[M];
@@ -937,7 +937,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
   for (int g = 0; g < kGroups; ++g)
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += sums[g][fi][fj + e];
-  epilogue8<T, kEpiLayer, 1, 2>(a, fi, j0 + fj, v, column, side);
+  epilogue8<T, EPI, 1, 2>(a, fi, j0 + fj, v, column, side);
 }
 
 // Joins the partial sums in their order and applies the epilogue: eight j a thread.  Bound by memory: two ranges of
@@ -1099,12 +1099,23 @@ bool operand_fits(const void* p, int64_t ld, int64_t r, bool trans, int bytes) {
 template <typename F>
 void with_form(int dtype, LinEpilogue epi, F&& fn) {
   with_element(dtype, [&](auto t) {
+    const auto with = [&](auto e) {
+      fn(t, std::integral_constant<bool, p_transposed(e())>(), std::integral_constant<bool, q_transposed(e())>(), e);
+    };
     if (epi == kEpiLayer)
-      fn(t, std::false_type(), std::false_type(), std::integral_constant<int, kEpiLayer>());
+      with(std::integral_constant<int, kEpiLayer>());
     else if (epi == kEpiDgrad)
-      fn(t, std::false_type(), std::true_type(), std::integral_constant<int, kEpiDgrad>());
+      with(std::integral_constant<int, kEpiDgrad>());
+    else if (epi == kEpiXent)
+      with(std::integral_constant<int, kEpiXent>());
+    else if (epi == kEpiXentGrad)
+      with(std::integral_constant<int, kEpiXentGrad>());
+    else if (epi == kEpiSum)
+      with(std::integral_constant<int, kEpiSum>());
+    else if (epi == kEpiScaled)
+      with(std::integral_constant<int, kEpiScaled>());
     else
-      fn(t, std::true_type(), std::true_type(), std::integral_constant<int, kEpiStore>());
+      with(std::integral_constant<int, kEpiStore>());
   });
 }
 }  // namespace
@@ -1250,7 +1261,7 @@ struct Operand {
 };
 // Operands 2 s and 2 s + 1 are P and Q of product s.
 void operands(const LinArgs& a, LinEpilogue epi, int bytes, Operand (&o)[4]) {
-  const bool pt = epi == kEpiStore, qt = epi != kEpiLayer;
+  const bool pt = p_transposed(epi), qt = q_transposed(epi);
   for (int s = 0; s < 2; ++s) {
     const LinProduct& pr = a.prod[s];
     o[2 * s] = {pr.p, pr.ldp, pt ? pr.r : a.i, pt ? a.i : pr.r, pr.r == 0 || operand_fits(pr.p, pr.ldp, pr.r, pt, bytes), pt};
@@ -1264,9 +1275,11 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int bytes = dtype == 1 ? 2 : 4;
   const int64_t deep = 128 / bytes;
   LinPlan best{};
-  Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0, 0.0, epi == kEpiLayer ? 0 : 128 / bytes};
+  Sizes z{a.i, a.j, div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep), 0.0, 0.0, q_transposed(epi) ? 128 / bytes : 0};
   if (epi == kEpiLayer) z.epilogue = (a.act ? 8.0 : 0.0) + (a.codes ? 6.0 : 0.0) + (a.mul ? 2.0 : 0.0) + (a.residual ? 2.0 : 0.0);
   if (epi == kEpiDgrad) z.epilogue = a.up_codes ? 22.0 : a.z_codes ? 13.0 : 0.0;
+  if (epi == kEpiXent || epi == kEpiXentGrad) z.epilogue = 8.0;
+  if (epi == kEpiSum) z.epilogue = 4.0;
   Operand o[4];
   operands(a, epi, bytes, o);
   int32_t off = 0;  // operands that cannot be copied to LDS directly as they lie
@@ -1279,7 +1292,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       wide |= packed_ld(o[k].run, bytes) >= wide_ld(o[k].trans);
       moved += 2.0 * (double)o[k].rows * (double)o[k].run * bytes;
     }
-  const int transposed = epi == kEpiStore ? 2 : epi == kEpiDgrad ? 1 : 0;  // operands
+  const int transposed = (p_transposed(epi) ? 1 : 0) + (q_transposed(epi) ? 1 : 0);  // operands
   const double direct = dtype == 1 ? choose_parts(kDirectCosts[transposed], 6, z, best) : choose_parts(kFp32Costs, 3, z, best);
   double least = direct;
   best.direct = 1;
@@ -1296,7 +1309,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
     }
   }
   // few rows: the kernel that takes operands of any alignment without a copy (16 threads a column where there are many)
-  if (epi == kEpiLayer && a.i <= kMaxRows && a.j <= kMaxThreads / 16 - 32) {
+  if ((epi == kEpiLayer || epi == kEpiXent) && a.i <= kMaxRows && a.j <= kMaxThreads / 16 - 32) {
     const double rate = kRowsRate[a.i > 4 ? 3 : a.i > 2 ? 2 : a.i - 1];
     if (kRowsStart + z.bytes / rate <= least) {
       best = LinPlan{};
@@ -1354,29 +1367,40 @@ LinArgs rows_of(LinArgs a, int64_t from, int64_t rows, int bytes, bool pt) {
   a.z_exps = static_cast<const uint8_t*>(skip_bytes(a.z_exps, from * nb));
   a.up_codes = static_cast<const int8_t*>(skip_bytes(a.up_codes, from * nb * kCkptBlock));
   a.up_exps = static_cast<const uint8_t*>(skip_bytes(a.up_exps, from * nb));
+  a.targets = static_cast<const int64_t*>(skip_bytes(a.targets, from * 8));
+  a.stats = static_cast<float*>(skip_bytes(a.stats, from * nb * 8));
+  a.target_z = static_cast<float*>(skip_bytes(a.target_z, from * 4));
+  a.lse = static_cast<const float*>(skip_bytes(a.lse, from * 4));
+  a.row_scale = static_cast<const float*>(skip_bytes(a.row_scale, from * 4));
+  a.sum_in = static_cast<const float*>(skip_bytes(a.sum_in, from * a.ldsum * 4));
+  a.sum_out = static_cast<float*>(skip_bytes(a.sum_out, from * a.ldsum * 4));
   return a;
 }
 
-template <typename T>
+template <typename T, int EPI>
 hipError_t launch_rows(const LinArgs& a, hipStream_t stream) {
-  // a checkpoint's blocks need 32 columns; without one narrower blocks until there are enough of them
+  // a checkpoint's blocks and a loss's sums need 32 columns; without them narrower blocks until there are enough of them
   const auto launch = [&](auto jb) {
     const dim3 grid((uint32_t)div_up(a.j, jb())), block(64 * kRowsWaves);
     if (a.i == 1)
-      k_linear_rows<T, 1, jb()><<<grid, block, 0, stream>>>(a);
+      k_linear_rows<T, EPI, 1, jb()><<<grid, block, 0, stream>>>(a);
     else if (a.i == 2)
-      k_linear_rows<T, 2, jb()><<<grid, block, 0, stream>>>(a);
+      k_linear_rows<T, EPI, 2, jb()><<<grid, block, 0, stream>>>(a);
     else if (a.i <= 4)
-      k_linear_rows<T, 4, jb()><<<grid, block, 0, stream>>>(a);
+      k_linear_rows<T, EPI, 4, jb()><<<grid, block, 0, stream>>>(a);
     else
-      k_linear_rows<T, 8, jb()><<<grid, block, 0, stream>>>(a);
+      k_linear_rows<T, EPI, 8, jb()><<<grid, block, 0, stream>>>(a);
   };
-  if (a.codes || a.j >= 32 * kComputeUnits)
+  if constexpr (EPI == kEpiXent) {
     launch(std::integral_constant<int, 32>());
-  else if (a.j >= 16 * kComputeUnits)
-    launch(std::integral_constant<int, 16>());
-  else
-    launch(std::integral_constant<int, 8>());
+  } else {
+    if (a.codes || a.j >= 32 * kComputeUnits)
+      launch(std::integral_constant<int, 32>());
+    else if (a.j >= 16 * kComputeUnits)
+      launch(std::integral_constant<int, 16>());
+    else
+      launch(std::integral_constant<int, 8>());
+  }
   return hipGetLastError();
 }
 }  // namespace
@@ -1410,7 +1434,7 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
   int64_t from = 0;
   for (int p = 0; p < plan.parts && e == hipSuccess; ++p) {
     const LinPart& part = plan.part[p];
-    LinArgs a = rows_of(whole, from, part.rows, bytes, epi == kEpiStore);
+    LinArgs a = rows_of(whole, from, part.rows, bytes, p_transposed(epi));
     a.splits = part.splits;
     from += part.rows;
     const int64_t eights = a.i * ckpt_blocks(a.j) * 4;  // of the join
@@ -1424,8 +1448,8 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
           e = hipGetLastError();
         }
       }
-      if constexpr (ep() == kEpiLayer) {
-        if (part.form == kRows) e = launch_rows<T>(a, stream);
+      if constexpr (ep() == kEpiLayer || ep() == kEpiXent) {
+        if (part.form == kRows) e = launch_rows<T, ep()>(a, stream);
       }
       if (part.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
       if (part.form == kSmall) e = launch_group<SmallShape, T, pt(), qt(), ep()>(a, plan.direct, stream);

@@ -12,6 +12,7 @@
 namespace smat {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ int64_t wide_block() { return ((int64_t)blockIdx.y << kWideShift) + blockIdx.x; }
 
@@ -265,6 +266,40 @@ struct Side<T, kEpiDgrad> {
   u32x2 z, up;
   uint32_t z_byte, up_byte;
 };
+template <typename T>
+struct Side<T, kEpiXent> {
+  int64_t target;
+};
+template <typename T>
+struct Side<T, kEpiXentGrad> {
+  int64_t target;
+  float lse, scale;
+};
+template <typename T>
+struct Side<T, kEpiSum> {
+  Raw8<float> sum;
+};
+template <typename T>
+struct ColumnSide<T, kEpiSum> {
+  float scale;
+};
+template <typename T>
+struct ColumnSide<T, kEpiScaled> {
+  float scale;
+};
+
+// scale[0] / totals[1]; 0 where no row counts.
+__device__ __forceinline__ float total_scale(const LinArgs& a) {
+  const float s = a.scale ? *a.scale : 1.f;
+  if (!a.totals) return s;
+  const float count = a.totals[1];
+  return count > 0.f ? s / count : 0.f;
+}
+// Where eight consecutive columns from j0 on hold the target, or a number outside [0, 8).
+__device__ __forceinline__ int target_place(const LinArgs& a, int64_t target, int64_t j0) {
+  const int64_t at = target - a.col0 - j0;
+  return at >= 0 && at < 8 ? (int)at : -1;
+}
 
 __device__ __forceinline__ int64_t row_blocks(const LinArgs& a) { return (a.j + kCkptBlock - 1) / kCkptBlock; }
 
@@ -290,6 +325,19 @@ __device__ __forceinline__ void side_load(const LinArgs& a, int64_t i, int64_t j
       }
     }
   }
+  if constexpr (EPI == kEpiXent) {
+    if (WHOLE || i < a.i) s.target = a.targets[i];
+  }
+  if constexpr (EPI == kEpiXentGrad) {
+    if (WHOLE || i < a.i) {
+      s.target = a.targets[i];
+      s.lse = a.lse[i];
+      s.scale = a.row_scale ? a.row_scale[i] : 1.f;
+    }
+  }
+  if constexpr (EPI == kEpiSum) {
+    if (a.sum_in && (WHOLE || (i < a.i && j0 < a.j))) s.sum.load(a.sum_in + i * a.ldsum + j0);  // rows of whole eights
+  }
 }
 
 template <typename T, int EPI>
@@ -297,6 +345,7 @@ __device__ __forceinline__ void column_load(const LinArgs& a, int64_t j0, Column
   if constexpr (EPI == kEpiLayer) {
     if (a.bias && j0 + 8 <= a.j) s.bias.load(static_cast<const typename El<T>::Mem*>(a.bias) + j0);
   }
+  if constexpr (EPI == kEpiSum || EPI == kEpiScaled) s.scale = total_scale(a);
 }
 
 // One side matrix's values: loaded ahead, or at a row's end element by element.
@@ -352,7 +401,50 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
       for (int e = 0; e < 8; ++e) v[e] += u[e];
     }
   }
+  if constexpr (EPI == kEpiXent) {
+    // the four lanes' 32 columns
+    float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = e < valid ? fmaxf(top, v[e]) : top;
+    top = fmaxf(top, __shfl_xor(top, A));
+    top = fmaxf(top, __shfl_xor(top, B));
+    const float from = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += e < valid ? act_exp<T>(v[e] - from) : 0.f;
+    sum += __shfl_xor(sum, A);
+    sum += __shfl_xor(sum, B);
+    if (valid <= 0) return;
+    const int at = target_place(a, s.target, j0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e == at && e < valid) a.target_z[i] = v[e];
+    if (j0 % kCkptBlock == 0) *reinterpret_cast<f32x2*>(a.stats + (i * row_blocks(a) + j0 / kCkptBlock) * 2) = f32x2{top, sum};
+    return;
+  }
   if (valid <= 0) return;
+  if constexpr (EPI == kEpiXentGrad) {
+    const int at = target_place(a, s.target, j0);
+    const bool none = s.target == a.ignore, outside = s.target < 0 || s.target >= a.classes;
+    const float scale = outside ? __builtin_nanf("") : s.scale;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = none ? 0.f : (act_exp<T>(v[e] - s.lse) - (e == at ? 1.f : 0.f)) * scale;
+  }
+  if constexpr (EPI == kEpiSum) {
+    if (a.sum_in) {
+      float u[8];
+      s.sum.get(u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += u[e];
+    }
+    if (a.sum_out) {
+      El<float>::store8(a.sum_out + i * a.ldsum + j0, v);
+      return;
+    }
+  }
+  if constexpr (EPI == kEpiSum || EPI == kEpiScaled) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= c.scale;
+  }
   if constexpr (EPI == kEpiDgrad) {
     if (a.z_codes) {
       float z[8];
