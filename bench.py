@@ -95,6 +95,9 @@ def parse_args():
     ap.add_argument("--train-mlp", choices=("torch", "checkpointed"), default="torch",
                     help="--train: the decoder's MLPs as torch modules, or through the fused products with activations "
                          "saved in 8 bits")
+    ap.add_argument("--train-ends", choices=("torch", "fused"), default="torch",
+                    help="--train: the decoder's embedding, norms and output layer with its loss as torch modules, or through "
+                         "the library's operators, which never store the logits")
     ap.add_argument("--train-batch", type=int, default=8)
     ap.add_argument("--train-seq", type=int, default=512)
     ap.add_argument("--train-reps", type=int, default=3)
@@ -947,7 +950,8 @@ def bench_train(args, torch, smat) -> int:
     W = max(t, -(-args.warmup // t) * t)
     clip = 1.0
     log(f"building the decoder ({parameter_count(shape) / 1e9:.2f}B params), batch {B} x {S} tokens")
-    model = make_decoder(shape, 0, "cuda", checkpointed=args.train_mlp == "checkpointed")
+    model = make_decoder(shape, 0, "cuda", checkpointed=args.train_mlp == "checkpointed",
+                         fused=args.train_ends == "fused")
     batches = token_batches(shape, B, S, 8, 1, "cuda")
     params = list(model.parameters())
     opt = torch.optim.AdamW(params, lr=2e-5, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-3, fused=True)
@@ -1031,6 +1035,7 @@ def bench_train(args, torch, smat) -> int:
         "tokens_per_s": {m: round(tokens / (med[m] * 1e-3), 1) for m in modes},
         "begin_ms_per_simulated_step": round(begin_ms, 3),
         "mlp": args.train_mlp,
+        "ends": args.train_ends,
         "peak_allocated_gib": round(torch.cuda.max_memory_allocated() / 2 ** 30, 3),
         "config": {"workload": f"decoder d={shape.d} L={shape.layers} heads={shape.heads} ffn={shape.ffn} "
                                f"vocab={shape.vocab} tied, {parameter_count(shape)} params",

@@ -14,6 +14,11 @@ saved activations (about one per cent of a weight gradient's norm), never in the
 derivatives of their own, and there are none in forward mode: asking for either raises.  Without gradients (a merged
 model answering) nothing is saved, and a few tokens take the product's form for few rows.
 
+What stands between a decoder's linear layers is here too: the token embedding, layer and RMS norms, and the output layer
+with its cross entropy, whose logits are never stored (smat_embed, smat_norm, smat_linear_xent).  Norms compute in fp32
+and return their input's dtype, whatever autocast says, and their weights may be fp32 beside bf16 activations; an
+embedding under autocast returns its dtype.  The loss is fp32.
+
 Tensors are fp32 or bf16 on the GPU; under torch.autocast floating inputs are cast to its dtype first, as
 torch's own linear layers do, except a residual: one of another dtype is added to the result in torch's
 promoted dtype.  Otherwise a call's tensors share one dtype.  A residual has the output's
@@ -28,7 +33,8 @@ import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
-from ._lib import SMAT_ERR_INVALID, SmatError
+from ._decoder import smat_embed, smat_embed_grad, smat_linear_xent, smat_linear_xent_grad, smat_norm, smat_norm_grad
+from ._lib import SMAT_ERR_INVALID, SMAT_NORM_LAYER, SMAT_NORM_RMS, SmatError
 from ._linear import (SMAT_ACT_NONE, SMAT_ACT_SILU, ActCheckpoint, smat_ckpt_read, smat_ckpt_write, smat_linear,
                       smat_linear_dgrad, smat_linear_wgrad)
 
@@ -254,6 +260,96 @@ class _GatedMlp(torch.autograd.Function):
         return dx, dwg, dwu, dwd, dy if need_r else None, None
 
 
+class _Norm(torch.autograd.Function):
+    """Rows of a matrix normalised."""
+
+    @staticmethod
+    def forward(ctx, x, w, b, kind, eps):
+        m = x.shape[0]
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        rstd = torch.empty(m, dtype=torch.float32, device=x.device)
+        mean = torch.empty_like(rstd) if kind == SMAT_NORM_LAYER else None
+        smat_norm(x, y, weight=w, bias=b, kind=kind, eps=eps, mean=mean, rstd=rstd)
+        ctx.kind = kind
+        ctx.bias = None if b is None else b.dtype
+        ctx.save_for_backward(x, w, mean, rstd)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, w, mean, rstd = ctx.saved_tensors
+        need_x, need_w, need_b, _, _ = ctx.needs_input_grad
+        dy = _rows(dy)
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
+        dw = torch.empty(x.shape[1], dtype=w.dtype, device=x.device) if need_w else None
+        db = torch.empty(x.shape[1], dtype=ctx.bias, device=x.device) if need_b else None
+        if need_x or need_w or need_b:
+            smat_norm_grad(dy, x, rstd, weight=w, mean=mean, kind=ctx.kind, dx=dx, dw=dw, db=db)
+        return dx, dw, db, None, None
+
+
+class _Embedding(torch.autograd.Function):
+    """Rows of a table by a vector of ids."""
+
+    @staticmethod
+    def forward(ctx, table, ids, scale, padding_idx, dtype):
+        out = torch.empty(ids.shape[0], table.shape[1], dtype=dtype, device=table.device)
+        smat_embed(table, ids, out, scale=scale)
+        ctx.scale, ctx.padding_idx, ctx.shape, ctx.dtype = scale, padding_idx, table.shape, table.dtype
+        ctx.save_for_backward(ids)
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        ids, = ctx.saved_tensors
+        dtable = torch.empty(ctx.shape, dtype=ctx.dtype, device=dy.device)
+        smat_embed_grad(_rows(dy), ids, dtable, scale=ctx.scale, padding_idx=ctx.padding_idx)
+        return dtable, None, None, None, None
+
+
+class _LinearXent(torch.autograd.Function):
+    """Per-row losses, or their sum (1) or mean (2), of x w^T against targets."""
+
+    @staticmethod
+    def forward(ctx, x, w, targets, ignore_index, reduction):
+        loss, lse, totals = _losses(x, w, targets, ignore_index, reduction)
+        ctx.ignore_index, ctx.reduction = ignore_index, reduction
+        ctx.save_for_backward(x, w, targets, lse, totals)
+        return loss if reduction == 0 else totals[2 * reduction - 2].clone()
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad):
+        x, w, targets, lse, totals = ctx.saved_tensors
+        need_x, need_w = ctx.needs_input_grad[:2]
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
+        dw = torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None
+        grad = grad.contiguous()
+        rows = ctx.reduction == 0
+        smat_linear_xent_grad(x, w, targets, lse, dx=dx, dw=dw, row_scale=grad if rows else None, scale=None if rows else grad,
+                              totals=totals if ctx.reduction == 2 else None, ignore_index=ctx.ignore_index)
+        return dx, dw, None, None, None
+
+
+def _losses(x, w, targets, ignore_index: int, reduction: int):
+    """(loss of each row, lse, totals or None)."""
+    empty = dict(dtype=torch.float32, device=x.device)
+    loss, lse = torch.empty(x.shape[0], **empty), torch.empty(x.shape[0], **empty)
+    totals = torch.empty(3, **empty) if reduction else None
+    smat_linear_xent(x, w, targets, loss, lse, totals=totals, ignore_index=ignore_index)
+    return loss, lse, totals
+
+
+def _ids(ids: torch.Tensor, like: torch.Tensor, what: str) -> torch.Tensor:
+    if ids.dtype != torch.int64:
+        raise SmatError(SMAT_ERR_INVALID, f"{what} must be int64, got {ids.dtype}")
+    if ids.device != like.device:
+        raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the GPU of the other tensors")
+    return ids.reshape(-1)
+
+
 # ------------------------------------------------------------------ public functions
 def linear(x, weight, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x weight^T + bias + residual for x [.., k]; the weight gradient reads x from an 8-bit checkpoint."""
@@ -309,3 +405,75 @@ def gated_mlp(x, w_gate, w_up, w_down, act: int = SMAT_ACT_SILU,
     out = torch.empty(x.shape[0], w_down.shape[0], dtype=x.dtype, device=x.device)
     smat_linear(h, w_down, out, residual=r)
     return _sum(out.view(shape), after)
+
+
+def _norm(x, weight, bias, kind: int, eps: float) -> torch.Tensor:
+    if not x.is_cuda:
+        raise SmatError(SMAT_ERR_INVALID, "the layers run on GPU tensors")
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return _norm(x, weight, bias, kind, eps)
+    for t, what in ((weight, "weight"), (bias, "bias")):
+        if t is not None and (t.dim() != 1 or t.shape[0] != x.shape[-1:].numel()):
+            raise SmatError(SMAT_ERR_INVALID, f"{what} has shape {tuple(t.shape)}, the rows of x {tuple(x.shape[-1:])}")
+    shape, x = x.shape, _rows(x)
+    weight, bias = _bias(weight), _bias(bias)
+    if _saves(x, weight, bias):
+        return _Norm.apply(x, weight, bias, kind, float(eps)).view(shape)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    smat_norm(x, y, weight=weight, bias=bias, kind=kind, eps=eps)
+    return y.view(shape)
+
+
+def layer_norm(x, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               eps: float = 1e-5) -> torch.Tensor:
+    """(x - mean) / sqrt(var + eps) weight + bias over the last dimension of x."""
+    return _norm(x, weight, bias, SMAT_NORM_LAYER, eps)
+
+
+def rms_norm(x, weight: Optional[torch.Tensor] = None, eps: float = 1e-6) -> torch.Tensor:
+    """x / sqrt(mean x^2 + eps) weight over the last dimension of x."""
+    return _norm(x, weight, None, SMAT_NORM_RMS, eps)
+
+
+def embedding(ids, weight, scale: float = 1.0, padding_idx: Optional[int] = None) -> torch.Tensor:
+    """scale * weight[ids] for int64 ids of any shape; the row of padding_idx has no gradient.  An id outside the table gives a
+    row of NaN.  Under autocast the result has its dtype."""
+    if not weight.is_cuda:
+        raise SmatError(SMAT_ERR_INVALID, "the layers run on GPU tensors")
+    if _elsewhere(weight):
+        with torch.cuda.device(weight.get_device()):
+            return embedding(ids, weight, scale, padding_idx)
+    if padding_idx is not None and not 0 <= padding_idx < weight.shape[0]:
+        raise SmatError(SMAT_ERR_INVALID, f"padding_idx {padding_idx} is outside the table")
+    dtype = torch.get_autocast_dtype("cuda") if torch.is_autocast_enabled("cuda") else weight.dtype
+    weight, shape, flat = _weight(weight), ids.shape, _ids(ids, weight, "ids")
+    if _saves(weight):
+        out = _Embedding.apply(weight, flat, float(scale), padding_idx, dtype)
+    else:
+        out = torch.empty(flat.shape[0], weight.shape[1], dtype=dtype, device=weight.device)
+        smat_embed(weight, flat, out, scale=scale)
+    return out.view(shape + weight.shape[1:])
+
+
+def linear_cross_entropy(x, weight, targets, ignore_index: int = -100, reduction: str = "mean") -> torch.Tensor:
+    """The cross entropy of the logits x weight^T for x [.., k] against int64 targets [..], in fp32, without storing the logits.
+    Rows whose target is ignore_index have no loss and no gradient; another target outside the vocabulary gives NaN.
+    reduction: "mean" over the rows with a target (NaN where there is none, with gradients of 0), "sum", or "none" for each
+    row's loss in targets' shape."""
+    if reduction not in ("none", "sum", "mean"):
+        raise SmatError(SMAT_ERR_INVALID, f"unknown reduction {reduction!r}")
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return linear_cross_entropy(x, weight, targets, ignore_index, reduction)
+    x, weight = _cast(x, weight)
+    if x.shape[:-1] != targets.shape:
+        raise SmatError(SMAT_ERR_INVALID, f"targets have shape {tuple(targets.shape)}, the rows of x {tuple(x.shape[:-1])}")
+    x, weight, flat, how = _rows(x), _weight(weight), _ids(targets, x, "targets"), ("none", "sum", "mean").index(reduction)
+    if _saves(x, weight):
+        loss = _LinearXent.apply(x, weight, flat, int(ignore_index), how)
+    else:
+        loss, _, totals = _losses(x, weight, flat, int(ignore_index), how)
+        if how:
+            loss = totals[2 * how - 2]
+    return loss.view(targets.shape) if how == 0 else loss

@@ -1,0 +1,314 @@
+"""The embedding, the norms and the output layer with its loss as torch functions: values and gradients against torch's own
+operators in float64, alone and as they follow each other in a decoder, and what they refuse.
+
+A chain's result in fp32 is compared in the 2-norm.  Its longest sum has N terms, each operator is off by at most
+(N + 64) 2^-23 of the magnitudes that it sums, and magnitudes exceed the result by a factor of at most sqrt(N) where signs
+are mixed; five operators one after the other: 5 (N + 64)^1.5 2^-23, below `FP32` for the N up to 200 here.  In bf16 each
+operator rounds its output (and its gradient) by 2^-8 or less: 2^-4 holds ten such roundings with a factor of 1.6."""
+import pytest
+import torch
+import torch.nn.functional as F
+
+import paper_2609_33437_amd as smat
+from paper_2609_33437_amd import layers
+from workloads.model import TINY, make_decoder, token_batches
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+FP32 = 5 * 264 ** 1.5 * 2.0 ** -23
+BF16 = 2.0 ** -4
+
+
+def off(got, want):
+    got, want = got.detach().double().cpu(), want.detach().double().cpu()
+    assert torch.isfinite(got).all()
+    return float((got - want).norm() / want.norm())
+
+
+def leaf(t, dtype=torch.float32):
+    return t.to(DEV, dtype).detach().requires_grad_()
+
+
+def double(*shape, seed):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+@pytest.mark.parametrize("dtype,tol", [(torch.float32, FP32), (torch.bfloat16, BF16)])
+@pytest.mark.parametrize("shape", [(12,), (1, 12), (5, 96), (2, 3, 130), (0, 8)])
+@pytest.mark.parametrize("which", ["layer", "layer_plain", "rms", "rms_plain"])
+def test_norms(dtype, tol, shape, which):
+    n = shape[-1]
+    x, w, b, dy = double(*shape, seed=1) + 0.3, double(n, seed=2), double(n, seed=3), double(*shape, seed=4)
+    x, w, b, dy = (t.to(dtype).double() for t in (x, w, b, dy))
+    ref = [t.clone().requires_grad_() for t in (x, w, b)]
+    own = [leaf(t, dtype) for t in (x, w, b)]
+    if which.startswith("layer"):
+        plain = which == "layer_plain"
+        want = F.layer_norm(ref[0], (n,), None if plain else ref[1], None if plain else ref[2], 1e-5)
+        got = layers.layer_norm(own[0], None if plain else own[1], None if plain else own[2])
+    else:
+        want = ref[0] * torch.rsqrt(ref[0].pow(2).mean(-1, keepdim=True) + 1e-6) * (1.0 if which == "rms_plain" else ref[1])
+        got = layers.rms_norm(own[0], None if which == "rms_plain" else own[1])
+    assert got.shape == shape and got.dtype == dtype
+    want.backward(dy)
+    got.backward(dy.to(DEV, dtype))
+    if 0 in shape:
+        assert own[0].grad.shape == shape
+        return
+    assert off(got, want) <= tol
+    for o, r in zip(own, ref):
+        if r.grad is not None:
+            assert o.grad.dtype == dtype and off(o.grad, r.grad) <= tol
+
+
+def test_norm_with_fp32_weights_beside_bf16_rows():
+    x, w = leaf(double(40, 64, seed=1), torch.bfloat16), leaf(double(64, seed=2))
+    y = layers.rms_norm(x, w)
+    y.backward(torch.ones_like(y))
+    assert y.dtype == torch.bfloat16 and w.grad.dtype == torch.float32 and x.grad.dtype == torch.bfloat16
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        assert layers.layer_norm(w.view(1, 64)).dtype == torch.float32
+        assert torch.equal(layers.rms_norm(x, w), y)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(), (7,), (2, 9), (0,)])
+def test_embedding(dtype, shape):
+    table = double(20, 24, seed=1).to(dtype)
+    ids = torch.randint(0, 20, shape, generator=torch.Generator().manual_seed(2))
+    ref, own = table.double().requires_grad_(), leaf(table, dtype)
+    want = F.embedding(ids, ref, padding_idx=3) * 2.0
+    got = layers.embedding(ids.to(DEV), own, scale=2.0, padding_idx=3)
+    assert got.shape == shape + (24,) and got.dtype == dtype
+    dy = torch.randint(-4, 5, got.shape, generator=torch.Generator().manual_seed(3)).double()
+    want.backward(dy)
+    got.backward(dy.to(DEV, dtype))
+    assert torch.equal(got.cpu(), want.to(dtype)) and torch.equal(own.grad.cpu(), ref.grad.to(dtype))
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        assert layers.embedding(ids.to(DEV), own).dtype == torch.bfloat16
+    with torch.no_grad():
+        assert torch.equal(layers.embedding(ids.to(DEV), own, scale=2.0), got)
+
+
+@pytest.mark.parametrize("dtype,tol", [(torch.float32, FP32), (torch.bfloat16, BF16)])
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+@pytest.mark.parametrize("shape", [(1,), (6,), (3, 11)])
+def test_cross_entropy(dtype, tol, reduction, shape):
+    x, w = (t.to(dtype).double() for t in (double(*shape, 48, seed=1), double(70, 48, seed=2) * 0.3))
+    t = torch.randint(0, 70, shape, generator=torch.Generator().manual_seed(3))
+    t.view(-1)[1::4] = -100
+    rx, rw, ox, ow = x.clone().requires_grad_(), w.clone().requires_grad_(), leaf(x, dtype), leaf(w, dtype)
+    want = F.cross_entropy((rx @ rw.t()).view(-1, 70), t.view(-1), reduction=reduction)
+    got = layers.linear_cross_entropy(ox, ow, t.to(DEV), reduction=reduction)
+    assert got.dtype == torch.float32 and got.shape == (shape if reduction == "none" else ())
+    assert off(got.view(-1), want.view(-1)) <= FP32
+    g = double(*got.shape, seed=4)
+    want.backward(g.view(want.shape))
+    got.backward(g.to(DEV, torch.float32))
+    assert ox.grad.dtype == dtype and off(ox.grad, rx.grad) <= tol and off(ow.grad, rw.grad) <= tol
+    with torch.no_grad():
+        assert torch.equal(layers.linear_cross_entropy(ox, ow, t.to(DEV), reduction=reduction), got)
+
+
+def test_gradients_against_differences():
+    """Directional differences of each function in fp32: (f(a + h v) - f(a - h v)) / 2h = <grad, v> within h^2 f''' / 6 and the
+    values' rounding over h: with h = 2^-6, |f| below 8 and third derivatives along v (of norm 1) below 32 that is
+    32 h^2 / 6 + 8 (64 2^-24) / h < 4e-3."""
+    h = 2.0 ** -6
+
+    def check(fn, *tensors):
+        own = [leaf(t) for t in tensors]
+        fn(*own).backward()
+        for i, t in enumerate(tensors):
+            v = double(*t.shape, seed=50 + i)
+            v = v / v.norm()
+            up, down = ([leaf(o + (s * h * v if j == i else 0)) for j, o in enumerate(tensors)] for s in (1, -1))
+            with torch.no_grad():
+                slope = float(fn(*up) - fn(*down)) / (2 * h)
+            assert abs(slope - float((own[i].grad.double().cpu() * v).sum())) < 4e-3
+
+    c = (double(6, 40, seed=9) / 16).to(DEV, torch.float32)
+    x, w, b = double(6, 40, seed=1), double(40, seed=2), double(40, seed=3)
+    check(lambda x, w, b: (layers.layer_norm(x, w, b) * c).sum(), x, w, b)
+    check(lambda x, w: (layers.rms_norm(x, w) * c).sum(), x, w)
+    ids = torch.tensor([1, 1, 4, 0, 1, 4], device=DEV)
+    check(lambda t: (layers.embedding(ids, t, scale=1.5) * c).sum(), double(6, 40, seed=4))
+    t = torch.tensor([3, 8, -100, 0, 8, 1], device=DEV)
+    check(lambda x, w: layers.linear_cross_entropy(x, w, t), x, double(9, 40, seed=5) * 0.3)
+
+
+def test_mean_of_no_rows():
+    """As torch's: the loss is NaN and the gradients are zeros."""
+    x, w = leaf(double(3, 8, seed=1)), leaf(double(5, 8, seed=2))
+    loss = layers.linear_cross_entropy(x, w, torch.full((3,), -100, device=DEV))
+    loss.backward()
+    assert loss.isnan() and not x.grad.any() and not w.grad.any()
+
+
+def chain(tokens, table, w1, b1, head, own):
+    """Embedding, layer norm, a linear layer, RMS norm, and the loss under the tied table plus one of another head."""
+    if own:
+        x = layers.embedding(tokens[:, :-1], table, scale=3.0, padding_idx=0)
+        h = layers.rms_norm(x + F.linear(layers.layer_norm(x, w1, b1), head[:x.shape[-1]]), w1)
+        return layers.linear_cross_entropy(h, table, tokens[:, 1:], ignore_index=0) + \
+            0.5 * layers.linear_cross_entropy(h, head, tokens[:, 1:], reduction="sum")
+    x = F.embedding(tokens[:, :-1], table, padding_idx=0) * 3.0
+    h = x + F.linear(F.layer_norm(x, (x.shape[-1],), w1, b1), head[:x.shape[-1]])
+    h = h * torch.rsqrt(h.pow(2).mean(-1, keepdim=True) + 1e-6) * w1
+    t = tokens[:, 1:].reshape(-1)
+    return F.cross_entropy((h @ table.t()).view(t.numel(), -1), t, ignore_index=0) + \
+        0.5 * F.cross_entropy((h @ head.t()).view(t.numel(), -1), t, reduction="sum")
+
+
+@pytest.mark.parametrize("dtype,tol", [(torch.float32, FP32), (torch.bfloat16, BF16)])
+def test_a_run_of_them_together(dtype, tol):
+    """Tied weights, whose gradients add up, shared norms, gradients that flow on, twice over (accumulated)."""
+    d, v = 40, 61
+    tensors = [t.to(dtype).double() for t in (double(v, d, seed=1) * 0.2, 1 + 0.1 * double(d, seed=2), 0.1 * double(d, seed=3),
+                                              double(v, d, seed=4) * 0.2)]
+    tokens = torch.randint(0, v, (3, 20), generator=torch.Generator().manual_seed(5))
+    ref, own = [t.clone().requires_grad_() for t in tensors], [leaf(t, dtype) for t in tensors]
+    want, got = chain(tokens, *ref, own=False), chain(tokens.to(DEV), *own, own=True)
+    assert off(got, want) <= tol
+    want.backward()
+    got.backward()
+    for o, r in zip(own, ref):
+        assert off(o.grad, r.grad) <= tol
+    first = [o.grad.clone() for o in own]
+    chain(tokens.to(DEV), *own, own=True).backward()
+    for o, f in zip(own, first):
+        assert off(o.grad, 2 * f) <= (2.0 ** -23 if dtype == torch.float32 else 2.0 ** -8)
+
+
+def test_decoder_runs_through_them():
+    """The workload's decoder: the same loss and gradients as with torch's modules in fp32, and under autocast it trains."""
+    tokens = token_batches(TINY, 3, 17, 1, 4, DEV)[0]
+    plain, fused = make_decoder(TINY, 3, DEV), make_decoder(TINY, 3, DEV, fused=True)
+    exact = make_decoder(TINY, 3).double()
+    losses = [m.loss(tokens.to(next(m.parameters()).device)) for m in (exact, plain, fused)]
+    for loss in losses:
+        loss.backward()
+    assert off(losses[2], losses[0]) <= FP32
+    for (name, a), b in zip(exact.named_parameters(), fused.parameters()):
+        assert off(b.grad, a.grad) <= FP32, name
+    assert torch.equal(plain(tokens).argmax(-1), fused(tokens).argmax(-1))
+    both = make_decoder(TINY, 3, DEV, checkpointed=True, fused=True)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        loss = both.loss(tokens)
+    loss.backward()
+    assert loss.dtype == torch.float32 and all(p.grad is not None and torch.isfinite(p.grad).all() for p in both.parameters())
+
+
+def test_the_loss_stores_no_logits():
+    """Memory that the forward and backward of the loss take beside inputs and gradients stays below the logits' size."""
+    m, n, k = 2048, 65536, 64
+    x, w = leaf(double(m, k, seed=1), torch.bfloat16), leaf(torch.randn(n, k), torch.bfloat16)
+    t = torch.randint(0, n, (m,), device=DEV)
+    layers.linear_cross_entropy(x, w, t).backward()
+    x.grad = w.grad = None
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    layers.linear_cross_entropy(x, w, t).backward()
+    assert torch.cuda.max_memory_allocated() - before < m * n * 2 * 0.75
+
+
+def test_layouts_and_views():
+    """Rows with a stride, transposed weights and expanded gradients give what contiguous tensors give."""
+    x, w = double(6, 10, seed=1).float().to(DEV), double(12, 10, seed=2).float().to(DEV)
+    wide = torch.zeros(6, 30, device=DEV)
+    wide[:, 5:15] = x
+    t = torch.arange(6, device=DEV)
+    a = layers.linear_cross_entropy(wide[:, 5:15], w.t().contiguous().t(), t)
+    assert torch.equal(a, layers.linear_cross_entropy(x, w, t))
+    assert torch.equal(layers.rms_norm(wide[:, 5:15], w[:1].expand(2, 10)[1]), layers.rms_norm(x, w[0]))
+    assert torch.equal(layers.layer_norm(x.t().contiguous().t()), layers.layer_norm(x))
+    own = leaf(x)
+    layers.layer_norm(own).sum().backward()                       # an expanded gradient
+    assert float(own.grad.abs().max()) < 1e-4                     # the sum of a row does not depend on it
+    table = leaf(w)
+    layers.embedding(torch.arange(12, device=DEV).view(3, 4).t(), table).sum().backward()
+    assert torch.equal(table.grad, torch.ones_like(table))
+    none = leaf(x)
+    layers.linear_cross_entropy(none, w, t, reduction="none").sum().backward()
+    assert torch.isfinite(none.grad).all()
+
+
+def test_frozen_and_partial_gradients():
+    x, w = double(6, 10, seed=1).float().to(DEV), leaf(double(12, 10, seed=2))
+    t = torch.arange(6, device=DEV)
+    layers.linear_cross_entropy(x, w, t).backward()
+    g = w.grad.clone()
+    w.grad = None
+    own = leaf(x)
+    layers.linear_cross_entropy(own, w.detach(), t).backward()
+    layers.linear_cross_entropy(own.detach(), w, t).backward()
+    assert torch.equal(w.grad, g) and torch.isfinite(own.grad).all()
+    b = leaf(double(10, seed=3))
+    layers.layer_norm(x, w.detach()[0], b).backward(torch.ones_like(x))
+    assert torch.equal(b.grad, torch.full_like(b, 6.0))
+
+
+def test_captured_training_step():
+    """Forward and backward of the chain captured once and replayed on new tokens: the eager gradients, bit for bit."""
+    d, v = 32, 50
+    tensors = [double(v, d, seed=1) * 0.2, 1 + 0.1 * double(d, seed=2), 0.1 * double(d, seed=3), double(v, d, seed=4) * 0.2]
+    own = [leaf(t) for t in tensors]
+    gen = torch.Generator(DEV).manual_seed(7)
+    tokens = torch.randint(0, v, (2, 33), generator=gen, device=DEV)
+
+    def step():
+        loss = chain(tokens, *own, own=True)
+        return (loss.detach(), *torch.autograd.grad(loss, own))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = step()
+    for turn in range(3):
+        tokens.copy_(torch.randint(0, v, tokens.shape, generator=gen, device=DEV))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [h.clone() for h in held]
+        want = step()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), turn
+
+
+def test_refusals():
+    x, w, t = leaf(double(4, 8, seed=1)), leaf(double(6, 8, seed=2)), torch.zeros(4, dtype=torch.int64, device=DEV)
+    v = torch.zeros(8, device=DEV)
+    for fn in (lambda: layers.layer_norm(x, v[:7]), lambda: layers.layer_norm(x, v, v.bfloat16()), lambda: layers.rms_norm(x, w),
+               lambda: layers.layer_norm(x.half()), lambda: layers.layer_norm(x, eps=-1.0), lambda: layers.rms_norm(x, v.cpu()),
+               lambda: layers.layer_norm(x.sum()), lambda: layers.embedding(t.int(), w), lambda: layers.embedding(t.cpu(), w),
+               lambda: layers.embedding(t, v), lambda: layers.embedding(t, w, padding_idx=6), lambda: layers.embedding(t, w, padding_idx=-1),
+               lambda: layers.embedding(t, w.half()), lambda: layers.linear_cross_entropy(x, w, t[:3]),
+               lambda: layers.linear_cross_entropy(x, w, t, reduction="max"), lambda: layers.linear_cross_entropy(x, w.bfloat16(), t),
+               lambda: layers.linear_cross_entropy(x, v, t), lambda: layers.linear_cross_entropy(x, w, t.int()),
+               lambda: layers.linear_cross_entropy(x, w[:0], t), lambda: layers.linear_cross_entropy(x, w[:, :7], t)):
+        with pytest.raises(smat.SmatError):
+            fn()
+
+
+def test_no_second_derivatives_and_no_tangents():
+    x, w, t = leaf(double(4, 8, seed=1)), leaf(double(6, 8, seed=2)), torch.zeros(4, dtype=torch.int64, device=DEV)
+    v = leaf(torch.ones(8))
+    fns = [lambda x, w: layers.layer_norm(x, v), lambda x, w: layers.rms_norm(x, v), lambda x, w: layers.embedding(t, w),
+           lambda x, w: layers.linear_cross_entropy(x, w, t)]
+    for i, fn in enumerate(fns):
+        by = w if i == 2 else x
+        g, = torch.autograd.grad(fn(x, w).pow(2).sum(), by, create_graph=True)
+        with pytest.raises(RuntimeError):
+            g.sum().backward()
+        with torch.autograd.forward_ad.dual_level():
+            dual = torch.autograd.forward_ad.make_dual(by.detach(), torch.ones_like(by))
+            with pytest.raises((RuntimeError, NotImplementedError)):
+                fn(dual if by is x else x.detach(), dual if by is w else w.detach())
+        with torch.autograd.forward_ad.dual_level():
+            dual = torch.autograd.forward_ad.make_dual(by, torch.ones_like(by))
+            with pytest.raises((RuntimeError, NotImplementedError)):
+                fn(dual if by is x else x, dual if by is w else w)

@@ -44,6 +44,15 @@ class RMSNorm(nn.Module):
         return (y * self.weight.float()).to(x.dtype)
 
 
+class FusedRMSNorm(RMSNorm):
+    """The same norm as one operator of the package."""
+
+    def forward(self, x):
+        from paper_2609_33437_amd import layers
+
+        return layers.rms_norm(x, self.weight, self.eps)
+
+
 class Attention(nn.Module):
     def __init__(self, d: int, heads: int):
         super().__init__()
@@ -92,11 +101,12 @@ class CheckpointedMLP(MLP):
 
 
 class Block(nn.Module):
-    def __init__(self, d: int, heads: int, ffn: int, checkpointed: bool = False):
+    def __init__(self, d: int, heads: int, ffn: int, checkpointed: bool = False, fused: bool = False):
         super().__init__()
-        self.input_norm = RMSNorm(d)
+        norm = FusedRMSNorm if fused else RMSNorm
+        self.input_norm = norm(d)
         self.attn = Attention(d, heads)
-        self.post_norm = RMSNorm(d)
+        self.post_norm = norm(d)
         self.mlp = (CheckpointedMLP if checkpointed else MLP)(d, ffn)
 
     def forward(self, x):
@@ -107,33 +117,52 @@ class Block(nn.Module):
 
 
 class Decoder(nn.Module):
-    def __init__(self, shape: DecoderShape, checkpointed: bool = False):
+    """With `fused` the embedding, the norms and the output layer's loss run through the package's operators; the loss then
+    never stores its logits."""
+
+    def __init__(self, shape: DecoderShape, checkpointed: bool = False, fused: bool = False):
         super().__init__()
         self.shape = shape
+        self.fused = fused
         self.embed = nn.Embedding(shape.vocab, shape.d)
-        self.blocks = nn.ModuleList([Block(shape.d, shape.heads, shape.ffn, checkpointed) for _ in range(shape.layers)])
-        self.norm = RMSNorm(shape.d)
+        self.blocks = nn.ModuleList([Block(shape.d, shape.heads, shape.ffn, checkpointed, fused)
+                                     for _ in range(shape.layers)])
+        self.norm = (FusedRMSNorm if fused else RMSNorm)(shape.d)
         self.lm_head = nn.Linear(shape.d, shape.vocab, bias=False)
         self.lm_head.weight = self.embed.weight
 
-    def forward(self, tokens):
-        x = self.embed(tokens)
-        if torch.is_autocast_enabled(tokens.device.type):
-            x = x.to(torch.get_autocast_dtype(tokens.device.type))
+    def hidden(self, tokens):
+        """What the output layer reads."""
+        if self.fused:
+            from paper_2609_33437_amd import layers
+
+            x = layers.embedding(tokens, self.embed.weight)
+        else:
+            x = self.embed(tokens)
+            if torch.is_autocast_enabled(tokens.device.type):
+                x = x.to(torch.get_autocast_dtype(tokens.device.type))
         for blk in self.blocks:
             x = blk(x)
-        return self.lm_head(self.norm(x))
+        return self.norm(x)
+
+    def forward(self, tokens):
+        return self.lm_head(self.hidden(tokens))
 
     def loss(self, tokens):
+        if self.fused:
+            from paper_2609_33437_amd import layers
+
+            return layers.linear_cross_entropy(self.hidden(tokens[:, :-1]), self.lm_head.weight, tokens[:, 1:])
         logits = self(tokens[:, :-1])
         return F.cross_entropy(logits.float().reshape(-1, logits.shape[-1]), tokens[:, 1:].reshape(-1))
 
 
-def make_decoder(shape: DecoderShape, seed: int, device="cpu", checkpointed: bool = False) -> Decoder:
+def make_decoder(shape: DecoderShape, seed: int, device="cpu", checkpointed: bool = False, fused: bool = False) -> Decoder:
     """Random-initialised decoder (normal(0, 0.02) linear and embedding weights, unit norms).  With
-    `checkpointed` its MLPs run through the package's operators (GPU only); the weights are the same."""
+    `checkpointed` its MLPs, with `fused` its embedding, norms and loss run through the package's operators (GPU only); the
+    weights are the same."""
     g = torch.Generator().manual_seed(seed)
-    model = Decoder(shape, checkpointed)
+    model = Decoder(shape, checkpointed, fused)
     with torch.no_grad():
         for name, p in model.named_parameters():
             if p.dim() >= 2:
