@@ -7,6 +7,8 @@
 // lie in the chunk; the sums of runs that chunks cut go to the workspace and another launch adds them, in order.  No
 // atomics, so a call's bits repeat.  Bound by HBM: dy is read once, and a gradient that is not accumulated writes every
 // row of the table, zeros where no token is.
+#include <type_traits>
+
 #include "smat_decoder.h"
 #include "smat_linear_dev.h"
 
@@ -23,24 +25,37 @@ void with_element(int dtype, F&& fn) {
 }
 
 // ---------------------------------------------------------------- lookup
-// Eight columns a thread.  An id outside the table gives a row of NaN.
+// kLookups eights of columns a thread, their ids and then their rows loaded together.  An id outside the table gives a row of
+// NaN.
+constexpr int kLookups = 4;
 template <typename T, typename U, typename Index>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs a, Index across, int64_t total) {
-  const int64_t t = wide_block() * 256 + threadIdx.x;
-  if (t >= total) return;
-  const Index row = (Index)t / across;
-  const int64_t j = (int64_t)((Index)t - row * across) * 8, valid = a.d - j;
-  const int64_t id = a.ids[row];
-  float v[8];
-  if (id >= 0 && id < a.rows) {
-    load_row8<T>(static_cast<const typename El<T>::Mem*>(a.table) + id * a.ldt + j, valid, v);
+  const int64_t first = wide_block() * (256 * kLookups) + threadIdx.x;
+  Index row[kLookups];
+  int64_t id[kLookups], j[kLookups];
+  Raw8<T> raw[kLookups];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= a.scale;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __builtin_nanf("");
+  for (int k = 0; k < kLookups; ++k) {
+    const int64_t t = first + k * 256;
+    row[k] = (Index)(t < total ? t : total - 1) / across;
+    j[k] = (int64_t)((Index)(t < total ? t : total - 1) - row[k] * across) * 8;
+    id[k] = a.ids[row[k]];
   }
-  store_row8<U>(static_cast<typename El<U>::Mem*>(a.out) + (int64_t)row * a.ldout + j, valid, v);
+#pragma unroll
+  for (int k = 0; k < kLookups; ++k) {
+    const bool in = id[k] >= 0 && id[k] < a.rows;
+    raw[k].load_some(static_cast<const typename El<T>::Mem*>(a.table) + (in ? id[k] : 0) * a.ldt + j[k], in ? a.d - j[k] : 0);
+  }
+#pragma unroll
+  for (int k = 0; k < kLookups; ++k) {
+    if (first + k * 256 >= total) return;
+    float v[8];
+    raw[k].get(v);
+    const bool in = id[k] >= 0 && id[k] < a.rows;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = in ? v[e] * a.scale : __builtin_nanf("");
+    store_row8<U>(static_cast<typename El<U>::Mem*>(a.out) + (int64_t)row[k] * a.ldout + j[k], a.d - j[k], v);
+  }
 }
 
 // ---------------------------------------------------------------- sort
@@ -165,8 +180,131 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(EmbedGradArgs a, So
   }
 }
 
+// ---------------------------------------------------------------- clearing, and the sort of few tokens beside it
+// A block of kSortThreads clears kClearEights eights a thread that follow each other over the block.  Rows end to end are
+// one row, whose whole 16 bytes are written at their addresses.
+constexpr int kClearEights = 8;
+struct ClearArgs {
+  void* table;
+  int64_t ld, rows, d;
+  int64_t before;  // elements up to the first 16-byte address of rows end to end
+  int64_t eights;  // in all
+};
+
+template <typename U>
+__device__ __forceinline__ void clear_block(const ClearArgs& c, int64_t block) {
+  auto* out = static_cast<typename El<U>::Mem*>(c.table);
+  const int64_t first = block * kSortThreads * kClearEights + threadIdx.x;
+  const float v[8] = {};
+  if (c.ld == c.d) {
+    const int64_t n = c.rows * c.d - c.before;
+    if (first < c.before) El<U>::store(out + first, 0.f);
+#pragma unroll
+    for (int k = 0; k < kClearEights; ++k) {
+      const int64_t j = (first + k * kSortThreads) * 8;
+      store_row8<U>(out + c.before + j, n - j, v);
+    }
+    return;
+  }
+  const int64_t across = (c.d + 7) / 8;
+#pragma unroll 1
+  for (int k = 0; k < kClearEights; ++k) {
+    const int64_t t = first + k * kSortThreads;
+    if (t >= c.eights) return;
+    const int64_t row = c.eights <= INT64_C(0x7FFFFFFF) ? (int64_t)((uint32_t)t / (uint32_t)across) : t / across;
+    const int64_t j = (t - row * across) * 8;
+    store_row8<U>(out + row * c.ld + j, c.d - j, v);
+  }
+}
+
+template <typename U>
+__global__ __launch_bounds__(kSortThreads) void k_embed_clear(ClearArgs c) {
+  clear_block<U>(c, wide_block());
+}
+
+// Up to kOneSort tokens are sorted in LDS by the first block, a wave's tokens consecutive, with their digits' places
+// counted as above.  The launch's other blocks clear the gradient meanwhile: 525 MB take 80 us, 6.6 TB/s, and the sort of
+// 4096 tokens 15 us of them.
+constexpr int64_t kOneSort = 16384;
+
+struct OneSort {
+  EmbedGradArgs a;
+  ClearArgs clear;
+  uint32_t* keys;
+  uint32_t* places;
+  int32_t bits, passes;
+};
+
+template <typename U, int ROUNDS>
+__global__ __launch_bounds__(kSortThreads) void k_embed_order(OneSort o) {
+  constexpr int kHeld = ROUNDS * kSortThreads;
+  __shared__ uint32_t keys[kHeld];
+  __shared__ uint16_t places[kHeld];
+  __shared__ uint32_t count[kSortWaves][kMaxDigits];
+  __shared__ uint32_t waves[kSortWaves];
+  if (wide_block() != 0) {
+    clear_block<U>(o.clear, wide_block() - 1);
+    return;
+  }
+  const EmbedGradArgs& a = o.a;
+  const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, first = wave * 64 * ROUNDS + lane, m = (int)a.m;
+  uint32_t key[ROUNDS], at[ROUNDS];
+  uint16_t place[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = first + r * 64;
+    key[r] = i < m ? token_key(a, i) : 0u;
+    place[r] = (uint16_t)i;
+  }
+  int32_t shift = 0, left = o.bits;
+  for (int p = 0; p < o.passes; ++p) {
+    const int bits = (left + o.passes - p - 1) / (o.passes - p);
+    const uint32_t mask = (1u << bits) - 1u;
+    for (int k = (int)threadIdx.x; k < kSortWaves * kMaxDigits; k += kSortThreads) (&count[0][0])[k] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) at[r] = wave_place((key[r] >> shift) & mask, bits, first + r * 64 < m, count[wave]);
+    __syncthreads();
+    // places of a digit's tokens of a wave: after all lower digits, and the digit's in earlier waves.  A thread adds up four
+    // waves' of a digit.
+    uint32_t c[4], total;
+    const int digit = (int)threadIdx.x >> 2, w0 = ((int)threadIdx.x & 3) * 4;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c[k] = count[w0 + k][digit];
+    uint32_t before = block_before(c[0] + c[1] + c[2] + c[3], waves, &total);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      count[w0 + k][digit] = before;
+      before += c[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+      if (first + r * 64 < m) {
+        const uint32_t to = count[wave][(key[r] >> shift) & mask] + at[r];
+        keys[to] = key[r];
+        places[to] = place[r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+      if (first + r * 64 < m) {
+        key[r] = keys[first + r * 64];
+        place[r] = places[first + r * 64];
+      }
+    shift += bits;
+    left -= bits;
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r)
+    if (first + r * 64 < m) {
+      o.keys[first + r * 64] = key[r];
+      o.places[first + r * 64] = place[r];
+    }
+}
+
 // ---------------------------------------------------------------- sums of rows
-struct RunArgs {
+struct RowArgs {
   EmbedGradArgs a;
   const uint32_t* keys;    // sorted
   const uint32_t* places;
@@ -186,56 +324,73 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& a, int64_t row, i
   store_row8<U>(out, valid, v);
 }
 
+// A lane holds one of the next 64 keys and places, so that a token's address waits for no load of its own.
 template <typename T, typename U>
-__global__ __launch_bounds__(256) void k_embed_sum(RunArgs r) {
+__global__ __launch_bounds__(256) void k_embed_sum(RowArgs r) {
   constexpr int kAhead = 8;
   const EmbedGradArgs& a = r.a;
-  const int64_t t = wide_block() * 4 + ((int)threadIdx.x >> 6);
+  const int lane = (int)threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int64_t t = wide_block() * 4 + wave;
   const int64_t c = t / r.tiles;
   if (c >= r.chunks) return;
-  const int32_t eight = (int32_t)(t - c * r.tiles) * 64 + ((int)threadIdx.x & 63);
-  const int64_t j = (int64_t)eight * 8, valid = a.d - j;
+  const int32_t eight = (int32_t)(t - c * r.tiles) * 64 + lane;
+  const int64_t j = (int64_t)eight * 8;
   const bool on = eight < r.across;
+  const int64_t valid = on ? a.d - j : 0;
   const int64_t begin = c * r.chunk, end = begin + r.chunk < a.m ? begin + r.chunk : a.m;
   const uint32_t none = (uint32_t)a.rows;
+  const auto* dy = static_cast<const typename El<T>::Mem*>(a.dy) + j;
   float* partial = r.partial + (c * 2 * r.across + eight) * 8;
-  uint32_t key = r.keys[begin];
-  // whether the run that is being summed began in an earlier chunk
-  bool cut = begin > 0 && r.keys[begin - 1] == key;
+  // the key before the chunk and after it: no key is 2^32 - 1
+  const uint32_t before = begin > 0 ? r.keys[begin - 1] : 0xFFFFFFFFu, after = end < a.m ? r.keys[end] : 0xFFFFFFFFu;
+  uint32_t key = 0;
+  bool cut = false;  // whether the run that is being summed began in an earlier chunk
   float sum[8] = {};
-  for (int64_t p0 = begin; p0 < end && key != none; p0 += kAhead) {
-    uint32_t keys[kAhead];
-    float v[kAhead][8];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int64_t p = p0 + u < end ? p0 + u : end - 1;
-      keys[u] = r.keys[p];
-      load_row8<T>(static_cast<const typename El<T>::Mem*>(a.dy) + (int64_t)r.places[p] * a.lddy + j, on ? valid : 0, v[u]);
+  for (int64_t p0 = begin; p0 < end; p0 += 64) {
+    const int64_t mine = p0 + lane < end ? p0 + lane : end - 1;
+    const uint32_t keys = r.keys[mine], places = r.places[mine];
+    const int count = (int)(end - p0 < 64 ? end - p0 : 64);
+    if (p0 == begin) {
+      key = (uint32_t)__builtin_amdgcn_readlane((int)keys, 0);
+      cut = key == before;
     }
+    for (int q = 0; q < count; q += kAhead) {
+      Raw8<T> raw[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (p0 + u >= end) break;
-      if (keys[u] != key) {  // the run's end
-        if (on) {
-          if (cut)
-            El<float>::store8(partial, sum);
-          else
-            write_row<U>(a, key, j, sum);
-        }
-        cut = false;
-        key = keys[u];
-        if (key == none) break;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+      for (int u = 0; u < kAhead; ++u) {
+        const int at = q + u < count ? q + u : count - 1;
+        const uint32_t place = (uint32_t)__builtin_amdgcn_readlane((int)places, at);
+        raw[u].load_some(dy + (int64_t)place * a.lddy, valid);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[u][e];
+      for (int u = 0; u < kAhead; ++u) {
+        if (q + u >= count) break;
+        const uint32_t next = (uint32_t)__builtin_amdgcn_readlane((int)keys, q + u);
+        if (next != key) {  // the run's end
+          if (on) {
+            if (cut)
+              El<float>::store8(partial, sum);
+            else
+              write_row<U>(a, key, j, sum);
+          }
+          cut = false;
+          key = next;
+          if (key == none) return;  // the rest has no row
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+        }
+        float v[8];
+        raw[u].get(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+      }
     }
   }
   if (key == none || !on) return;
   if (cut)
     El<float>::store8(partial, sum);
-  else if (end < a.m && r.keys[end] == key)
+  else if (after == key)
     El<float>::store8(partial + (int64_t)r.across * 8, sum);
   else
     write_row<U>(a, key, j, sum);
@@ -243,7 +398,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(RunArgs r) {
 
 // The run that begins in chunk c and goes on behind it: its sums in the chunks' order.
 template <typename U>
-__global__ __launch_bounds__(256) void k_embed_join(RunArgs r) {
+__global__ __launch_bounds__(256) void k_embed_join(RowArgs r) {
   const EmbedGradArgs& a = r.a;
   const int64_t t = wide_block() * 4 + ((int)threadIdx.x >> 6);
   const int64_t c = t / r.tiles;
@@ -267,25 +422,20 @@ __global__ __launch_bounds__(256) void k_embed_join(RunArgs r) {
   const float* p = r.partial + (c * 2 * r.across + eight) * 8;
   float sum[8];
   El<float>::load8(p + (int64_t)r.across * 8, sum);
-#pragma unroll 4
-  for (int64_t k = c + 1; k <= low; ++k) {
-    float v[8];
-    El<float>::load8(p + (k - c) * step, v);
+  constexpr int kAhead = 8;
+  for (int64_t k = 1; k <= low - c; k += kAhead) {
+    Raw8<float> raw[kAhead];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    for (int u = 0; u < kAhead; ++u) raw[u].load(p + (k + u <= low - c ? k + u : k) * step);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      float v[8];
+      raw[u].get(v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += k + u <= low - c ? v[e] : 0.f;
+    }
   }
   write_row<U>(a, key, (int64_t)eight * 8, sum);
-}
-
-// Zeros in every row.
-template <typename U, typename Index>
-__global__ __launch_bounds__(256) void k_embed_clear(EmbedGradArgs a, Index across, int64_t total) {
-  const int64_t t = wide_block() * 256 + threadIdx.x;
-  if (t >= total) return;
-  const Index row = (Index)t / across;
-  const int64_t j = (int64_t)((Index)t - row * across) * 8;
-  const float v[8] = {};
-  store_row8<U>(static_cast<typename El<U>::Mem*>(a.dtable) + (int64_t)row * a.ldt + j, a.d - j, v);
 }
 
 template <typename F>
@@ -303,7 +453,7 @@ hipError_t launch_embed(const EmbedArgs& a, int table_dtype, int dtype, hipStrea
     with_element(dtype, [&](auto u) {
       with_index(total, [&](auto index) {
         using Index = decltype(index);
-        k_embed<decltype(t), decltype(u), Index><<<wide_grid(div_up(total, 256)), dim3(256), 0, stream>>>(a, (Index)across, total);
+        k_embed<decltype(t), decltype(u), Index><<<wide_grid(div_up(total, 256 * kLookups)), dim3(256), 0, stream>>>(a, (Index)across, total);
       });
     });
   });
@@ -314,12 +464,12 @@ EmbedGradPlan embed_grad_plan(const EmbedGradArgs& a) {
   EmbedGradPlan p{};
   if (a.m == 0 || a.d == 0 || a.rows == 0) return p;
   // few tokens a wave where they are few; with many, as many chunks as keep the join's sums short
-  p.chunk = 32;
+  p.chunk = 8;
   while (p.chunk * 1024 < a.m) p.chunk *= 2;
   p.chunks = div_up(a.m, p.chunk);
   while ((a.rows >> p.bits) > 0) ++p.bits;
   p.passes = (p.bits + 7) / 8;
-  p.tiles = div_up(a.m, kSortTile);
+  p.tiles = a.m <= kOneSort ? 0 : div_up(a.m, kSortTile);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -340,22 +490,44 @@ hipError_t launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype,
                              void* workspace, hipStream_t stream) {
   hipError_t e = hipSuccess;
   const int64_t across = div_up(a.d, 8);
-  if (!a.accumulate) {
-    const int64_t total = a.rows * across;
-    with_element(table_dtype, [&](auto u) {
-      with_index(total, [&](auto index) {
-        using Index = decltype(index);
-        k_embed_clear<decltype(u), Index><<<wide_grid(div_up(total, 256)), dim3(256), 0, stream>>>(a, (Index)across, total);
-      });
-    });
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.m == 0) return e;
   char* ws = static_cast<char*>(workspace);
   const auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
   SortPass s{nullptr, nullptr, nullptr, nullptr, words(plan.counts), plan.tiles, 0, 0};
+  ClearArgs c{a.dtable, a.ldt, a.rows, a.d};
+  if (!a.accumulate) {
+    const int64_t n = a.rows * a.d, bytes = table_dtype == 1 ? 2 : 4;
+    c.before = (int64_t)(-reinterpret_cast<uintptr_t>(a.dtable) & 15u) / bytes;
+    if (c.before > n) c.before = n;
+    c.eights = a.ldt == a.d ? div_up(n - c.before, 8) : a.rows * across;
+  }
+  const int64_t clears = a.accumulate ? 0 : c.eights > 0 ? div_up(c.eights, kSortThreads * kClearEights) : 1;
+  const bool one = a.m > 0 && a.m <= kOneSort;
+  if (one) {
+    const OneSort o{a, c, words(plan.keys[0]), words(plan.places[0]), plan.bits, plan.passes};
+    with_element(table_dtype, [&](auto u) {
+      using U = decltype(u);
+      const auto order = [&](auto rounds) {
+        k_embed_order<U, rounds()><<<wide_grid(1 + clears), dim3(kSortThreads), 0, stream>>>(o);
+      };
+      if (a.m <= kSortThreads)
+        order(std::integral_constant<int, 1>());
+      else if (a.m <= 4 * kSortThreads)
+        order(std::integral_constant<int, 4>());
+      else if (a.m <= 8 * kSortThreads)
+        order(std::integral_constant<int, 8>());
+      else
+        order(std::integral_constant<int, 16>());
+    });
+    s.keys = o.keys;
+    s.places = o.places;
+  } else if (clears > 0) {
+    with_element(table_dtype, [&](auto u) {
+      k_embed_clear<decltype(u)><<<wide_grid(clears), dim3(kSortThreads), 0, stream>>>(c);
+    });
+  }
+  if ((e = hipGetLastError()) != hipSuccess || a.m == 0) return e;
   int32_t left = plan.bits;
-  for (int p = 0; p < plan.passes; ++p) {
+  for (int p = 0; p < plan.passes && !one; ++p) {
     s.bits = (left + plan.passes - p - 1) / (plan.passes - p);
     s.keys_to = words(plan.keys[p % 2]);
     s.places_to = words(plan.places[p % 2]);
@@ -369,7 +541,7 @@ hipError_t launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype,
     s.keys = s.keys_to;
     s.places = s.places_to;
   }
-  RunArgs r{a, s.keys, s.places, reinterpret_cast<float*>(ws + plan.partial), plan.chunk, plan.chunks, (int32_t)across,
+  RowArgs r{a, s.keys, s.places, reinterpret_cast<float*>(ws + plan.partial), plan.chunk, plan.chunks, (int32_t)across,
             (int32_t)div_up(across, 64)};
   const dim3 grid = wide_grid(div_up(r.chunks * r.tiles, 4));
   with_element(table_dtype, [&](auto u) {

@@ -110,31 +110,6 @@ __device__ __forceinline__ Frag<T> read_frag(const char* stage, int row0, int t,
   return f;
 }
 
-// ---------------------------------------------------------------- operands of any alignment
-// 16 bytes at any element's address where `valid` elements or more of them exist, else what there is, zeros after it.
-template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const typename El<T>::Mem* p, int32_t valid) {
-  constexpr int kChunk = 16 / El<T>::kBytes;
-  typedef uint32_t word_mem __attribute__((aligned(2)));
-  if (valid >= kChunk) return *reinterpret_cast<const typename El<T>::vec_mem*>(p);
-  u32x4 x = {0u, 0u, 0u, 0u};
-  if (valid <= 0) return x;
-  const int32_t words = valid * El<T>::kBytes / 4;  // whole ones; bf16 may have half a word more
-  const auto* w = reinterpret_cast<const word_mem*>(p);
-#pragma unroll
-  for (int e = 0; e < 3; ++e)
-    if (e < words) x[e] = w[e];
-  if constexpr (El<T>::kBytes == 2) {
-    if (valid & 1) {
-      const uint32_t half = p[valid - 1];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e == words) x[e] = half;
-    }
-  }
-  return x;
-}
-
 // The epilogue of a wave's accumulators, or their store as a partial sum: four eights of values a lane at a
 // time, chosen by a branch on a uniform number.  Unrolled over all 16 eights an epilogue with an activation is 100 KB
 // of instructions that every tile reads anew; one eight at a time, its branches, its loads of other matrices and its

@@ -82,6 +82,30 @@ __device__ __forceinline__ void store_row8(typename El<T>::Mem* p, int64_t valid
   }
 }
 
+// 16 bytes at any element's address where `valid` elements or more of them exist, else what there is, zeros after it.
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const typename El<T>::Mem* p, int32_t valid) {
+  constexpr int kChunk = 16 / El<T>::kBytes;
+  typedef uint32_t word_mem __attribute__((aligned(2)));
+  if (valid >= kChunk) return *reinterpret_cast<const typename El<T>::vec_mem*>(p);
+  u32x4 x = {0u, 0u, 0u, 0u};
+  if (valid <= 0) return x;
+  const int32_t words = valid * El<T>::kBytes / 4;  // whole ones; bf16 may have half a word more
+  const auto* w = reinterpret_cast<const word_mem*>(p);
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < words) x[e] = w[e];
+  if constexpr (El<T>::kBytes == 2) {
+    if (valid & 1) {
+      const uint32_t half = p[valid - 1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e == words) x[e] = half;
+    }
+  }
+  return x;
+}
+
 // ---------------------------------------------------------------- activations
 // exp, erf and a reciprocal to the accuracy that the type of the result holds: the library's functions
 // for fp32; for bf16 the hardware's exp2 and reciprocal, and erfc by formula 7.1.26 of Abramowitz and
@@ -228,6 +252,10 @@ template <>
 struct Raw8<Bf16> {
   u32x4 x;
   __device__ __forceinline__ void load(const uint16_t* p) { x = *reinterpret_cast<const El<Bf16>::vec_mem*>(p); }
+  // the first `valid` elements, zeros after them
+  __device__ __forceinline__ void load_some(const uint16_t* p, int64_t valid) {
+    x = load_chunk<Bf16>(p, (int32_t)(valid < 8 ? valid : 8));
+  }
   __device__ __forceinline__ void get(float v[8]) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -242,6 +270,11 @@ struct Raw8<float> {
   __device__ __forceinline__ void load(const float* p) {
     x[0] = *reinterpret_cast<const f32x4_mem*>(p);
     x[1] = *reinterpret_cast<const f32x4_mem*>(p + 4);
+  }
+  __device__ __forceinline__ void load_some(const float* p, int64_t valid) {
+    const int32_t n = (int32_t)(valid < 8 ? valid : 8);
+    x[0] = __builtin_bit_cast(f32x4, load_chunk<float>(p, n < 4 ? n : 4));
+    x[1] = __builtin_bit_cast(f32x4, load_chunk<float>(p + 4, n - 4));
   }
   __device__ __forceinline__ void get(float v[8]) const {
 #pragma unroll
