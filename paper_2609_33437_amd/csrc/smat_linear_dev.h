@@ -106,6 +106,46 @@ __device__ __forceinline__ u32x4 load_chunk(const typename El<T>::Mem* p, int32_
   return x;
 }
 
+// ---------------------------------------------------------------- sums over lanes
+// What `op` makes of the values of N consecutive lanes (N = 4, 8, 16, 32 or 64), in each of them: neighbours are exchanged
+// within 16 lanes by the vector unit's own lane operands, and rows of 16 by the swaps, where a shuffle would pass
+// LDS six times.  op is symmetric, so all lanes form the same bits.
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+// op of this lane's value and that of lane l ^ 16, l ^ 32.
+template <typename F>
+__device__ __forceinline__ float with_lane16(float v, F&& op) {
+  const uint32_t b = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <typename F>
+__device__ __forceinline__ float with_lane32(float v, F&& op) {
+  const uint32_t b = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <int N, typename F>
+__device__ __forceinline__ float over_lanes(float v, F&& op) {
+  v = op(v, lane_move<0xB1>(v));                       // l ^ 1
+  v = op(v, lane_move<0x4E>(v));                       // l ^ 2
+  if constexpr (N > 4) v = op(v, lane_move<0x141>(v));  // 7 - l: the other four
+  if constexpr (N > 8) v = op(v, lane_move<0x140>(v));  // 15 - l: the other eight
+  if constexpr (N > 16) v = with_lane16(v, op);
+  if constexpr (N > 32) v = with_lane32(v, op);
+  return v;
+}
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return over_lanes<N>(v, [](float a, float b) { return a + b; });
+}
+template <int N>
+__device__ __forceinline__ float lanes_max(float v) {
+  return over_lanes<N>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
 // ---------------------------------------------------------------- activations
 // exp, erf and a reciprocal to the accuracy that the type of the result holds: the library's functions
 // for fp32; for bf16 the hardware's exp2 and reciprocal, and erfc by formula 7.1.26 of Abramowitz and
