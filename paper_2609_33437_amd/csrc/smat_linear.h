@@ -60,10 +60,11 @@ struct LinArgs {
   int64_t ldup;
   int32_t act;
   // cross entropy of logits v, columns col0 .. col0 + j of `classes` ones: the largest value and the sum of exponentials of
-  // each 32 columns of a row, and the target's logit; or out = (exp(v - lse) - [column is the target]) row_scale
+  // each tile's columns of a row, and the target's logit; or out = (exp(v - lse) - [column is the target]) row_scale
   const int64_t* targets;
   int64_t ignore, classes, col0;
-  float* stats;  // [i][ceil(j / 32)][2]
+  float* stats;  // [i][stat_ld][2]
+  int64_t stat_ld;
   float* target_z;
   const float* lse;
   const float* row_scale;  // NULL: 1
@@ -94,6 +95,8 @@ struct LinPlan {
 };
 // Element types by smat_dtype code: 0 = fp32, 1 = bf16.
 LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi);
+// Columns that one pair of a row's stats covers in a part of a plan.
+int64_t stat_columns(const LinPart& part);
 hipError_t launch_linear(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
                          hipStream_t stream);
 

@@ -169,6 +169,61 @@ __device__ __forceinline__ void finish_eights(const LinArgs& a, int64_t i0, int6
   }
 }
 
+// The statistics of a tile's rows from the waves' accumulators (see finish_eights): every wave's over its columns, in
+// registers, then over the WJ waves that share the rows (this is number wave_j), through LDS (`lds`, which nothing else uses any more).  One pair a
+// row and tile is written.  65,536 logits take about 4 us so (9 us eight by eight, with sixteen pairs a row and shuffles
+// through LDS).
+template <typename T, int KI, int WJ, int THREADS, int NI, int NJ, typename R, typename C>
+__device__ __forceinline__ void finish_stats(const LinArgs& a, int64_t i0, int wi, int64_t j0, int wj, int wave_j,
+                                             const f32x4 (&acc)[NI][NJ], uint32_t tj, char* lds, R rows, C cols) {
+  const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+  f32x2* slots = reinterpret_cast<f32x2*>(lds);  // [KI][WJ + 1]
+  const int32_t left = (int32_t)(a.j - j0 < 0x40000000 ? a.j - j0 : 0x40000000);  // columns of the tile that exist
+  const int first = wj + 8 * g;
+  __syncthreads();
+#pragma unroll
+  for (int p = 0; p < NI; ++p) {
+    const int at = wi + rows(p) + l;
+    const int64_t i = i0 + at;
+    float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < NJ / 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (first + cols(q) + e < left) top = fmaxf(top, acc[p][2 * q + e / 4][e % 4]);
+    const auto larger = [](float x, float y) { return fmaxf(x, y); };
+    const auto add = [](float x, float y) { return x + y; };
+    top = with_lane32(with_lane16(top, larger), larger);
+    const StatExp<T> from(top);
+#pragma unroll
+    for (int q = 0; q < NJ / 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += first + cols(q) + e < left ? from(acc[p][2 * q + e / 4][e % 4]) : 0.f;
+    sum = with_lane32(with_lane16(sum, add), add);
+    if (g == 0) slots[at * (WJ + 1) + wave_j] = f32x2{top, sum};
+    // the target's logit, where one of these columns is it
+    const int64_t target = i < a.i ? a.targets[i] - a.col0 - j0 - first : -1;
+#pragma unroll
+    for (int q = 0; q < NJ / 2; ++q) {
+      const int64_t d = target - cols(q);
+      if (d >= 0 && d < 8 && first + cols(q) + d < left) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (d == e) a.target_z[i] = acc[p][2 * q + e / 4][e % 4];
+      }
+    }
+  }
+  __syncthreads();
+  for (int at = (int)threadIdx.x; at < KI; at += THREADS) {
+    if (i0 + at >= a.i) break;
+    f32x2 s = slots[at * (WJ + 1)];
+    float top = s[0], sum = s[1];
+#pragma unroll
+    for (int k = 1; k < WJ; ++k) join_stats(top, sum, slots[at * (WJ + 1) + k][0], slots[at * (WJ + 1) + k][1]);
+    *reinterpret_cast<f32x2*>(a.stats + ((i0 + at) * a.stat_ld + tj) * 2) = f32x2{top, sum};
+  }
+}
+
 // ROWS and COLS of the last tile and pair bound the wave's part of the tile.
 template <typename T, int EPI, int NI, int NJ, typename R, typename C>
 __device__ __forceinline__ void finish(const LinArgs& a, int64_t i0, int64_t j0, const f32x4 (&acc)[NI][NJ], R rows,
@@ -550,9 +605,15 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy outlives the block's LDS
   if (wave < 4) __builtin_amdgcn_s_barrier();
-  finish<T, EPI>(
-      a, i0 + wi, j0 + wj, acc, [](int p) { return p / 4 * kFastHalf + p % 4 * 16; },
-      [](int q) { return q * kFastHalf; });
+  const auto rows = [](int p) { return p / 4 * kFastHalf + p % 4 * 16; };
+  const auto cols = [](int q) { return q * kFastHalf; };
+  if constexpr (EPI == kEpiXent) {
+    if (a.splits == 1) {
+      finish_stats<T, kFastB, 4, kFastThreads>(a, i0, wi, j0, wj, wave % 4, acc, tj, smem, rows, cols);
+      return;
+    }
+  }
+  finish<T, EPI>(a, i0 + wi, j0 + wj, acc, rows, cols);
 }
 
 // ---------------------------------------------------------------- smaller tiles
@@ -748,8 +809,15 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   }
   wait_copies<0>();  // no copy outlives the block's LDS, or lands on the sums
   if constexpr (S::G == 1) {
-    finish<T, EPI>(
-        a, i0 + wi, j0 + wj, acc, [](int p) { return 16 * p; }, [](int q) { return 32 * q; });
+    const auto rows = [](int p) { return 16 * p; };
+    const auto cols = [](int q) { return 32 * q; };
+    if constexpr (EPI == kEpiXent) {
+      if (a.splits == 1) {
+        finish_stats<T, S::kI, S::WJ, S::kThreads>(a, i0, wi, j0, wj, w % S::WJ, acc, tj, smem, rows, cols);
+        return;
+      }
+    }
+    finish<T, EPI>(a, i0 + wi, j0 + wj, acc, rows, cols);
   } else {
     // the groups' sums side by side, added in the groups' order
     __syncthreads();
@@ -787,6 +855,8 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
       if (a.splits > 1) {
         const int64_t ld = (a.j + 7) & ~(int64_t)7;
         if (gi < a.i && gj < ld) El<float>::store8(a.partial + ((int64_t)blockIdx.y * a.i + gi) * ld + gj, v);
+      } else if constexpr (EPI == kEpiXent) {
+        eight_stats<T, S::kJ / 8>(a, gi, gj, a.j - gj, v, side.target, tj);
       } else {
         epilogue8<T, EPI, 1, 2>(a, gi, gj, v, column, side);
       }
@@ -912,7 +982,10 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
   for (int g = 0; g < kGroups; ++g)
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += sums[g][fi][fj + e];
-  epilogue8<T, EPI, 1, 2>(a, fi, j0 + fj, v, column, side);
+  if constexpr (EPI == kEpiXent)
+    eight_stats<T, JB / 8>(a, fi, j0 + fj, a.j - j0 - fj, v, side.target, blockIdx.x);
+  else
+    epilogue8<T, EPI, 1, 2>(a, fi, j0 + fj, v, column, side);
 }
 
 // Joins the partial sums in their order and applies the epilogue: eight j a thread.  Bound by memory: two ranges of
@@ -935,7 +1008,10 @@ __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
   ColumnSide<T, EPI> c;
   column_load<T, EPI>(a, j, c);
   side_load<T, EPI>(a, i, j, s);
-  epilogue8<T, EPI, 1, 2>(a, i, j, v, c, s);
+  if constexpr (EPI == kEpiXent)
+    eight_stats<T, kCkptBlock / 8>(a, i, j, a.j - j, v, s.target, j / kCkptBlock);
+  else
+    epilogue8<T, EPI, 1, 2>(a, i, j, v, c, s);
 }
 
 // ---------------------------------------------------------------- copies on 16-byte rows
@@ -1246,6 +1322,18 @@ void operands(const LinArgs& a, LinEpilogue epi, int bytes, Operand (&o)[4]) {
 int64_t packed_ld(int64_t run, int bytes) { return div_up(run * bytes, 16) * 16 / bytes; }
 }  // namespace
 
+int64_t stat_columns(const LinPart& part) {
+  if (part.splits > 1) return kCkptBlock;  // as the join writes them
+  switch (part.form) {
+    case kFast: return kFastB;
+    case kMiddle: return MiddleShape::kJ;
+    case kPair: return PairShape::kJ;
+    case kSmall: return SmallShape::kJ;
+    case kNarrow: return NarrowShape::kJ;
+    default: return kCkptBlock;  // kTiny, kRows
+  }
+}
+
 LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   const int bytes = dtype == 1 ? 2 : 4;
   const int64_t deep = 128 / bytes;
@@ -1343,7 +1431,6 @@ LinArgs rows_of(LinArgs a, int64_t from, int64_t rows, int bytes, bool pt) {
   a.up_codes = static_cast<const int8_t*>(skip_bytes(a.up_codes, from * nb * kCkptBlock));
   a.up_exps = static_cast<const uint8_t*>(skip_bytes(a.up_exps, from * nb));
   a.targets = static_cast<const int64_t*>(skip_bytes(a.targets, from * 8));
-  a.stats = static_cast<float*>(skip_bytes(a.stats, from * nb * 8));
   a.target_z = static_cast<float*>(skip_bytes(a.target_z, from * 4));
   a.lse = static_cast<const float*>(skip_bytes(a.lse, from * 4));
   a.row_scale = static_cast<const float*>(skip_bytes(a.row_scale, from * 4));
@@ -1407,11 +1494,17 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   int64_t from = 0;
+  float* stats = whole.stats;
   for (int p = 0; p < plan.parts && e == hipSuccess; ++p) {
     const LinPart& part = plan.part[p];
     LinArgs a = rows_of(whole, from, part.rows, bytes, p_transposed(epi));
     a.splits = part.splits;
     from += part.rows;
+    if (epi == kEpiXent) {  // the parts' statistics one after the other
+      a.stat_ld = div_up(a.j, stat_columns(part));
+      a.stats = stats;
+      stats += a.i * a.stat_ld * 2;
+    }
     const int64_t eights = a.i * ckpt_blocks(a.j) * 4;  // of the join
     if (part.form == 0 || (a.splits > 1 && eights > kMaxThreads - 256)) return hipErrorInvalidConfiguration;
     with_form(dtype, epi, [&](auto t, auto pt, auto qt, auto ep) {

@@ -368,7 +368,7 @@ __device__ __forceinline__ float total_scale(const LinArgs& a) {
   const float count = a.totals[1];
   return count > 0.f ? s / count : 0.f;
 }
-// Where eight consecutive columns from j0 on hold the target, or a number outside [0, 8).
+// Where eight consecutive columns from j0 on hold the target, or -1.
 __device__ __forceinline__ int target_place(const LinArgs& a, int64_t target, int64_t j0) {
   const int64_t at = target - a.col0 - j0;
   return at >= 0 && at < 8 ? (int)at : -1;
@@ -432,6 +432,52 @@ __device__ __forceinline__ void side_values(const Raw8<T>& raw, const void* row,
   }
 }
 
+// ---------------------------------------------------------------- statistics of logits
+// exp(v - top) as the sums take it.  In bf16 the product with log2 e is one fused operation, which rounds top log2 e: an error
+// of an fp32 rounding of top in the row's log sum.
+template <typename T>
+struct StatExp {
+  float top, shift;
+  __device__ __forceinline__ explicit StatExp(float t) {
+    top = t == -__builtin_inff() ? 0.f : t;  // only -inf: a sum of zeros
+    shift = -top * 1.44269504088896340736f;
+  }
+  __device__ __forceinline__ float operator()(float v) const {
+    if constexpr (El<T>::kBytes == 4)
+      return expf(v - top);
+    else
+      return __builtin_amdgcn_exp2f(__builtin_fmaf(v, 1.44269504088896340736f, shift));
+  }
+};
+// (top, sum) of two sets of values: sum = sum exp(v - top), and exp(v - 0) where there is only -inf.
+__device__ __forceinline__ void join_stats(float& top, float& sum, float other_top, float other_sum) {
+  const float t = fmaxf(top, other_top), from = t == -__builtin_inff() ? 0.f : t;
+  sum = sum * expf(top - from) + other_sum * expf(other_top - from);
+  top = t;
+}
+// Row i's values v[8] of columns j0 on, of which `valid` exist, the rest of the row's tile in the LANES - 1 neighbouring lanes:
+// its largest value and sum of exponentials, written by the first lane to stats number `slot`, and its target's logit.
+template <typename T, int LANES>
+__device__ __forceinline__ void eight_stats(const LinArgs& a, int64_t i, int64_t j0, int64_t valid, const float v[8],
+                                            int64_t target, int64_t slot) {
+  float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = e < valid ? fmaxf(top, v[e]) : top;
+  top = lanes_max<LANES>(top);
+  const StatExp<T> from(top);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum += e < valid ? from(v[e]) : 0.f;
+  sum = lanes_sum<LANES>(sum);
+  if (i >= a.i) return;
+  if (valid > 0) {
+    const int at = target_place(a, target, j0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e == at && e < valid) a.target_z[i] = v[e];
+  }
+  if ((threadIdx.x & (LANES - 1)) == 0) *reinterpret_cast<f32x2*>(a.stats + (i * a.stat_ld + slot) * 2) = f32x2{top, sum};
+}
+
 // The epilogue on out[i][j0 .. j0 + 8), j0 a multiple of 8, with what column_load and side_load loaded for it;
 // the four lanes of a checkpoint block differ in lane bits A and B.  Every lane of the wave calls it (i or j0 may
 // lie outside).
@@ -474,33 +520,22 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
       for (int e = 0; e < 8; ++e) v[e] += u[e];
     }
   }
-  if constexpr (EPI == kEpiXent) {
-    // the four lanes' 32 columns
-    float top = -__builtin_inff(), sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = e < valid ? fmaxf(top, v[e]) : top;
-    top = fmaxf(top, __shfl_xor(top, A));
-    top = fmaxf(top, __shfl_xor(top, B));
-    const float from = top == -__builtin_inff() ? 0.f : top;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += e < valid ? act_exp<T>(v[e] - from) : 0.f;
-    sum += __shfl_xor(sum, A);
-    sum += __shfl_xor(sum, B);
-    if (valid <= 0) return;
-    const int at = target_place(a, s.target, j0);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e == at && e < valid) a.target_z[i] = v[e];
-    if (j0 % kCkptBlock == 0) *reinterpret_cast<f32x2*>(a.stats + (i * row_blocks(a) + j0 / kCkptBlock) * 2) = f32x2{top, sum};
-    return;
-  }
   if (valid <= 0) return;
   if constexpr (EPI == kEpiXentGrad) {
-    const int at = target_place(a, s.target, j0);
-    const bool none = s.target == a.ignore, outside = s.target < 0 || s.target >= a.classes;
+    const bool outside = s.target < 0 || s.target >= a.classes;
     const float scale = outside ? __builtin_nanf("") : s.scale;
+    if (s.target == a.ignore) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = none ? 0.f : (act_exp<T>(v[e] - s.lse) - (e == at ? 1.f : 0.f)) * scale;
+      for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    } else {
+      const int at = target_place(a, s.target, j0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = act_exp<T>(v[e] - s.lse) * scale;
+      if (at >= 0) {  // one eight of a row
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] -= e == at ? scale : 0.f;
+      }
+    }
   }
   if constexpr (EPI == kEpiSum) {
     if (a.sum_in) {

@@ -3,7 +3,7 @@
 //   lse_i = log sum_j exp z_ij,  loss_i = lse_i - z_i,t_i
 //   dz_ij = (exp(z_ij - lse_i) - [j = t_i]) g_i,  dx = s dz W,  dW = s dz^T x
 //
-// The forward product's epilogue leaves the largest value and the sum of exponentials of each 32 columns of a row, which
+// The forward product's epilogue leaves the largest value and the sum of exponentials of each tile's columns of a row, which
 // k_xent_rows joins.  The gradient goes through the vocabulary in pieces: a piece's logits again, turned into dz (in the
 // call's dtype) by their epilogue, then dz W added to dx in fp32 and dz^T x, which is the piece's part of dW.  So beside
 // its outputs a call holds one piece, whatever the vocabulary, for a fourth product beside the three that
@@ -16,19 +16,13 @@ namespace {
 
 constexpr int kRowThreads = 256;
 
-// (top, sum) of two sets of values: sum = sum exp(v - top), and exp(v - 0) where there is only -inf.
-__device__ __forceinline__ void join_stats(float& top, float& sum, float other_top, float other_sum) {
-  const float t = fmaxf(top, other_top), from = t == -__builtin_inff() ? 0.f : t;
-  sum = sum * expf(top - from) + other_sum * expf(other_top - from);
-  top = t;
-}
-
 // A row's log sum of exponentials from its parts, and its loss.
-__global__ __launch_bounds__(kRowThreads) void k_xent_rows(XentArgs a, const float* stats, const float* target_z, int64_t parts) {
+__global__ __launch_bounds__(kRowThreads) void k_xent_rows(XentArgs a, const float* stats, const float* target_z, int64_t from,
+                                                           int64_t rows, int64_t parts) {
   __shared__ float tops[kRowThreads / 64], sums[kRowThreads / 64];
-  const int64_t i = wide_block();
-  if (i >= a.m) return;
-  const f32x2* s = reinterpret_cast<const f32x2*>(stats) + i * parts;
+  if (wide_block() >= rows) return;
+  const f32x2* s = reinterpret_cast<const f32x2*>(stats) + wide_block() * parts;
+  const int64_t i = from + wide_block();
   float top = -__builtin_inff(), sum = 0.f;
   for (int64_t k = threadIdx.x; k < parts; k += kRowThreads) {
     const f32x2 v = s[k];
@@ -103,7 +97,10 @@ XentPlan xent_plan(const XentArgs& a, int dtype) {
   if (a.m == 0) return p;
   p.logits = linear_plan(logits_args(a, nullptr, p), dtype, kEpiXent);
   p.stats = round16(p.logits.workspace);
-  p.target_z = p.stats + round16((size_t)a.m * (size_t)ckpt_blocks(a.n) * 8);
+  size_t pairs = 0;
+  for (int k = 0; k < p.logits.parts; ++k)
+    pairs += (size_t)p.logits.part[k].rows * (size_t)div_up(a.n, stat_columns(p.logits.part[k]));
+  p.target_z = p.stats + round16(pairs * 8);
   p.workspace = p.target_z + round16((size_t)a.m * 4);
   return p;
 }
@@ -114,8 +111,15 @@ hipError_t launch_xent(const XentArgs& a, int dtype, const XentPlan& plan, void*
     const LinArgs l = logits_args(a, workspace, plan);
     e = launch_linear(l, dtype, kEpiXent, plan.logits, workspace, stream);
     if (e != hipSuccess) return e;
-    k_xent_rows<<<wide_grid(a.m), dim3(kRowThreads), 0, stream>>>(a, l.stats, l.target_z, ckpt_blocks(a.n));
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const float* stats = l.stats;
+    int64_t from = 0;
+    for (int p = 0; p < plan.logits.parts; ++p) {
+      const int64_t rows = plan.logits.part[p].rows, parts = div_up(a.n, stat_columns(plan.logits.part[p]));
+      k_xent_rows<<<wide_grid(rows), dim3(kRowThreads), 0, stream>>>(a, stats, l.target_z, from, rows, parts);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      from += rows;
+      stats += rows * parts * 2;
+    }
   }
   if (a.totals) {
     k_xent_totals<<<dim3(1), dim3(1024), 0, stream>>>(a);
