@@ -113,8 +113,9 @@ struct XentGradArgs {
 // Pieces of `width` columns of the vocabulary, the last one narrower: how each piece's products are computed.
 struct XentGradPlan {
   int64_t width, pieces;
+  int32_t pack;  // bits: x, and each piece of W, are copied to 16-byte rows for all products
   LinPlan logits[2], dx[2], dw[2];  // of a whole piece and of the last one
-  size_t dz, sum, product, workspace;
+  size_t dz, sum, x, w, workspace;  // behind the products' own
 };
 XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype);
 hipError_t launch_xent_grad(const XentGradArgs& a, int dtype, const XentGradPlan& plan, void* workspace, hipStream_t stream);

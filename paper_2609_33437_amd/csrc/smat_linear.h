@@ -37,6 +37,7 @@ struct LinProduct {
   const void* q;
   int64_t ldp, ldq;
   int64_t r;
+  bool p_clean;  // P's rows hold finite values, whatever they are, from their end to the next 16 bytes
 };
 
 struct LinArgs {
@@ -92,6 +93,7 @@ struct LinPlan {
   int32_t pack;      // bits: operands copied to 16-byte rows first (P, Q of prod[0], then of prod[1])
   size_t packed[4];  // where in the workspace
   size_t workspace;  // bytes
+  double us;         // estimated
 };
 // Element types by smat_dtype code: 0 = fp32, 1 = bf16.
 LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi);
@@ -99,6 +101,11 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi);
 int64_t stat_columns(const LinPart& part);
 hipError_t launch_linear(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,
                          hipStream_t stream);
+
+// Copies `rows` runs of `run` elements to rows of packed_stride(run) elements, whole 16 bytes with zeros at their ends.
+int64_t packed_stride(int64_t run, int dtype);
+hipError_t launch_pack(const void* from, int64_t ld, int64_t rows, int64_t run, int dtype, void* to, hipStream_t stream);
+constexpr double pack_us(double bytes) { return 3.0 + 2.0 * bytes / 5.0e6; }
 
 // db[j] = sum_i dy[i][j] for dy [rows, cols].
 hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t cols, int dtype, void* db,

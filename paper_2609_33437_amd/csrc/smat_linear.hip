@@ -1225,6 +1225,7 @@ struct Sizes {
   double epilogue;
   double bytes;  // of the operands
   int64_t line;  // columns of a transposed Q in a cache line, or 0
+  double rows;   // bytes of Q where rows of P that are left over may take the kernel for few rows, or 0
 };
 
 // Microseconds of `splits` ranges of r with tile f, or kNever where its grid cannot be launched.
@@ -1293,7 +1294,15 @@ double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& p
     first.i = rows;
     rest.i = z.i - rows;
     LinPart other;
-    const double us = time_of(f, first, 1) + kLaunch + choose(costs, count, rest, other);
+    double after = choose(costs, count, rest, other);
+    if (z.rows > 0.0 && rest.i <= kMaxRows) {
+      const double few = kRowsStart + z.rows / kRowsRate[rest.i > 4 ? 3 : rest.i > 2 ? 2 : rest.i - 1];
+      if (few < after) {
+        after = few;
+        other = {rest.i, kRows, 1};
+      }
+    }
+    const double us = time_of(f, first, 1) + kLaunch + after;
     if (us < least) {
       least = us;
       plan.part[0] = {rows, f.form, 1};
@@ -1315,7 +1324,8 @@ void operands(const LinArgs& a, LinEpilogue epi, int bytes, Operand (&o)[4]) {
   const bool pt = p_transposed(epi), qt = q_transposed(epi);
   for (int s = 0; s < 2; ++s) {
     const LinProduct& pr = a.prod[s];
-    o[2 * s] = {pr.p, pr.ldp, pt ? pr.r : a.i, pt ? a.i : pr.r, pr.r == 0 || operand_fits(pr.p, pr.ldp, pr.r, pt, bytes), pt};
+    const int64_t ends = pr.p_clean ? 0 : pr.r;  // Q's rows past r read as zeros, so finite values past P's do no harm
+    o[2 * s] = {pr.p, pr.ldp, pt ? pr.r : a.i, pt ? a.i : pr.r, pr.r == 0 || operand_fits(pr.p, pr.ldp, ends, pt, bytes), pt};
     o[2 * s + 1] = {pr.q, pr.ldq, qt ? pr.r : a.j, qt ? a.j : pr.r, pr.r == 0 || operand_fits(pr.q, pr.ldq, pr.r, qt, bytes), qt};
   }
 }
@@ -1345,6 +1355,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   if (epi == kEpiSum) z.epilogue = 4.0;
   Operand o[4];
   operands(a, epi, bytes, o);
+  if (epi == kEpiXent || epi == kEpiXentGrad) z.rows = (double)a.j * (double)a.prod[0].r * bytes;
   int32_t off = 0;  // operands that cannot be copied to LDS directly as they lie
   bool wide = false;  // one of them is too wide for direct copies even where it is packed
   double moved = 0.0;
@@ -1372,14 +1383,16 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
     }
   }
   // few rows: the kernel that takes operands of any alignment without a copy (16 threads a column where there are many)
-  if ((epi == kEpiLayer || epi == kEpiXent) && a.i <= kMaxRows && a.j <= kMaxThreads / 16 - 32) {
+  if ((epi == kEpiLayer || epi == kEpiXent || epi == kEpiXentGrad) && a.i <= kMaxRows && a.j <= kMaxThreads / 16 - 32) {
     const double rate = kRowsRate[a.i > 4 ? 3 : a.i > 2 ? 2 : a.i - 1];
     if (kRowsStart + z.bytes / rate <= least) {
+      least = kRowsStart + z.bytes / rate;
       best = LinPlan{};
       best.part[0] = {a.i, kRows, 1};
       best.parts = 1;
     }
   }
+  best.us = least;
   // the parts run one after the other and share the place of their partial sums
   for (int p = 0; p < best.parts; ++p) {
     const LinPart& q = best.part[p];
@@ -1453,7 +1466,7 @@ hipError_t launch_rows(const LinArgs& a, hipStream_t stream) {
     else
       k_linear_rows<T, EPI, 8, jb()><<<grid, block, 0, stream>>>(a);
   };
-  if constexpr (EPI == kEpiXent) {
+  if constexpr (EPI == kEpiXent || EPI == kEpiXentGrad) {
     launch(std::integral_constant<int, 32>());
   } else {
     if (a.codes || a.j >= 32 * kComputeUnits)
@@ -1516,7 +1529,7 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
           e = hipGetLastError();
         }
       }
-      if constexpr (ep() == kEpiLayer || ep() == kEpiXent) {
+      if constexpr (ep() == kEpiLayer || ep() == kEpiXent || ep() == kEpiXentGrad) {
         if (part.form == kRows) e = launch_rows<T, ep()>(a, stream);
       }
       if (part.form == kMiddle) e = launch_group<MiddleShape, T, pt(), qt(), ep()>(a, plan.direct, stream);
@@ -1532,6 +1545,21 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
     });
   }
   return e;
+}
+
+int64_t packed_stride(int64_t run, int dtype) { return packed_ld(run, dtype == 1 ? 2 : 4); }
+
+hipError_t launch_pack(const void* from, int64_t ld, int64_t rows, int64_t run, int dtype, void* to, hipStream_t stream) {
+  const int64_t across = packed_stride(run, dtype) * (dtype == 1 ? 2 : 4) / 16, chunks = rows * across;
+  const int64_t blocks = div_up(chunks, kPackChunks);
+  if (chunks == 0) return hipSuccess;
+  if (blocks > kMaxThreads / 256) return hipErrorInvalidConfiguration;
+  PackJobs jobs{};
+  jobs.job[0] = {from, to, ld, run, across, chunks, 256 / across, 256 % across, (uint32_t)blocks};
+  jobs.count = 1;
+  jobs.blocks = (uint32_t)blocks;
+  with_element(dtype, [&](auto t) { k_pack<decltype(t)><<<dim3(jobs.blocks), dim3(256), 0, stream>>>(jobs); });
+  return hipGetLastError();
 }
 
 hipError_t launch_column_sum(const void* dy, int64_t ld, int64_t rows, int64_t cols, int dtype, void* db,

@@ -521,7 +521,7 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
     }
   }
   if (valid <= 0) return;
-  if constexpr (EPI == kEpiXentGrad) {
+  if constexpr (EPI == kEpiXentGrad) {  // out's rows hold whole eights: zeros past the last column
     const bool outside = s.target < 0 || s.target >= a.classes;
     const float scale = outside ? __builtin_nanf("") : s.scale;
     if (s.target == a.ignore) {
@@ -536,6 +536,12 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
         for (int e = 0; e < 8; ++e) v[e] -= e == at ? scale : 0.f;
       }
     }
+    if (!WHOLE) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = e < valid ? v[e] : 0.f;
+    }
+    El<T>::store8(static_cast<Mem*>(a.out) + i * a.ldout + j0, v);
+    return;
   }
   if constexpr (EPI == kEpiSum) {
     if (a.sum_in) {

@@ -136,10 +136,21 @@ struct Piece {
 };
 Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int64_t p, char* ws) {
   const int64_t bytes = dtype == 1 ? 2 : 4, from = p * plan.width, width = a.n - from < plan.width ? a.n - from : plan.width;
-  const char* w = static_cast<const char*>(a.w) + from * a.ldw * bytes;
+  const int64_t packed = packed_stride(a.k, dtype);
+  const void* w = static_cast<const char*>(a.w) + from * a.ldw * bytes;
+  const void* x = a.x;
+  int64_t ldw = a.ldw, ldx = a.ldx;
+  if (plan.pack & 1) {
+    x = ws + plan.x;
+    ldx = packed;
+  }
+  if (plan.pack & 2) {
+    w = ws + plan.w;
+    ldw = packed;
+  }
   void* dz = ws + plan.dz;
   Piece q{};
-  q.logits.prod[0] = LinProduct{a.x, w, a.ldx, a.ldw, a.k};
+  q.logits.prod[0] = LinProduct{x, w, ldx, ldw, plan.pack == 3 ? packed : a.k};  // both end in zeros
   q.logits.i = a.m;
   q.logits.j = width;
   q.logits.out = dz;
@@ -150,7 +161,7 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
   q.logits.col0 = from;
   q.logits.lse = a.lse;
   q.logits.row_scale = a.row_scale;
-  q.dx.prod[0] = LinProduct{dz, w, plan.width, a.ldw, width};
+  q.dx.prod[0] = LinProduct{dz, w, plan.width, ldw, width, true};
   q.dx.i = a.m;
   q.dx.j = a.k;
   q.dx.out = a.dx;
@@ -161,7 +172,7 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
   q.dx.sum_out = p + 1 < plan.pieces ? sum : nullptr;
   q.dx.scale = a.scale;
   q.dx.totals = a.totals;
-  q.dw.prod[0] = LinProduct{dz, a.x, plan.width, a.ldx, a.m};
+  q.dw.prod[0] = LinProduct{dz, x, plan.width, ldx, a.m};
   q.dw.i = width;
   q.dw.j = a.k;
   q.dw.out = a.dw ? static_cast<char*>(a.dw) + from * a.lddw * bytes : nullptr;
@@ -170,43 +181,86 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
   q.dw.totals = a.totals;
   return q;
 }
+
+bool on_16_bytes(const void* p, int64_t ld, int64_t run, int64_t bytes) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * bytes % 16 == 0 && run * bytes % 16 == 0;
+}
+
+// The products' plans and the workspace where x and W are copied as `pack` says; their estimated microseconds.
+double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
+  const int64_t bytes = dtype == 1 ? 2 : 4;
+  char* base = reinterpret_cast<char*>(uintptr_t(1) << 20);  // a workspace's address, for its alignment
+  double us = 0.0;
+  size_t product = 0;
+  p.dz = p.sum = p.x = p.w = 0;
+  for (int last = 0; last < 2; ++last) {
+    const Piece q = piece_args(a, dtype, p, last ? p.pieces - 1 : 0, base);
+    p.logits[last] = p.dx[last] = p.dw[last] = LinPlan{};
+    if (a.m > 0) p.logits[last] = linear_plan(q.logits, dtype, kEpiXentGrad);
+    if (a.m > 0 && a.k > 0 && a.dx) p.dx[last] = linear_plan(q.dx, dtype, kEpiSum);
+    if (a.k > 0 && a.dw) p.dw[last] = linear_plan(q.dw, dtype, kEpiScaled);
+    double piece = 0.0;
+    for (const LinPlan* l : {&p.logits[last], &p.dx[last], &p.dw[last]}) {
+      if (l->workspace > product) product = l->workspace;
+      piece += l->us;
+    }
+    if (p.pack & 2) piece += pack_us((double)q.logits.j * (double)a.k * (double)bytes);
+    us += piece * (double)(last ? 1 : p.pieces - 1);
+  }
+  if (p.pack & 1) us += pack_us((double)a.m * (double)a.k * (double)bytes);
+  size_t at = round16(product);
+  const auto take = [&](int64_t elements, int64_t size, bool wanted) {
+    const size_t here = at;
+    if (wanted) at += round16((size_t)elements * (size_t)size);
+    return here;
+  };
+  const int64_t packed = packed_stride(a.k, dtype);
+  p.dz = take(a.m * p.width, bytes, true);
+  p.sum = take(a.m * (div_up(a.k, 8) * 8), 4, a.dx && p.pieces > 1);
+  p.x = take(a.m * packed, bytes, p.pack & 1);
+  p.w = take(p.width * packed, bytes, p.pack & 2);
+  p.workspace = at;
+  return us;
+}
 }  // namespace
 
 XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   XentGradPlan p{};
   const int64_t bytes = dtype == 1 ? 2 : 4;
-  if (a.n == 0 || (!a.dx && !a.dw)) return p;
+  if (!a.dx && !a.dw) return p;
   // a piece's dz of up to 128 MB stays in the Infinity Cache between the three products that write and read it
+  // (4096 x 128256 x 2048: 6.61 ms with losses, in pieces of 64 MB 6.81 ms, of 512 MB 6.53 ms, in one of 1.05 GB 6.50 ms)
   constexpr int64_t kPieceBytes = 128ll << 20, kLeast = 1024;
   int64_t most = a.m > 0 ? kPieceBytes / (a.m * bytes) / 256 * 256 : a.n;
   if (most < kLeast) most = kLeast;
   p.pieces = div_up(a.n, most);
   p.width = div_up(div_up(a.n, p.pieces), 256) * 256;
   p.pieces = div_up(a.n, p.width);
-  char* base = reinterpret_cast<char*>(uintptr_t(1) << 20);  // a workspace's address, for its alignment
-  for (int last = 0; last < 2; ++last) {
-    const Piece q = piece_args(a, dtype, p, last ? p.pieces - 1 : 0, base);
-    if (a.m > 0) p.logits[last] = linear_plan(q.logits, dtype, kEpiXentGrad);
-    if (a.m > 0 && a.k > 0 && a.dx) p.dx[last] = linear_plan(q.dx, dtype, kEpiSum);
-    if (a.k > 0 && a.dw) p.dw[last] = linear_plan(q.dw, dtype, kEpiScaled);
-    for (const LinPlan* l : {&p.logits[last], &p.dx[last], &p.dw[last]})
-      if (l->workspace > p.product) p.product = l->workspace;
+  const double us = plan_products(a, dtype, p);
+  // operands off 16-byte rows serve two products each: copies for both, where that is estimated to be faster
+  const bool fits_x = on_16_bytes(a.x, a.ldx, a.k, bytes), fits_w = on_16_bytes(a.w, a.ldw, a.k, bytes);
+  if (a.m > 0 && a.k > 0 && (!fits_x || !fits_w)) {
+    XentGradPlan q = p;
+    q.pack = (fits_x ? 0 : 1) | (fits_w ? 0 : 2);
+    if (plan_products(a, dtype, q) < us) return q;
   }
-  p.dz = round16(p.product);
-  p.sum = p.dz + round16((size_t)a.m * (size_t)p.width * (size_t)bytes);
-  p.workspace = p.sum + (a.dx && p.pieces > 1 ? (size_t)a.m * (size_t)(div_up(a.k, 8) * 8) * 4 : 0);
   return p;
 }
 
 hipError_t launch_xent_grad(const XentGradArgs& a, int dtype, const XentGradPlan& plan, void* workspace, hipStream_t stream) {
   hipError_t e = hipSuccess;
-  for (int64_t p = 0; p < plan.pieces; ++p) {
-    const Piece q = piece_args(a, dtype, plan, p, static_cast<char*>(workspace));
+  char* ws = static_cast<char*>(workspace);
+  if (plan.pack & 1) e = launch_pack(a.x, a.ldx, a.m, a.k, dtype, ws + plan.x, stream);
+  for (int64_t p = 0; p < plan.pieces && e == hipSuccess; ++p) {
+    const Piece q = piece_args(a, dtype, plan, p, ws);
     const int last = p + 1 == plan.pieces;
+    if (plan.pack & 2) {
+      const char* w = static_cast<const char*>(a.w) + p * plan.width * a.ldw * (dtype == 1 ? 2 : 4);
+      if ((e = launch_pack(w, a.ldw, q.logits.j, a.k, dtype, ws + plan.w, stream)) != hipSuccess) break;
+    }
     if (a.m > 0) e = launch_linear(q.logits, dtype, kEpiXentGrad, plan.logits[last], workspace, stream);
     if (e == hipSuccess && a.m > 0 && a.k > 0 && a.dx) e = launch_linear(q.dx, dtype, kEpiSum, plan.dx[last], workspace, stream);
     if (e == hipSuccess && a.k > 0 && a.dw) e = launch_linear(q.dw, dtype, kEpiScaled, plan.dw[last], workspace, stream);
-    if (e != hipSuccess) break;
   }
   return e;
 }
