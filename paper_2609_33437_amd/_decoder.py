@@ -12,7 +12,7 @@ from ctypes import byref
 from ._lib import (SMAT_ERR_DTYPE, SMAT_ERR_INVALID, SMAT_NORM_LAYER, SMAT_NORM_RMS, SmatError, _check, _torch, dtype_code, lib,
                    smat_embed_args, smat_embed_grad_args, smat_linear_xent_args, smat_linear_xent_grad_args, smat_norm_args,
                    smat_norm_grad_args)
-from ._linear import _call, _first, _matrix, _stream_on, _vector
+from ._linear import _call, _first, _matrix, _stream_on
 
 
 def _typed(t, n: int, dtype, device: int, what: str) -> int:
@@ -28,15 +28,31 @@ def _typed(t, n: int, dtype, device: int, what: str) -> int:
     return t.data_ptr()
 
 
-def _like(vectors, n: int, x):
-    """(dtype code, pointers) of the vectors [n] that are given, which share a dtype; x's where there are none."""
-    first = next((t for _, t in vectors if t is not None), None)
-    if first is None:
-        return dtype_code(x), [None] * len(vectors)
-    code = dtype_code(first)
-    if not first.is_cuda or first.get_device() != x.get_device():
-        raise SmatError(SMAT_ERR_INVALID, "weights must be on the same GPU as the call's first matrix")
-    return code, [None if t is None else _vector(t, n, first, what) for what, t in vectors]
+def _weight(t, n: int, device: int, what: str):
+    """(dtype code, pointer) of a contiguous vector [n] of weights on that GPU."""
+    if t.dim() != 1 or t.shape[0] != n:
+        raise SmatError(SMAT_ERR_INVALID, f"{what} has shape {tuple(t.shape)}, expected ({n},)")
+    if t.get_device() != device:
+        raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the same GPU as the call's first matrix")
+    if n > 1 and t.stride(0) != 1:
+        raise SmatError(SMAT_ERR_INVALID, f"{what} must be contiguous")
+    return dtype_code(t), t.data_ptr()
+
+
+def _weights(code: int, n: int, device: int, *named):
+    """(their dtype code, pointers) of the vectors [n] that are given, which share a dtype; `code` where there are none."""
+    first, ptrs = None, []
+    for t, what in named:
+        if t is None:
+            ptrs.append(None)
+            continue
+        c, ptr = _weight(t, n, device, what)
+        if first is None:
+            first = c
+        elif c != first:
+            raise SmatError(SMAT_ERR_DTYPE, f"{what} has dtype {t.dtype}, another one than the weights before it")
+        ptrs.append(ptr)
+    return (code if first is None else first), ptrs
 
 
 # ------------------------------------------------------------------ norms
@@ -48,8 +64,8 @@ def smat_norm(x, y, weight=None, bias=None, kind: int = SMAT_NORM_LAYER, eps: fl
     a = smat_norm_args(dtype=code, kind=int(kind), eps=float(eps), m=m, n=n)
     a.x, a.ldx = _matrix(x, m, n, x, "x")
     a.y, a.ldy = _matrix(y, m, n, x, "y")
-    a.wdtype, (a.weight, a.bias) = _like((("weight", weight), ("bias", bias)), n, x)
     device, f32 = x.get_device(), _torch().float32
+    a.wdtype, (a.weight, a.bias) = _weights(code, n, device, (weight, "weight"), (bias, "bias"))
     if mean is not None:
         a.mean = _typed(mean, m, f32, device, "mean")
     if rstd is not None:
@@ -71,7 +87,7 @@ def smat_norm_grad(dy, x, rstd, weight=None, mean=None, kind: int = SMAT_NORM_LA
         if mean is None:
             raise SmatError(SMAT_ERR_INVALID, "a layer norm's gradients need mean")
         a.mean = _typed(mean, m, f32, device, "mean")
-    a.wdtype, (a.weight, a.dweight, a.dbias) = _like((("weight", weight), ("dw", dw), ("db", db)), n, dy)
+    a.wdtype, (a.weight, a.dweight, a.dbias) = _weights(code, n, device, (weight, "weight"), (dw, "dw"), (db, "db"))
     if dx is not None:
         a.dx, a.lddx = _matrix(dx, m, n, dy, "dx")
     L = lib()
