@@ -114,8 +114,9 @@ struct XentGradArgs {
 struct XentGradPlan {
   int64_t width, pieces;
   int32_t pack;  // bits: x, and each piece of W, are copied to 16-byte rows for all products
+  int32_t some;  // the products take the rows with a target only, in order; x is copied so
   LinPlan logits[2], dx[2], dw[2];  // of a whole piece and of the last one
-  size_t dz, sum, x, w, workspace;  // behind the products' own
+  size_t dz, sum, x, w, rows, workspace;  // behind the products' own
 };
 XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype);
 hipError_t launch_xent_grad(const XentGradArgs& a, int dtype, const XentGradPlan& plan, void* workspace, hipStream_t stream);

@@ -75,6 +75,11 @@ struct LinArgs {
   int64_t ldsum;
   const float* scale;
   const float* totals;
+  // rows that there are of the i (of the r of kEpiScaled) that were planned, in device memory, or NULL: all; row_from: the part's
+  // first; out_rows: where kEpiSum writes them, or NULL: as they are numbered
+  const int32_t* count;
+  const int32_t* out_rows;
+  int64_t row_from;
   // sums of `splits` ranges of r, joined by a second kernel: [splits][i][j rounded up to 8] fp32
   int32_t splits;
   float* partial;

@@ -325,7 +325,8 @@ struct Stream {
 // whole stages are passed by additions alone, since what a stage adds to a wave's instructions delays its matrix
 // instructions; a product's last stage and the end of the share are set up apart.
 // set(product) deals the operands' rows to the copies, end(r) cuts the copies of direct operands to the first r of the stage.
-template <typename T, bool PT, bool QT>
+// ONE: there is no prod[1].
+template <typename T, bool PT, bool QT, bool ONE>
 struct Feed {
   static constexpr int kDeep = 128 / El<T>::kBytes;
   Stream<T, PT, false> p;
@@ -340,22 +341,22 @@ struct Feed {
                                         Set set, End end) {
     i0 = i0_;
     j0 = j0_;
-    second = first >= n0 && a.prod[1].r > 0;
+    second = !ONE && first >= n0 && a.prod[1].r > 0;
     at = (int32_t)(second ? first - n0 : first);
     last_second = (int32_t)(end_ - n0);
     last = second ? last_second : (int32_t)(end_ < n0 ? end_ : n0);
-    set(a.prod[second]);
+    set(a.prod[ONE ? 0 : second]);
     next_run(a, n0, set, end);
   }
   template <typename Set, typename End>
   __device__ __forceinline__ void next_run(const LinArgs& a, int64_t n0, Set set, End end) {
-    if (at >= last && !second && last_second > 0) {
+    if (!ONE && at >= last && !second && last_second > 0) {
       second = 1;
       at = 0;
       last = last_second;
       set(a.prod[1]);
     }
-    const LinProduct& pr = a.prod[second];
+    const LinProduct& pr = a.prod[ONE ? 0 : second];
     p.set(pr, i0, at);
     q.set(pr, j0, at);
     if (at >= last) {  // none is left: what is copied from here on are zeros
@@ -503,18 +504,30 @@ __device__ __forceinline__ void tile_place(uint32_t b, uint32_t ti, uint32_t tj,
   i = band * kHigh + (in - j * high);
 }
 
+// This block's tile; false where there are fewer rows than the launch was made for, and it has none.
+template <int EPI>
+__device__ __forceinline__ bool tile_place(const LinArgs& a, int ki, int kj, uint32_t& i, uint32_t& j) {
+  const uint32_t ti = (uint32_t)((a.i + ki - 1) / ki), tj = (uint32_t)((a.j + kj - 1) / kj);
+  if constexpr (EPI == kEpiXentGrad || EPI == kEpiSum) {
+    if (blockIdx.x >= ti * tj) return false;
+  }
+  tile_place(blockIdx.x, ti, tj, i, j);
+  return true;
+}
+
 template <bool PT, bool QT, int EPI>
 __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   using T = Bf16;
   extern __shared__ char smem[];  // [stage parity][P half 0, P half 1, Q half 0, Q half 1]
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
   uint32_t ti, tj;
-  tile_place(blockIdx.x, (uint32_t)((a.i + kFastB - 1) / kFastB), (uint32_t)((a.j + kFastB - 1) / kFastB), ti, tj);
+  if (without_rows<EPI>(a)) return;
+  if (!tile_place<EPI>(a, kFastB, kFastB, ti, tj)) return;
   const int64_t i0 = (int64_t)ti * kFastB, j0 = (int64_t)tj * kFastB;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
   const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
-  Feed<T, PT, QT> feed;
+  Feed<T, PT, QT, kOneProduct<EPI>> feed;
   Copy<T, PT, false, kFastHalf, 2> cp[2];
   Copy<T, QT, true, kFastHalf, 2> cq[2];
   const auto set = [&](const LinProduct& pr) {
@@ -652,7 +665,8 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   extern __shared__ char smem[];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), group = wave / kWaves, w = wave % kWaves;
   uint32_t ti, tj;
-  tile_place(blockIdx.x, (uint32_t)((a.i + S::kI - 1) / S::kI), (uint32_t)((a.j + S::kJ - 1) / S::kJ), ti, tj);
+  if (without_rows<EPI>(a)) return;
+  if (!tile_place<EPI>(a, S::kI, S::kJ, ti, tj)) return;
   const int64_t i0 = (int64_t)ti * S::kI, j0 = (int64_t)tj * S::kJ;
   const int wi = w / S::WJ * S::TI, wj = w % S::WJ * S::TJ;
   const int64_t n0 = (a.prod[0].r + kDeep - 1) / kDeep, n = n0 + (a.prod[1].r + kDeep - 1) / kDeep;
@@ -660,7 +674,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   const int64_t first = split_start(n, share, a.splits * S::G), last = split_start(n, share + 1, a.splits * S::G);
   // every group of a block takes the same number of steps, so that barriers meet (shares differ by one stage)
   const int64_t steps = (n + a.splits * S::G - 1) / (a.splits * S::G);
-  Feed<T, PT, QT> feed;
+  Feed<T, PT, QT, kOneProduct<EPI>> feed;
   Copy<T, PT, false, S::kI, kNp> cp;
   Copy<T, QT, true, S::kJ, kNq> cq;
   Staged<T, PT, false, S::kI, kNp> rp;
@@ -676,7 +690,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   // by way of registers: the next stage's number, and of its product
   int64_t at = first;
   const auto stage_of = [&] {
-    const bool second = at >= n0 && a.prod[1].r > 0;
+    const bool second = !kOneProduct<EPI> && at >= n0 && a.prod[1].r > 0;
     rp.set(a.prod[second], i0, a.i, (second ? at - n0 : at) * kDeep, w);
     rq.set(a.prod[second], j0, a.j, (second ? at - n0 : at) * kDeep, w);
   };
@@ -895,6 +909,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
   constexpr int kChunk = 16 / El<T>::kBytes, kGroups = kRowsWaves * kRowsEach / JB, kValues = kRowsEach * M;
   constexpr int kStep = 64 * kChunk, kAhead = M <= 2 ? 4 : 2;
   __shared__ float sums[kGroups][M][JB + 4];
+  if (without_rows<EPI>(a)) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   const int group = wave % kGroups, jrow = wave / kGroups * kRowsEach;
   const int64_t j0 = (int64_t)blockIdx.x * JB, r = a.prod[0].r;
@@ -992,6 +1007,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
 // 4096 x 2048 take 14 us, 6.2 TB/s.
 template <typename T, int EPI>
 __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
+  if (without_rows<EPI>(a)) return;
   const int64_t eights = ((a.j + kCkptBlock - 1) / kCkptBlock) * 4, ld = (a.j + 7) & ~(int64_t)7;
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t i = t / eights, j = (t - i * eights) * 8;
@@ -1433,7 +1449,9 @@ LinArgs rows_of(LinArgs a, int64_t from, int64_t rows, int bytes, bool pt) {
   for (LinProduct& pr : a.prod)
     if (pr.r > 0) pr.p = skip_bytes(pr.p, (pt ? from : from * pr.ldp) * bytes);
   a.i = rows;
-  a.out = skip_bytes(a.out, from * a.ldout * bytes);
+  if (!a.out_rows) a.out = skip_bytes(a.out, from * a.ldout * bytes);
+  a.out_rows = static_cast<const int32_t*>(skip_bytes(a.out_rows, from * 4));
+  a.row_from = from;
   a.mul = skip_bytes(a.mul, from * a.ldmul * bytes);
   a.residual = skip_bytes(a.residual, from * a.ldres * bytes);
   a.out_up = skip_bytes(a.out_up, from * a.ldup * bytes);

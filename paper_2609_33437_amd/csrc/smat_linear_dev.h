@@ -351,6 +351,7 @@ struct Side<T, kEpiXentGrad> {
 template <typename T>
 struct Side<T, kEpiSum> {
   Raw8<float> sum;
+  int64_t row;  // of out
 };
 template <typename T>
 struct ColumnSide<T, kEpiSum> {
@@ -360,6 +361,25 @@ template <typename T>
 struct ColumnSide<T, kEpiScaled> {
   float scale;
 };
+
+// Products of which only some rows are there (LinArgs::count): sets their number, and says whether there are none.
+template <int EPI>
+__device__ __forceinline__ bool without_rows(LinArgs& a) {
+  if constexpr (EPI == kEpiXentGrad || EPI == kEpiSum || EPI == kEpiScaled) {
+    if (a.count) {
+      const int64_t rows = *a.count;
+      if (EPI == kEpiScaled) {
+        if (rows < a.prod[0].r) a.prod[0].r = rows;
+      } else {
+        if (rows - a.row_from < a.i) a.i = rows - a.row_from;
+        return a.i <= 0;
+      }
+    }
+  }
+  return false;
+}
+template <int EPI>
+constexpr bool kOneProduct = EPI == kEpiXent || EPI == kEpiXentGrad || EPI == kEpiSum || EPI == kEpiScaled;
 
 // scale[0] / totals[1]; 0 where no row counts.
 __device__ __forceinline__ float total_scale(const LinArgs& a) {
@@ -409,7 +429,10 @@ __device__ __forceinline__ void side_load(const LinArgs& a, int64_t i, int64_t j
     }
   }
   if constexpr (EPI == kEpiSum) {
-    if (a.sum_in && (WHOLE || (i < a.i && j0 < a.j))) s.sum.load(a.sum_in + i * a.ldsum + j0);  // rows of whole eights
+    if (WHOLE || (i < a.i && j0 < a.j)) {
+      if (a.sum_in) s.sum.load(a.sum_in + i * a.ldsum + j0);  // rows of whole eights
+      s.row = a.out_rows ? a.out_rows[i] : i;
+    }
   }
 }
 
@@ -559,6 +582,7 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= c.scale;
   }
+  if constexpr (EPI == kEpiSum) i = s.row;
   if constexpr (EPI == kEpiDgrad) {
     if (a.z_codes) {
       float z[8];

@@ -164,6 +164,34 @@ def test_vocabulary_in_pieces(dtype, m, n, k):
     check_gradients(x, w, t, dtype, z, e_z, lse, totals=tot)
 
 
+@pytest.mark.parametrize("dtype,m,n,k,pad,shift", [("bf16", 4096, 40000, 1024, 0, 0), ("bf16", 3001, 50257, 768, 8, 0),
+                                                   ("bf16", 2500, 40001, 1025, 1, 3), ("f32", 1500, 16000, 768, 0, 0),
+                                                   ("f32", 1030, 20001, 770, 1, 1)])
+@pytest.mark.parametrize("ignored", [0.0, 0.6, 0.999, 1.0])
+def test_large_batches_take_their_rows_with_a_target(dtype, m, n, k, pad, shift, ignored):
+    """Where the products are long the gradient's take the rows with a target alone: none left out, a part, a handful, none."""
+    x, w, t = make(m, n, k, dtype, pad, shift, ignored)
+    if ignored == 1.0:
+        t.fill_(IGNORE)
+    elif ignored:
+        t[:300] = IGNORE        # whole tiles of them
+        t[-300:] = IGNORE
+        t[301] = 5
+    z, e_z, _, lse, tot = check_forward(x, w, t)
+    check_gradients(x, w, t, dtype, z, e_z, lse, totals=tot if ignored < 1.0 else None, pad=pad, shift=shift)
+    weights = torch.randn(m, generator=torch.Generator(DEV).manual_seed(5), device=DEV)
+    dx, dw = check_gradients(x, w, t, dtype, z, e_z, lse, row_scale=weights)
+    if ignored == 1.0:
+        assert not dw.any()
+    # one gradient at a time
+    only = torch.full_like(dx, float("nan"))
+    smat.smat_linear_xent_grad(x, w, t, lse, dx=only, row_scale=weights, ignore_index=IGNORE)
+    assert torch.equal(only, dx)
+    only = torch.full_like(dw, float("nan"))
+    smat.smat_linear_xent_grad(x, w, t, lse, dw=only, row_scale=weights, ignore_index=IGNORE)
+    assert torch.equal(only, dw)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_each_gradient_alone_and_repeated(dtype):
     x, w, t = make(1200, 3000, 96, dtype)
