@@ -736,8 +736,8 @@ typedef struct smat_embed_grad_args {
   int64_t ldtable;
 } smat_embed_grad_args;
 
-/* smat_embed_grad -- the gradient of a table.  Tokens are sorted by id and a row's summed in fp32 in their order, in runs of
- * at least 32 whose sums are then added.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
+/* smat_embed_grad -- the gradient of a table.  Tokens are taken by id, and a row's summed in fp32 in their order (with many
+ * tokens in runs whose sums are then added, in order).  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE, SMAT_ERR_HIP. */
 smat_status smat_embed_grad_workspace_bytes(const smat_embed_grad_args* args, size_t* bytes);
 smat_status smat_embed_grad(const smat_embed_grad_args* args, void* workspace, size_t workspace_bytes, hipStream_t stream);
 

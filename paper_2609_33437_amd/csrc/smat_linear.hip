@@ -325,9 +325,9 @@ struct Stream {
 // whole stages are passed by additions alone, since what a stage adds to a wave's instructions delays its matrix
 // instructions; a product's last stage and the end of the share are set up apart.
 // set(product) deals the operands' rows to the copies, end(r) cuts the copies of direct operands to the first r of the stage.
-// ONE: there is no prod[1].
-template <typename T, bool PT, bool QT, bool ONE>
+template <typename T, bool PT, bool QT, int EPI>
 struct Feed {
+  static constexpr bool ONE = kOneProduct<EPI>;
   static constexpr int kDeep = 128 / El<T>::kBytes;
   Stream<T, PT, false> p;
   Stream<T, QT, true> q;
@@ -345,7 +345,7 @@ struct Feed {
     at = (int32_t)(second ? first - n0 : first);
     last_second = (int32_t)(end_ - n0);
     last = second ? last_second : (int32_t)(end_ < n0 ? end_ : n0);
-    set(a.prod[ONE ? 0 : second]);
+    set(product_of<EPI>(a, second));
     next_run(a, n0, set, end);
   }
   template <typename Set, typename End>
@@ -354,9 +354,9 @@ struct Feed {
       second = 1;
       at = 0;
       last = last_second;
-      set(a.prod[1]);
+      set(product_of<EPI>(a, 1));
     }
-    const LinProduct& pr = a.prod[ONE ? 0 : second];
+    const LinProduct& pr = product_of<EPI>(a, second);
     p.set(pr, i0, at);
     q.set(pr, j0, at);
     if (at >= last) {  // none is left: what is copied from here on are zeros
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
   const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
-  Feed<T, PT, QT, kOneProduct<EPI>> feed;
+  Feed<T, PT, QT, EPI> feed;
   Copy<T, PT, false, kFastHalf, 2> cp[2];
   Copy<T, QT, true, kFastHalf, 2> cq[2];
   const auto set = [&](const LinProduct& pr) {
@@ -674,7 +674,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   const int64_t first = split_start(n, share, a.splits * S::G), last = split_start(n, share + 1, a.splits * S::G);
   // every group of a block takes the same number of steps, so that barriers meet (shares differ by one stage)
   const int64_t steps = (n + a.splits * S::G - 1) / (a.splits * S::G);
-  Feed<T, PT, QT, kOneProduct<EPI>> feed;
+  Feed<T, PT, QT, EPI> feed;
   Copy<T, PT, false, S::kI, kNp> cp;
   Copy<T, QT, true, S::kJ, kNq> cq;
   Staged<T, PT, false, S::kI, kNp> rp;
@@ -691,8 +691,8 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   int64_t at = first;
   const auto stage_of = [&] {
     const bool second = !kOneProduct<EPI> && at >= n0 && a.prod[1].r > 0;
-    rp.set(a.prod[second], i0, a.i, (second ? at - n0 : at) * kDeep, w);
-    rq.set(a.prod[second], j0, a.j, (second ? at - n0 : at) * kDeep, w);
+    rp.set(product_of<EPI>(a, second), i0, a.i, (second ? at - n0 : at) * kDeep, w);
+    rq.set(product_of<EPI>(a, second), j0, a.j, (second ? at - n0 : at) * kDeep, w);
   };
   if constexpr (DIRECT)
     feed.begin(a, i0, j0, first, last, n0, set, end);
@@ -1406,6 +1406,7 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       best = LinPlan{};
       best.part[0] = {a.i, kRows, 1};
       best.parts = 1;
+      best.direct = 1;  // it has no stages that pass registers
     }
   }
   best.us = least;
@@ -1450,6 +1451,7 @@ LinArgs rows_of(LinArgs a, int64_t from, int64_t rows, int bytes, bool pt) {
     if (pr.r > 0) pr.p = skip_bytes(pr.p, (pt ? from : from * pr.ldp) * bytes);
   a.i = rows;
   if (!a.out_rows) a.out = skip_bytes(a.out, from * a.ldout * bytes);
+  a.out_low = skip_bytes(a.out_low, from * a.ldout * bytes);
   a.out_rows = static_cast<const int32_t*>(skip_bytes(a.out_rows, from * 4));
   a.row_from = from;
   a.mul = skip_bytes(a.mul, from * a.ldmul * bytes);

@@ -378,8 +378,19 @@ __device__ __forceinline__ bool without_rows(LinArgs& a) {
   }
   return false;
 }
+// The products that an epilogue's launches sum, by number.  Where without_rows changes one they are chosen between, not
+// indexed, so that the arguments stay where they are passed.
 template <int EPI>
-constexpr bool kOneProduct = EPI == kEpiXent || EPI == kEpiXentGrad || EPI == kEpiSum || EPI == kEpiScaled;
+constexpr bool kOneProduct = EPI == kEpiXent || EPI == kEpiXentGrad;
+template <int EPI>
+__device__ __forceinline__ decltype(auto) product_of(const LinArgs& a, int32_t second) {
+  if constexpr (kOneProduct<EPI>)
+    return (a.prod[0]);
+  else if constexpr (EPI == kEpiSum || EPI == kEpiScaled)
+    return second ? LinProduct(a.prod[1]) : LinProduct(a.prod[0]);
+  else
+    return (a.prod[second]);
+}
 
 // scale[0] / totals[1]; 0 where no row counts.
 __device__ __forceinline__ float total_scale(const LinArgs& a) {
@@ -564,6 +575,13 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
       for (int e = 0; e < 8; ++e) v[e] = e < valid ? v[e] : 0.f;
     }
     El<T>::store8(static_cast<Mem*>(a.out) + i * a.ldout + j0, v);
+    if constexpr (El<T>::kBytes == 2) {
+      if (a.out_low) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] -= bf16_to_f32(to_bf16(v[e]));
+        El<T>::store8(static_cast<Mem*>(a.out_low) + i * a.ldout + j0, v);
+      }
+    }
     return;
   }
   if constexpr (EPI == kEpiSum) {

@@ -226,13 +226,14 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
     w = ws + plan.w;
     ldw = packed;
   }
-  void* dz = ws + plan.dz;
+  char *dz = ws + plan.dz, *low = plan.low ? dz + a.m * plan.width * bytes : nullptr;
   Piece q{};
   q.logits.prod[0] = LinProduct{x, w, ldx, ldw, plan.pack == 3 ? packed : a.k};  // both end in zeros
   q.logits.i = a.m;
   q.logits.j = width;
   q.logits.out = dz;
   q.logits.ldout = plan.width;
+  q.logits.out_low = low;
   q.logits.targets = a.targets;
   q.logits.ignore = a.ignore;
   q.logits.classes = a.n;
@@ -240,6 +241,7 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
   q.logits.lse = a.lse;
   q.logits.row_scale = a.row_scale;
   q.dx.prod[0] = LinProduct{dz, w, plan.width, ldw, width, true};
+  if (low) q.dx.prod[1] = LinProduct{low, w, plan.width, ldw, width, true};
   q.dx.i = a.m;
   q.dx.j = a.k;
   q.dx.out = a.dx;
@@ -259,6 +261,7 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
     q.logits.count = q.dx.count = q.dw.count = r.count;
   }
   q.dw.prod[0] = LinProduct{dz, x, plan.width, ldx, a.m};
+  if (low) q.dw.prod[1] = LinProduct{low, x, plan.width, ldx, a.m};
   q.dw.i = width;
   q.dw.j = a.k;
   q.dw.out = a.dw ? static_cast<char*>(a.dw) + from * a.lddw * bytes : nullptr;
@@ -271,6 +274,8 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
 bool on_16_bytes(const void* p, int64_t ld, int64_t run, int64_t bytes) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * bytes % 16 == 0 && run * bytes % 16 == 0;
 }
+
+constexpr int64_t kLowRows = 128;
 
 // The products' plans and the workspace where x and W are copied as `pack` says; their estimated microseconds.
 double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
@@ -288,7 +293,9 @@ double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
     double piece = 0.0;
     for (const LinPlan* l : {&p.logits[last], &p.dx[last], &p.dw[last]}) {
       if (l->workspace > product) product = l->workspace;
-      piece += l->us;
+      // stages by way of registers take 1.5 times their estimate in bf16 where rows of W are far from whole cache lines (160 x
+      // 62106 x 2982: 190 us)
+      piece += l->us * (dtype == 1 && l->parts && !l->direct ? 1.5 : 1.0);
     }
     if (p.pack & 2) piece += pack_us((double)q.logits.j * (double)a.k * (double)bytes);
     us += piece * (double)(last ? 1 : p.pieces - 1);
@@ -301,7 +308,7 @@ double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
     return here;
   };
   const int64_t packed = packed_stride(a.k, dtype);
-  p.dz = take(a.m * p.width, bytes, true);
+  p.dz = take(a.m * p.width * (p.low ? 2 : 1), bytes, true);
   p.sum = take(a.m * (div_up(a.k, 8) * 8), 4, a.dx && p.pieces > 1);
   p.x = take(a.m * packed, bytes, p.pack & 1);
   p.w = take(p.width * packed, bytes, p.pack & 2);
@@ -315,6 +322,9 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   XentGradPlan p{};
   const int64_t bytes = dtype == 1 ? 2 : 4;
   if (!a.dx && !a.dw) return p;
+  // With few rows a rounding of dz is not averaged out in dx and dW, and W's and dW's bytes bound the products: both halves of
+  // dz are multiplied.
+  p.low = dtype == 1 && a.m <= kLowRows;
   // a piece's dz of up to 128 MB stays in the Infinity Cache between the three products that write and read it
   // (4096 x 128256 x 2048: 6.61 ms with losses, in pieces of 64 MB 6.81 ms, of 512 MB 6.53 ms, in one of 1.05 GB 6.50 ms)
   constexpr int64_t kPieceBytes = 128ll << 20, kLeast = 1024;
@@ -344,7 +354,7 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   // fiftieth of the call or less.  (2048 x 128256 x 4096, half of the rows without: losses and gradients 4.75 ms, 6.15 ms with
   // products over all rows.)
   const double some = 10.0 + pack_us((double)a.m * (double)a.k * (double)bytes);
-  if (a.k > 0 && us > 50.0 * some) {
+  if (a.k > 0 && !p.low && us > 50.0 * some) {
     p.some = 1;
     p.pack |= 1;
   }

@@ -72,7 +72,7 @@ def ids_of(kind, m, rows, gen):
 
 
 # from one token to several tiles of the sort, chunk ends inside and between runs, vocabularies of one to four digits
-GRADS = [(1, 1, 1, "one"), (1, 50, 40, "any"), (31, 7, 9, "any"), (32, 5, 8, "one"), (33, 5, 8, "one"), (64, 2, 65, "any"),
+GRADS = [(255, 40, 600, "skew"), (256, 300, 9, "outside"), (60, 64, 1300, "all"), (64, 9, 40, "any"), (65, 9, 3, "one"), (1, 1, 1, "one"), (1, 50, 40, "any"), (31, 7, 9, "any"), (32, 5, 8, "one"), (33, 5, 8, "one"), (64, 2, 65, "any"),
          (100, 100, 513, "all"), (1000, 37, 1025, "skew"), (257, 300, 2048, "any"), (4096, 1000, 64, "skew"),
          (4097, 255, 31, "any"), (4097, 256, 31, "any"), (5000, 257, 17, "outside"), (8192, 70000, 8, "skew"),
          (20000, 3, 24, "any"), (40000, 65535, 5, "any"), (40000, 65536, 5, "skew"), (70001, 131072, 3, "skew"),
