@@ -106,81 +106,7 @@ __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* waves, ui
   return before + sum - v;
 }
 
-struct SortPass {
-  const uint32_t* keys;    // NULL: the first pass, from the ids
-  const uint32_t* places;
-  uint32_t* keys_to;
-  uint32_t* places_to;
-  uint32_t* counts;        // [digits][tiles]
-  int64_t tiles;
-  int32_t shift, bits;
-};
-
-__global__ __launch_bounds__(kSortThreads) void k_sort_count(EmbedGradArgs a, SortPass s) {
-  __shared__ uint32_t count[kMaxDigits];
-  const uint32_t digits = 1u << s.bits;
-  if (threadIdx.x < kMaxDigits) count[threadIdx.x] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int r = 0; r < kTileRounds; ++r) {
-    const int64_t i = (int64_t)blockIdx.x * kSortTile + r * kSortThreads + threadIdx.x;
-    if (i < a.m) atomicAdd(&count[((s.keys ? s.keys[i] : token_key(a, i)) >> s.shift) & (digits - 1)], 1u);
-  }
-  __syncthreads();
-  if (threadIdx.x < digits) s.counts[(int64_t)threadIdx.x * s.tiles + blockIdx.x] = count[threadIdx.x];
-}
-
-// counts <- their exclusive sums, by one block.
-__global__ __launch_bounds__(kSortThreads) void k_sort_sum(uint32_t* counts, int64_t n) {
-  __shared__ uint32_t waves[kSortWaves];
-  uint32_t before = 0;
-  for (int64_t i0 = 0; i0 < n; i0 += kSortThreads) {
-    const int64_t i = i0 + threadIdx.x;
-    uint32_t total;
-    const uint32_t v = i < n ? counts[i] : 0u, at = block_before(v, waves, &total);
-    if (i < n) counts[i] = before + at;
-    before += total;
-  }
-}
-
-// Wave w of a block takes its tokens [w 64 kTileRounds, ..): the order within a digit is the tokens'.
-__global__ __launch_bounds__(kSortThreads) void k_sort_place(EmbedGradArgs a, SortPass s) {
-  __shared__ uint32_t count[kSortWaves][kMaxDigits];
-  const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
-  const uint32_t digits = 1u << s.bits;
-  for (int k = (int)threadIdx.x; k < kSortWaves * kMaxDigits; k += kSortThreads) count[k / kMaxDigits][k % kMaxDigits] = 0;
-  __syncthreads();
-  uint32_t key[kTileRounds], place[kTileRounds], at[kTileRounds];
-  const int64_t first = (int64_t)blockIdx.x * kSortTile + wave * 64 * kTileRounds + lane;
-#pragma unroll
-  for (int r = 0; r < kTileRounds; ++r) {
-    const int64_t i = first + r * 64;
-    const bool on = i < a.m;
-    key[r] = on ? (s.keys ? s.keys[i] : token_key(a, i)) : 0u;
-    place[r] = on ? (s.keys ? s.places[i] : (uint32_t)i) : 0u;
-    at[r] = wave_place((key[r] >> s.shift) & (digits - 1), s.bits, on, count[wave]);
-  }
-  __syncthreads();
-  if (threadIdx.x < digits) {
-    uint32_t before = s.counts[(int64_t)threadIdx.x * s.tiles + blockIdx.x];
-    for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t c = count[w][threadIdx.x];
-      count[w][threadIdx.x] = before;
-      before += c;
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int r = 0; r < kTileRounds; ++r) {
-    if (first + r * 64 < a.m) {
-      const uint32_t to = count[wave][(key[r] >> s.shift) & (digits - 1)] + at[r];
-      s.keys_to[to] = key[r];
-      s.places_to[to] = place[r];
-    }
-  }
-}
-
-// ---------------------------------------------------------------- clearing, and the sort of few tokens beside it
+// ---------------------------------------------------------------- clearing
 // A block of kSortThreads clears kClearEights eights a thread that follow each other over the block.  Rows end to end are
 // one row, whose whole 16 bytes are written at their addresses.
 constexpr int kClearEights = 8;
@@ -217,6 +143,107 @@ __device__ __forceinline__ void clear_block(const ClearArgs& c, int64_t block) {
   }
 }
 
+// ---------------------------------------------------------------- the sort of many tokens
+// A pass counts a digit of each tile's tokens, adds the counts up, and places the tokens.  Blocks of the first pass's count clear
+// the gradient meanwhile.
+struct SortPass {
+  const uint32_t* keys;    // NULL: the first pass, from the ids
+  const uint32_t* places;
+  uint32_t* keys_to;
+  uint32_t* places_to;
+  uint32_t* counts;        // [digits][tiles]
+  int64_t tiles;
+  int32_t shift, bits, summed;
+};
+constexpr int64_t kAddedTiles = 64;  // up to so many tiles' counts are added up by each placing block: a launch less a pass
+
+template <typename U>
+__global__ __launch_bounds__(kSortThreads) void k_sort_count(EmbedGradArgs a, SortPass s, ClearArgs c) {
+  __shared__ uint32_t count[kMaxDigits];
+  if (wide_block() >= s.tiles) {
+    clear_block<U>(c, wide_block() - s.tiles);
+    return;
+  }
+  const uint32_t digits = 1u << s.bits;
+  if (threadIdx.x < kMaxDigits) count[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kTileRounds; ++r) {
+    const int64_t i = (int64_t)blockIdx.x * kSortTile + r * kSortThreads + threadIdx.x;
+    if (i < a.m) atomicAdd(&count[((s.keys ? s.keys[i] : token_key(a, i)) >> s.shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  if (threadIdx.x < digits) s.counts[(int64_t)threadIdx.x * s.tiles + blockIdx.x] = count[threadIdx.x];
+}
+
+// counts <- their exclusive sums, by one block, where the tiles are too many for each block to add them up itself.
+__global__ __launch_bounds__(kSortThreads) void k_sort_sum(uint32_t* counts, int64_t n) {
+  __shared__ uint32_t waves[kSortWaves];
+  uint32_t before = 0;
+  for (int64_t i0 = 0; i0 < n; i0 += kSortThreads) {
+    const int64_t i = i0 + threadIdx.x;
+    uint32_t total;
+    const uint32_t v = i < n ? counts[i] : 0u, at = block_before(v, waves, &total);
+    if (i < n) counts[i] = before + at;
+    before += total;
+  }
+}
+
+// Wave w of a block takes its tokens [w 64 kTileRounds, ..): the order within a digit is the tokens'.
+__global__ __launch_bounds__(kSortThreads) void k_sort_place(EmbedGradArgs a, SortPass s) {
+  __shared__ uint32_t count[kSortWaves][kMaxDigits];
+  __shared__ uint32_t waves[kSortWaves];
+  const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
+  const uint32_t digits = 1u << s.bits;
+  for (int k = (int)threadIdx.x; k < kSortWaves * kMaxDigits; k += kSortThreads) count[k / kMaxDigits][k % kMaxDigits] = 0;
+  __syncthreads();
+  uint32_t key[kTileRounds], place[kTileRounds], at[kTileRounds];
+  const int64_t first = (int64_t)blockIdx.x * kSortTile + wave * 64 * kTileRounds + lane;
+#pragma unroll
+  for (int r = 0; r < kTileRounds; ++r) {
+    const int64_t i = first + r * 64;
+    const bool on = i < a.m;
+    key[r] = on ? (s.keys ? s.keys[i] : token_key(a, i)) : 0u;
+    place[r] = on ? (s.keys ? s.places[i] : (uint32_t)i) : 0u;
+    at[r] = wave_place((key[r] >> s.shift) & (digits - 1), s.bits, on, count[wave]);
+  }
+  // a digit's first place: after all lower digits, and the digit's in earlier tiles
+  uint32_t place0 = 0, total;
+  if (s.summed) {
+    if (threadIdx.x < digits) place0 = s.counts[(int64_t)threadIdx.x * s.tiles + blockIdx.x];
+    __syncthreads();
+  } else {
+    uint32_t all = 0;
+    if (threadIdx.x < digits) {
+      for (int64_t k = 0; k < s.tiles; ++k) {
+        const uint32_t c = s.counts[(int64_t)threadIdx.x * s.tiles + k];
+        place0 += k < blockIdx.x ? c : 0u;
+        all += c;
+      }
+    }
+    place0 += block_before(all, waves, &total);
+  }
+  if (threadIdx.x < digits) {
+    uint32_t before = place0;
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = count[w][threadIdx.x];
+      count[w][threadIdx.x] = before;
+      before += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kTileRounds; ++r) {
+    if (first + r * 64 < a.m) {
+      const uint32_t to = count[wave][(key[r] >> s.shift) & (digits - 1)] + at[r];
+      s.keys_to[to] = key[r];
+      s.places_to[to] = place[r];
+    }
+  }
+}
+
+// ---------------------------------------------------------------- the sort of few tokens
+// A gradient of no tokens.
 template <typename U>
 __global__ __launch_bounds__(kSortThreads) void k_embed_clear(ClearArgs c) {
   clear_block<U>(c, wide_block());
@@ -531,7 +558,7 @@ EmbedGradPlan embed_grad_plan(const EmbedGradArgs& a) {
   if (a.m <= kFewTokens || a.d == 0 || a.rows == 0) return p;
   // few tokens a wave where they are few; with many, as many chunks as keep the join's sums short
   p.chunk = 8;
-  while (p.chunk * 1024 < a.m) p.chunk *= 2;
+  while (p.chunk * 2048 < a.m) p.chunk *= 2;
   p.chunks = div_up(a.m, p.chunk);
   while ((a.rows >> p.bits) > 0) ++p.bits;
   p.passes = (p.bits + 7) / 8;
@@ -558,7 +585,7 @@ hipError_t launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype,
   const int64_t across = div_up(a.d, 8);
   char* ws = static_cast<char*>(workspace);
   const auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
-  SortPass s{nullptr, nullptr, nullptr, nullptr, words(plan.counts), plan.tiles, 0, 0};
+  SortPass s{nullptr, nullptr, nullptr, nullptr, words(plan.counts), plan.tiles, 0, 0, plan.tiles > kAddedTiles};
   if (a.m > 0 && a.m <= kFewTokens) {
     const int64_t tiles = div_up(across, 64), sums = div_up(a.m * tiles, 4);
     const int64_t clears = a.accumulate ? 0 : div_up(a.rows, 4 * kClearRows);
@@ -596,7 +623,7 @@ hipError_t launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype,
     });
     s.keys = o.keys;
     s.places = o.places;
-  } else if (clears > 0) {
+  } else if (a.m == 0 && clears > 0) {
     with_element(table_dtype, [&](auto u) {
       k_embed_clear<decltype(u)><<<wide_grid(clears), dim3(kSortThreads), 0, stream>>>(c);
     });
@@ -608,8 +635,10 @@ hipError_t launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype,
     s.keys_to = words(plan.keys[p % 2]);
     s.places_to = words(plan.places[p % 2]);
     const dim3 grid((uint32_t)plan.tiles), block(kSortThreads);
-    k_sort_count<<<grid, block, 0, stream>>>(a, s);
-    k_sort_sum<<<dim3(1), block, 0, stream>>>(s.counts, plan.tiles << s.bits);
+    with_element(table_dtype, [&](auto u) {
+      k_sort_count<decltype(u)><<<wide_grid(plan.tiles + (p == 0 ? clears : 0)), block, 0, stream>>>(a, s, c);
+    });
+    if (s.summed) k_sort_sum<<<dim3(1), block, 0, stream>>>(s.counts, plan.tiles << s.bits);
     k_sort_place<<<grid, block, 0, stream>>>(a, s);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     s.shift += s.bits;

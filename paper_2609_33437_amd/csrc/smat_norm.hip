@@ -405,7 +405,7 @@ void with_shape(int64_t n, F&& fn) {
   else if (n <= 4096)
     fn(RowShape<256, 2>());
   else if (n <= 8192)
-    fn(RowShape<1024, 1>());
+    fn(RowShape<512, 2>());
   else
     fn(RowShape<1024, 2, false>());
 }

@@ -76,7 +76,7 @@ GRADS = [(255, 40, 600, "skew"), (256, 300, 9, "outside"), (60, 64, 1300, "all")
          (100, 100, 513, "all"), (1000, 37, 1025, "skew"), (257, 300, 2048, "any"), (4096, 1000, 64, "skew"),
          (4097, 255, 31, "any"), (4097, 256, 31, "any"), (5000, 257, 17, "outside"), (8192, 70000, 8, "skew"),
          (20000, 3, 24, "any"), (40000, 65535, 5, "any"), (40000, 65536, 5, "skew"), (70001, 131072, 3, "skew"),
-         (33000, 20000000, 2, "any"), (130000, 11, 12, "one")]
+         (33000, 20000000, 2, "any"), (130000, 11, 12, "one"), (300000, 70000, 2, "any")]
 
 
 @pytest.mark.parametrize("dtype,tdtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
