@@ -768,7 +768,8 @@ smat_status smat_linear_xent(const smat_linear_xent_args* args, void* workspace,
 /* Arguments of smat_linear_xent_grad: the gradients of s * sum_i row_scale[i] loss[i],
  *   dz[i][j] = (exp(z[i][j] - lse[i]) - [j = targets[i]]) row_scale[i]      0 in rows without a target
  *   dx = s dz W,  dW = s dz^T x,  s = scale[0] / totals[1]
- * The vocabulary is taken in pieces: z is computed again and dz, rounded to dtype, held for one piece (in the workspace), so
+ * Rows without a target take no part, whatever x, lse and row_scale hold in them, and their rows of dx are zeros.  The
+ * vocabulary is taken in pieces: z is computed again and dz, rounded to dtype, held for one piece (in the workspace), so
  * nothing of the size m * n is stored.  s multiplies the fp32 sums; it is 0 where totals[1] is. */
 typedef struct smat_linear_xent_grad_args {
   int32_t dtype, reserved; /* smat_dtype of x, w, dx and dw; reserved must be 0 */

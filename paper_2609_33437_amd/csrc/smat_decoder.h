@@ -113,7 +113,7 @@ struct XentGradArgs {
 // Pieces of `width` columns of the vocabulary, the last one narrower: how each piece's products are computed.
 struct XentGradPlan {
   int64_t width, pieces;
-  int32_t pack;  // bits: x, and each piece of W, are copied to 16-byte rows for all products
+  int32_t pack;  // each piece of W is copied to 16-byte rows for its products; x always is
   int32_t low;   // what rounding dz to bf16 leaves is kept too, behind dz, and multiplied
   int32_t some;  // the products take the rows with a target only, in order; x is copied so
   LinPlan logits[2], dx[2], dw[2];  // of a whole piece and of the last one

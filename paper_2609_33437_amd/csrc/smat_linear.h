@@ -70,7 +70,7 @@ struct LinArgs {
   const float* lse;
   const float* row_scale;  // NULL: 1
   void* out_low;  // what rounding out to bf16 left, in bf16; or NULL
-  // out = s (v + sum_in), or sum_out = v + sum_in (NULL: 0), with s = scale[0] / totals[1] (NULL: 1)
+  // out = s (v + sum_in), zeros in rows without a target (targets not NULL), or sum_out = v + sum_in (NULL: 0), with s = scale[0] / totals[1] (NULL: 1)
   const float* sum_in;
   float* sum_out;
   int64_t ldsum;

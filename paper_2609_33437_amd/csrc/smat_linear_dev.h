@@ -351,7 +351,7 @@ struct Side<T, kEpiXentGrad> {
 template <typename T>
 struct Side<T, kEpiSum> {
   Raw8<float> sum;
-  int64_t row;  // of out
+  int64_t row;  // of out; -1 - row: it is zeros
 };
 template <typename T>
 struct ColumnSide<T, kEpiSum> {
@@ -442,7 +442,7 @@ __device__ __forceinline__ void side_load(const LinArgs& a, int64_t i, int64_t j
   if constexpr (EPI == kEpiSum) {
     if (WHOLE || (i < a.i && j0 < a.j)) {
       if (a.sum_in) s.sum.load(a.sum_in + i * a.ldsum + j0);  // rows of whole eights
-      s.row = a.out_rows ? a.out_rows[i] : i;
+      s.row = a.out_rows ? a.out_rows[i] : a.targets && a.targets[i] == a.ignore ? -1 - i : i;
     }
   }
 }
@@ -600,7 +600,14 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= c.scale;
   }
-  if constexpr (EPI == kEpiSum) i = s.row;
+  if constexpr (EPI == kEpiSum) {
+    i = s.row;
+    if (i < 0) {
+      i = -1 - i;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    }
+  }
   if constexpr (EPI == kEpiDgrad) {
     if (a.z_codes) {
       float z[8];

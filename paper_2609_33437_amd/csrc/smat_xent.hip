@@ -181,27 +181,29 @@ __global__ __launch_bounds__(1024) void k_xent_some(XentGradArgs a, SomeRows r) 
   if (threadIdx.x == 0) *r.count = before;
 }
 
-// Their rows of x, on 16-byte rows with zeros at their ends, and zeros in the other rows of dx: a wave a row.
+// x on 16-byte rows with zeros at their ends, a wave a row: rows without a target as zeros, so that a padded row's NaN
+// reaches no gradient, or with `place` the other rows alone, and then the zeros of such rows of dx too.
 template <typename T>
-__global__ __launch_bounds__(256) void k_xent_gather(XentGradArgs a, const int32_t* place, void* to, int64_t stride) {
+__global__ __launch_bounds__(256) void k_xent_rows_of_x(XentGradArgs a, const int32_t* place, void* to, int64_t stride) {
   using Mem = typename El<T>::Mem;
-  const int64_t i = wide_block() * 4 + ((int)threadIdx.x >> 6);
+  const int64_t i = wide_block() * 4 + ((int)threadIdx.x >> 6), first = (int64_t)(threadIdx.x & 63) * 8;
   if (i >= a.m) return;
-  const int64_t at = place[i];
+  const int64_t at = place ? place[i] : i;
+  const bool on = place ? at >= 0 : a.targets[i] != a.ignore;
+  const float zeros[8] = {};
   if (at >= 0) {
     const Mem* x = static_cast<const Mem*>(a.x) + i * a.ldx;
     Mem* row = static_cast<Mem*>(to) + at * stride;
 #pragma unroll 4
-    for (int64_t j = (int64_t)(threadIdx.x & 63) * 8; j < stride; j += 512) {
+    for (int64_t j = first; j < stride; j += 512) {
       float v[8];
-      load_row8<T>(x + j, a.k - j, v);
+      load_row8<T>(x + j, on ? a.k - j : 0, v);
       store_row8<T>(row + j, stride - j, v);
     }
   } else if (a.dx) {
-    const float v[8] = {};
     Mem* row = static_cast<Mem*>(a.dx) + i * a.lddx;
 #pragma unroll 4
-    for (int64_t j = (int64_t)(threadIdx.x & 63) * 8; j < a.k; j += 512) store_row8<T>(row + j, a.k - j, v);
+    for (int64_t j = first; j < a.k; j += 512) store_row8<T>(row + j, a.k - j, zeros);
   }
 }
 }  // namespace
@@ -216,19 +218,16 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
   const int64_t bytes = dtype == 1 ? 2 : 4, from = p * plan.width, width = a.n - from < plan.width ? a.n - from : plan.width;
   const int64_t packed = packed_stride(a.k, dtype);
   const void* w = static_cast<const char*>(a.w) + from * a.ldw * bytes;
-  const void* x = a.x;
-  int64_t ldw = a.ldw, ldx = a.ldx;
-  if (plan.pack & 1) {
-    x = ws + plan.x;
-    ldx = packed;
-  }
-  if (plan.pack & 2) {
+  const void* x = ws + plan.x;
+  const int64_t ldx = packed;
+  int64_t ldw = a.ldw;
+  if (plan.pack) {
     w = ws + plan.w;
     ldw = packed;
   }
   char *dz = ws + plan.dz, *low = plan.low ? dz + a.m * plan.width * bytes : nullptr;
   Piece q{};
-  q.logits.prod[0] = LinProduct{x, w, ldx, ldw, plan.pack == 3 ? packed : a.k};  // both end in zeros
+  q.logits.prod[0] = LinProduct{x, w, ldx, ldw, plan.pack ? packed : a.k};  // both end in zeros
   q.logits.i = a.m;
   q.logits.j = width;
   q.logits.out = dz;
@@ -259,6 +258,9 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
     if (a.row_scale) q.logits.row_scale = r.row_scale;
     q.dx.out_rows = r.from;
     q.logits.count = q.dx.count = q.dw.count = r.count;
+  } else {
+    q.dx.targets = a.targets;
+    q.dx.ignore = a.ignore;
   }
   q.dw.prod[0] = LinProduct{dz, x, plan.width, ldx, a.m};
   if (low) q.dw.prod[1] = LinProduct{low, x, plan.width, ldx, a.m};
@@ -297,10 +299,9 @@ double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
       // 62106 x 2982: 190 us)
       piece += l->us * (dtype == 1 && l->parts && !l->direct ? 1.5 : 1.0);
     }
-    if (p.pack & 2) piece += pack_us((double)q.logits.j * (double)a.k * (double)bytes);
+    if (p.pack) piece += pack_us((double)q.logits.j * (double)a.k * (double)bytes);
     us += piece * (double)(last ? 1 : p.pieces - 1);
   }
-  if (p.pack & 1) us += pack_us((double)a.m * (double)a.k * (double)bytes);
   size_t at = round16(product);
   const auto take = [&](int64_t elements, int64_t size, bool wanted) {
     const size_t here = at;
@@ -310,8 +311,8 @@ double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
   const int64_t packed = packed_stride(a.k, dtype);
   p.dz = take(a.m * p.width * (p.low ? 2 : 1), bytes, true);
   p.sum = take(a.m * (div_up(a.k, 8) * 8), 4, a.dx && p.pieces > 1);
-  p.x = take(a.m * packed, bytes, p.pack & 1);
-  p.w = take(p.width * packed, bytes, p.pack & 2);
+  p.x = take(a.m * packed, bytes, true);
+  p.w = take(p.width * packed, bytes, p.pack);
   p.rows = take(some_rows_bytes(a.m), 1, p.some);
   p.workspace = at;
   return us;
@@ -338,11 +339,10 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   if (!a.dx) both.dx = a.dw;
   if (!a.dw) both.dw = a.dx;
   double us = plan_products(both, dtype, p);
-  // operands off 16-byte rows serve two products each: copies for both, where that is estimated to be faster
-  const bool fits_x = on_16_bytes(a.x, a.ldx, a.k, bytes), fits_w = on_16_bytes(a.w, a.ldw, a.k, bytes);
-  if (a.m > 0 && a.k > 0 && (!fits_x || !fits_w)) {
+  // rows of W off 16 bytes serve two products: a copy of each piece for both, where that is estimated to be faster
+  if (a.m > 0 && a.k > 0 && !on_16_bytes(a.w, a.ldw, a.k, bytes)) {
     XentGradPlan q = p;
-    q.pack = (fits_x ? 0 : 1) | (fits_w ? 0 : 2);
+    q.pack = 1;
     const double copied = plan_products(both, dtype, q);
     if (copied < us) {
       us = copied;
@@ -350,14 +350,10 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
     }
   }
   // Rows without a target (a prompt's, padding) have no gradient.  Only the device knows them, so the launches are for all rows
-  // and blocks without any end at once.  Two launches and a copy of x find them; they are spent where they are estimated at a
-  // fiftieth of the call or less.  (2048 x 128256 x 4096, half of the rows without: losses and gradients 4.75 ms, 6.15 ms with
+  // and blocks without any end at once.  A launch finds them; it is spent where it is estimated at a fiftieth of the call or
+  // less.  (2048 x 128256 x 4096, half of the rows without: losses and gradients 4.75 ms, 6.15 ms with
   // products over all rows.)
-  const double some = 10.0 + pack_us((double)a.m * (double)a.k * (double)bytes);
-  if (a.k > 0 && !p.low && us > 50.0 * some) {
-    p.some = 1;
-    p.pack |= 1;
-  }
+  p.some = a.k > 0 && !p.low && us > 50.0 * (10.0 + (double)a.m / 1000.0);
   plan_products(a, dtype, p);
   return p;
 }
@@ -365,23 +361,26 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
 hipError_t launch_xent_grad(const XentGradArgs& a, int dtype, const XentGradPlan& plan, void* workspace, hipStream_t stream) {
   hipError_t e = hipSuccess;
   char* ws = static_cast<char*>(workspace);
-  if (plan.some) {
-    const SomeRows r = some_rows(ws + plan.rows, a.m);
-    k_xent_some<<<dim3(1), dim3(1024), 0, stream>>>(a, r);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (plan.pieces == 0) return e;  // no gradient is wanted, and there is no workspace
+  if (a.m > 0) {
+    const int32_t* place = nullptr;
+    if (plan.some) {
+      const SomeRows r = some_rows(ws + plan.rows, a.m);
+      k_xent_some<<<dim3(1), dim3(1024), 0, stream>>>(a, r);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      place = r.place;
+    }
     const dim3 grid = wide_grid(div_up(a.m, 4));
     if (dtype == 1)
-      k_xent_gather<Bf16><<<grid, dim3(256), 0, stream>>>(a, r.place, ws + plan.x, packed_stride(a.k, dtype));
+      k_xent_rows_of_x<Bf16><<<grid, dim3(256), 0, stream>>>(a, place, ws + plan.x, packed_stride(a.k, dtype));
     else
-      k_xent_gather<float><<<grid, dim3(256), 0, stream>>>(a, r.place, ws + plan.x, packed_stride(a.k, dtype));
+      k_xent_rows_of_x<float><<<grid, dim3(256), 0, stream>>>(a, place, ws + plan.x, packed_stride(a.k, dtype));
     e = hipGetLastError();
-  } else if (plan.pack & 1) {
-    e = launch_pack(a.x, a.ldx, a.m, a.k, dtype, ws + plan.x, stream);
   }
   for (int64_t p = 0; p < plan.pieces && e == hipSuccess; ++p) {
     const Piece q = piece_args(a, dtype, plan, p, ws);
     const int last = p + 1 == plan.pieces;
-    if (plan.pack & 2) {
+    if (plan.pack) {
       const char* w = static_cast<const char*>(a.w) + p * plan.width * a.ldw * (dtype == 1 ? 2 : 4);
       if ((e = launch_pack(w, a.ldw, q.logits.j, a.k, dtype, ws + plan.w, stream)) != hipSuccess) break;
     }

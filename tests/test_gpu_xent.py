@@ -232,6 +232,38 @@ def test_rows_without_a_target(dtype, m):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(3, 40, 16), (100, 500, 64), (600, 3000, 130), (4096, 40000, 1024)])
+def test_padded_rows_without_a_number(dtype, m, n, k):
+    """What lies in the rows without a target, NaN and infinities, reaches no loss and no gradient."""
+    if dtype == "f32" and n > 3000:
+        m, n, k = 1500, 16000, 768
+    x, w, t = make(m, n, k, dtype, ignored=0.3)
+    t[1] = IGNORE
+    t[0] = 0
+    none = t == IGNORE
+    weights = torch.rand(m, generator=torch.Generator(DEV).manual_seed(5), device=DEV) + 0.5
+    clean = x.clone()
+    clean[none] = 0
+    want = []
+    for rows in (clean, x):
+        if rows is x:
+            x[none] = float("nan")
+            x[1] = float("inf")
+            weights[none] = float("nan")
+        loss, lse, tot = torch.empty(m, device=DEV), torch.empty(m, device=DEV), torch.empty(3, device=DEV)
+        smat.smat_linear_xent(rows, w, t, loss, lse, totals=tot, ignore_index=IGNORE)
+        dx, dw = torch.full_like(rows, 3.0), torch.full_like(w, 3.0)
+        smat.smat_linear_xent_grad(rows, w, t, lse, dx=dx, dw=dw, row_scale=weights, totals=tot, ignore_index=IGNORE)
+        want.append((loss, lse[~none], tot, dx, dw))
+    assert all(torch.equal(a, b) for a, b in zip(*want)) and not want[1][3][none].any() and torch.isfinite(want[1][4]).all()
+    # and a W that spoils everything else leaves those rows of dx alone
+    w[3] = float("nan")
+    smat.smat_linear_xent(x, w, t, loss, lse, ignore_index=IGNORE)
+    smat.smat_linear_xent_grad(x, w, t, lse, dx=dx, ignore_index=IGNORE)
+    assert not loss[none].any() and not dx[none].any() and dx[~none].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m", [3, 64, 600])
 def test_logits_without_a_number(dtype, m):
     """Logits of -inf have no probability; +inf and NaN spoil their rows and no others; huge logits do not overflow."""
