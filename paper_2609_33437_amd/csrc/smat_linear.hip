@@ -1371,7 +1371,8 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
   if (epi == kEpiSum) z.epilogue = 4.0;
   Operand o[4];
   operands(a, epi, bytes, o);
-  if (epi == kEpiXent || epi == kEpiXentGrad) z.rows = (double)a.j * (double)a.prod[0].r * bytes;
+  const bool few_fit = a.j <= kMaxThreads / 16 - 32;  // the kernel for few rows has 16 threads a column
+  if ((epi == kEpiXent || epi == kEpiXentGrad) && few_fit) z.rows = (double)a.j * (double)a.prod[0].r * bytes;
   int32_t off = 0;  // operands that cannot be copied to LDS directly as they lie
   bool wide = false;  // one of them is too wide for direct copies even where it is packed
   double moved = 0.0;
@@ -1398,8 +1399,8 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       best.pack = off;
     }
   }
-  // few rows: the kernel that takes operands of any alignment without a copy (16 threads a column where there are many)
-  if ((epi == kEpiLayer || epi == kEpiXent || epi == kEpiXentGrad) && a.i <= kMaxRows && a.j <= kMaxThreads / 16 - 32) {
+  // few rows: the kernel that takes operands of any alignment without a copy
+  if ((epi == kEpiLayer || epi == kEpiXent || epi == kEpiXentGrad) && a.i <= kMaxRows && few_fit) {
     const double rate = kRowsRate[a.i > 4 ? 3 : a.i > 2 ? 2 : a.i - 1];
     if (kRowsStart + z.bytes / rate <= least) {
       least = kRowsStart + z.bytes / rate;
