@@ -41,8 +41,9 @@ struct NormGradArgs {
   int64_t m, n;
   int32_t layer, wdtype, blocks;
 };
-// Blocks that share the rows, each with its sums of dw and db.
+// Blocks that share the rows, each with its sums of dw and db, and the bytes of `partial` for so many outputs.
 int32_t norm_grad_blocks(int64_t m, int64_t n);
+size_t norm_grad_partial(int64_t m, int64_t n, int outputs);
 hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, hipStream_t stream);
 
 // ---------------------------------------------------------------- embedding

@@ -81,7 +81,7 @@ smat_status norm_grad_call(const smat_norm_grad_args* g, NormGradCall* c, const 
   if (smat_status st = check_grid(g->m, g->n, where)) return st;
   c->a = NormGradArgs{g->dy, g->lddy, g->x, g->ldx, g->weight, g->mean, g->rstd, g->dx, g->lddx, g->dweight, g->dbias,
                       nullptr, g->m, g->n, g->kind == SMAT_NORM_LAYER, g->wdtype, norm_grad_blocks(g->m, g->n)};
-  c->workspace = round16((size_t)((g->dweight ? 1 : 0) + (g->dbias ? 1 : 0)) * (size_t)c->a.blocks * (size_t)g->n * 4);
+  c->workspace = round16(norm_grad_partial(g->m, g->n, (g->dweight ? 1 : 0) + (g->dbias ? 1 : 0)));
   return SMAT_OK;
 }
 

@@ -264,6 +264,7 @@ __global__ __launch_bounds__(S::kBlock) void k_norm_grad(NormGradArgs a) {
   // the block's sums, its groups' added in order
   for (int which = 0; which < 2; ++which) {
     if (!(which ? a.db : a.dw)) continue;
+    void* last = which ? a.db : a.dw;  // of one block
     float* to = a.partial + ((int64_t)(which && a.dw ? a.blocks : 0) + blockIdx.x) * a.n;
     if constexpr (S::kRows > 1) {
       for (int k = 0; k < S::kRows; ++k) {
@@ -281,7 +282,13 @@ __global__ __launch_bounds__(S::kBlock) void k_norm_grad(NormGradArgs a) {
         }
       }
       __syncthreads();
-      for (int j = (int)threadIdx.x; j < a.n; j += S::kBlock) to[j] = shared[j % 8 * (S::kColumns / 8) + j / 8];
+      for (int j = (int)threadIdx.x; j < a.n; j += S::kBlock) {
+        const float v = shared[j % 8 * (S::kColumns / 8) + j / 8];
+        if (a.blocks == 1)
+          store_weight(last, a.wdtype, j, v);
+        else
+          to[j] = v;
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < S::kE; ++e) {
@@ -289,7 +296,12 @@ __global__ __launch_bounds__(S::kBlock) void k_norm_grad(NormGradArgs a) {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = which ? db[e][i] : dw[e][i];
-        store_row8<float>(to + j, a.n - j, v);
+        if (a.blocks > 1)
+          store_row8<float>(to + j, a.n - j, v);
+        else if (a.wdtype == SMAT_BF16)
+          store_row8<Bf16>(static_cast<uint16_t*>(last) + j, a.n - j, v);
+        else
+          store_row8<float>(static_cast<float*>(last) + j, a.n - j, v);
       }
     }
   }
@@ -437,7 +449,16 @@ int32_t norm_grad_blocks(int64_t m, int64_t n) {
   int64_t rows = 1;
   if (n <= kMaxHeld) with_shape(n, [&](auto s) { rows = decltype(s)::kRows; });
   const int64_t blocks = div_up(m, rows);
+  // a handful of rows is one block's, which writes dw and db itself and spares the second launch. Replayed, two rows of 4096 take
+  // 4.8 us so and 6.1 apart, of 16384 10.7 and 11.8; three 5.8 and 6.1, 13.3 and 11.8. A call with 8 x 64 takes 9.0 us, host
+  // bound, and 13.2 with two launches.
+  if (n <= kMaxHeld && blocks > 0 && blocks <= 2) return 1;
   return (int32_t)(blocks < 512 ? blocks : 512);
+}
+
+size_t norm_grad_partial(int64_t m, int64_t n, int outputs) {
+  const int32_t blocks = norm_grad_blocks(m, n);
+  return blocks == 1 && n <= kMaxHeld ? 0 : (size_t)outputs * (size_t)blocks * (size_t)n * 4;
 }
 
 hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, hipStream_t stream) {
@@ -461,7 +482,7 @@ hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, hipStream_t stream
     });
     if (e == hipSuccess) e = hipGetLastError();
   }
-  if (e == hipSuccess && sums) {
+  if (e == hipSuccess && sums && (a.blocks != 1 || a.n > kMaxHeld)) {
     dim3 grid = wide_grid(div_up(a.n, kJoinColumns));
     grid.z = a.dw && a.db ? 2 : 1;
     k_norm_join<<<grid, dim3(kJoinColumns * kJoinRows), 0, stream>>>(a);

@@ -31,7 +31,7 @@ def make(kind, base, kw):
 
 NORM = dict(dtype=BF16, wdtype=F32, kind=0, eps=1e-5, m=8, n=96, x=at(0), ldx=96, weight=at(1), bias=at(2), y=at(3), ldy=96,
             mean=at(4), rstd=at(5))
-NORM_GRAD = dict(dtype=BF16, wdtype=F32, kind=0, m=8, n=96, dy=at(0), lddy=96, x=at(1), ldx=96, weight=at(2), mean=at(3),
+NORM_GRAD = dict(dtype=BF16, wdtype=F32, kind=0, m=300, n=96, dy=at(0), lddy=96, x=at(1), ldx=96, weight=at(2), mean=at(3),
                  rstd=at(4), dx=at(5), lddx=96, dweight=at(6), dbias=at(7))
 EMBED = dict(dtype=BF16, table_dtype=F32, scale=1.0, m=8, rows=50, d=96, table=at(0), ldtable=96, ids=at(1), out=at(2), ldout=96)
 EMBED_GRAD = dict(dtype=BF16, table_dtype=F32, scale=1.0, m=300, rows=50, d=96, padding=-1, dy=at(0), lddy=96, ids=at(1),
