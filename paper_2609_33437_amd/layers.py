@@ -347,7 +347,7 @@ def _ids(ids: torch.Tensor, like: torch.Tensor, what: str) -> torch.Tensor:
         raise SmatError(SMAT_ERR_INVALID, f"{what} must be int64, got {ids.dtype}")
     if ids.device != like.device:
         raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the GPU of the other tensors")
-    return ids.reshape(-1)
+    return ids.reshape(-1).contiguous()      # a column of a batch stays strided
 
 
 # ------------------------------------------------------------------ public functions

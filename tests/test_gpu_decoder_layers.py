@@ -234,6 +234,24 @@ def test_layouts_and_views():
     assert torch.isfinite(none.grad).all()
 
 
+def test_columns_of_a_batch_as_ids():
+    """Strided vectors of ids, as tokens[:, -1], and repeated ones are taken like their copies."""
+    w, x = double(12, 10, seed=2).float().to(DEV), double(6, 10, seed=1).float().to(DEV)
+    batch = torch.arange(18, device=DEV).view(6, 3) % 12
+    for ids in (batch[:, -1], batch[0, :1].expand(6), batch[::2, 1]):
+        assert torch.equal(layers.embedding(ids, w), layers.embedding(ids.clone(), w))
+        table, copied = leaf(w), leaf(w)
+        layers.embedding(ids, table).sum().backward()
+        layers.embedding(ids.clone(), copied).sum().backward()
+        assert torch.equal(table.grad, copied.grad)
+        rows = x[:ids.shape[0]]
+        own, other = leaf(rows), leaf(rows)
+        a, b = layers.linear_cross_entropy(own, w, ids), layers.linear_cross_entropy(other, w, ids.clone())
+        a.backward()
+        b.backward()
+        assert torch.equal(a, b) and torch.equal(own.grad, other.grad)
+
+
 def test_frozen_and_partial_gradients():
     x, w = double(6, 10, seed=1).float().to(DEV), leaf(double(12, 10, seed=2))
     t = torch.arange(6, device=DEV)
