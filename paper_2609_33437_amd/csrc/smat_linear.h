@@ -81,6 +81,8 @@ struct LinArgs {
   const int32_t* count;
   const int32_t* out_rows;
   int64_t row_from;
+  // of kEpiSum: rows of a tile and the ranges of r that may be made, for fewer rows than planned; the block's own range
+  int32_t tile_rows, most_splits, range;
   // sums of `splits` ranges of r, joined by a second kernel: [splits][i][j rounded up to 8] fp32
   int32_t splits;
   float* partial;

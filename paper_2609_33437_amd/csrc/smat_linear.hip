@@ -158,7 +158,7 @@ __device__ __forceinline__ void finish_eights(const LinArgs& a, int64_t i0, int6
       const int64_t i = i0 + rows(which % NI + n);
       if (partial) {
         if (WHOLE || (i < a.i && j < ld))
-          El<float>::store8(a.partial + ((int64_t)blockIdx.y * a.i + i) * ld + j, v[n]);
+          El<float>::store8(a.partial + ((int64_t)range_of<EPI>(a) * a.i + i) * ld + j, v[n]);
       } else {
         epilogue8<T, EPI, 16, 32, WHOLE>(a, i, j, v[n], column, side[n]);
       }
@@ -504,14 +504,21 @@ __device__ __forceinline__ void tile_place(uint32_t b, uint32_t ti, uint32_t tj,
   i = band * kHigh + (in - j * high);
 }
 
-// This block's tile; false where there are fewer rows than the launch was made for, and it has none.
+// This block's tile, and for kEpiSum its range; false where there are fewer rows than the launch was made for, and it has none.
 template <int EPI>
-__device__ __forceinline__ bool tile_place(const LinArgs& a, int ki, int kj, uint32_t& i, uint32_t& j) {
-  const uint32_t ti = (uint32_t)((a.i + ki - 1) / ki), tj = (uint32_t)((a.j + kj - 1) / kj);
-  if constexpr (EPI == kEpiXentGrad || EPI == kEpiSum) {
-    if (blockIdx.x >= ti * tj) return false;
+__device__ __forceinline__ bool tile_place(LinArgs& a, int ki, int kj, uint32_t& i, uint32_t& j) {
+  const uint32_t ti = (uint32_t)((a.i + ki - 1) / ki), tj = (uint32_t)((a.j + kj - 1) / kj), tiles = ti * tj;
+  uint32_t b = blockIdx.x;
+  if constexpr (EPI == kEpiXentGrad) {
+    if (b >= tiles) return false;
   }
-  tile_place(blockIdx.x, ti, tj, i, j);
+  if constexpr (EPI == kEpiSum) {
+    b += blockIdx.y * gridDim.x;
+    a.range = (int32_t)(b / tiles);
+    if (a.range >= a.splits) return false;
+    b -= (uint32_t)a.range * tiles;
+  }
+  tile_place(b, ti, tj, i, j);
   return true;
 }
 
@@ -526,7 +533,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   const int64_t i0 = (int64_t)ti * kFastB, j0 = (int64_t)tj * kFastB;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
   const int64_t n0 = (a.prod[0].r + 63) / 64, n = n0 + (a.prod[1].r + 63) / 64;
-  const int64_t first = split_start(n, blockIdx.y, a.splits), last = split_start(n, blockIdx.y + 1, a.splits);
+  const int64_t first = split_start(n, range_of<EPI>(a), a.splits), last = split_start(n, range_of<EPI>(a) + 1, a.splits);
   Feed<T, PT, QT, EPI> feed;
   Copy<T, PT, false, kFastHalf, 2> cp[2];
   Copy<T, QT, true, kFastHalf, 2> cq[2];
@@ -670,7 +677,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   const int64_t i0 = (int64_t)ti * S::kI, j0 = (int64_t)tj * S::kJ;
   const int wi = w / S::WJ * S::TI, wj = w % S::WJ * S::TJ;
   const int64_t n0 = (a.prod[0].r + kDeep - 1) / kDeep, n = n0 + (a.prod[1].r + kDeep - 1) / kDeep;
-  const uint32_t share = blockIdx.y * S::G + (uint32_t)group;
+  const uint32_t share = range_of<EPI>(a) * S::G + (uint32_t)group;
   const int64_t first = split_start(n, share, a.splits * S::G), last = split_start(n, share + 1, a.splits * S::G);
   // every group of a block takes the same number of steps, so that barriers meet (shares differ by one stage)
   const int64_t steps = (n + a.splits * S::G - 1) / (a.splits * S::G);
@@ -868,7 +875,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
         }
       if (a.splits > 1) {
         const int64_t ld = (a.j + 7) & ~(int64_t)7;
-        if (gi < a.i && gj < ld) El<float>::store8(a.partial + ((int64_t)blockIdx.y * a.i + gi) * ld + gj, v);
+        if (gi < a.i && gj < ld) El<float>::store8(a.partial + ((int64_t)range_of<EPI>(a) * a.i + gi) * ld + gj, v);
       } else if constexpr (EPI == kEpiXent) {
         eight_stats<T, S::kJ / 8>(a, gi, gj, a.j - gj, v, side.target, tj);
       } else {
@@ -1246,6 +1253,7 @@ struct Sizes {
 
 // Microseconds of `splits` ranges of r with tile f, or kNever where its grid cannot be launched.
 constexpr double kNever = 1e30;
+constexpr int64_t kMostSplits = 16;
 double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
   const int64_t tiles = div_up(z.i, f.i) * div_up(z.j, f.j), blocks = tiles * splits;
   const int64_t slots = (int64_t)kComputeUnits * f.resident;
@@ -1280,7 +1288,7 @@ double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part) {
     const FormCost& f = costs[c];
     const int64_t tiles = div_up(z.i, f.i) * div_up(z.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
     int64_t most = slots / tiles + 1;
-    if (most > 16) most = 16;
+    if (most > kMostSplits) most = kMostSplits;
     if (most > z.stages / (2 * f.groups)) most = z.stages / (2 * f.groups);
     for (int64_t splits = 1; splits == 1 || splits <= most; ++splits) {
       const double us = time_of(f, z, splits);
@@ -1538,6 +1546,15 @@ hipError_t launch_linear(const LinArgs& args, int dtype, LinEpilogue epi, const 
       a.stat_ld = div_up(a.j, stat_columns(part));
       a.stats = stats;
       stats += a.i * a.stat_ld * 2;
+    }
+    if (a.count && a.splits > 1) {
+      const int64_t deep = 128 / bytes, stages = div_up(a.prod[0].r, deep) + div_up(a.prod[1].r, deep);
+      for (const FormCost& f : kDirectCosts[0])
+        if (f.form == part.form) {
+          const int64_t most = stages / (2 * f.groups);
+          a.tile_rows = f.i;
+          a.most_splits = (int32_t)(most < kMostSplits ? most : kMostSplits);
+        }
     }
     const int64_t eights = a.i * ckpt_blocks(a.j) * 4;  // of the join
     if (part.form == 0 || (a.splits > 1 && eights > kMaxThreads - 256)) return hipErrorInvalidConfiguration;
