@@ -190,8 +190,7 @@ __global__ __launch_bounds__(1024) void k_norm_wide(NormArgs a) {
   }
 }
 
-// Blocks take rows in turn and keep their sums of dw and db in registers; k_norm_join adds the blocks' sums in order.  512
-// blocks: with 256 the rows of 16384 x 4096 take 94 us, with 512 81, with 768 80 and with 1536 77, and the join 5, 5, 5 and 9.
+// Blocks take rows in turn and keep their sums of dw and db in registers; k_norm_join adds the blocks' sums in order.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kBlock) void k_norm_grad(NormGradArgs a) {
   using Mem = typename El<T>::Mem;
@@ -453,7 +452,12 @@ int32_t norm_grad_blocks(int64_t m, int64_t n) {
   // 4.8 us so and 6.1 apart, of 16384 10.7 and 11.8; three 5.8 and 6.1, 13.3 and 11.8. A call with 8 x 64 takes 9.0 us, host
   // bound, and 13.2 with two launches.
   if (n <= kMaxHeld && blocks > 0 && blocks <= 2) return 1;
-  return (int32_t)(blocks < 512 ? blocks : 512);
+  // One block a compute unit; two where each still has several turns, and rows are narrow enough for both blocks' registers.
+  // Replayed, with 256 and 512 blocks: 600 x 4096 13.5 and 17.5 us, 1024 x 2048 10.5 and 12.2, 2000 x 4096 18.2 and 19.1, 3000 x
+  // 12288 60 and 75, 12115 x 5544 82 and 87; 8192 x 512 11.8 and 11.1, 4096 x 2048 18.4 and 16.4, 10000 x 768 18.5 and 16.4,
+  // 16384 x 4096 80 and 81.
+  const int64_t most = n <= 4096 && blocks >= 2048 ? 512 : 256;
+  return (int32_t)(blocks < most ? blocks : most);
 }
 
 size_t norm_grad_partial(int64_t m, int64_t n, int outputs) {
