@@ -15,44 +15,39 @@ from ._lib import (SMAT_ERR_DTYPE, SMAT_ERR_INVALID, SMAT_NORM_LAYER, SMAT_NORM_
 from ._linear import _call, _first, _matrix, _stream_on
 
 
+def _refuse_vector(t, n: int, device: int, what: str) -> None:
+    """Raises for what makes t no contiguous vector [n] on that GPU."""
+    if t.shape != (n,):
+        raise SmatError(SMAT_ERR_INVALID, f"{what} has shape {tuple(t.shape)}, expected ({n},)")
+    if t.get_device() != device:
+        raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the same GPU as the call's first matrix")
+    raise SmatError(SMAT_ERR_INVALID, f"{what} must be contiguous")
+
+
 def _typed(t, n: int, dtype, device: int, what: str) -> int:
     """Pointer of a contiguous vector [n] of that dtype on that GPU."""
-    if t.dim() != 1 or t.shape[0] != n:
-        raise SmatError(SMAT_ERR_INVALID, f"{what} has shape {tuple(t.shape)}, expected ({n},)")
     if t.dtype is not dtype:
         raise SmatError(SMAT_ERR_DTYPE, f"{what} has dtype {t.dtype}, expected {dtype}")
-    if t.get_device() != device:
-        raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the same GPU as the call's first matrix")
-    if n > 1 and t.stride(0) != 1:
-        raise SmatError(SMAT_ERR_INVALID, f"{what} must be contiguous")
+    if t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
+        _refuse_vector(t, n, device, what)
     return t.data_ptr()
-
-
-def _weight(t, n: int, device: int, what: str):
-    """(dtype code, pointer) of a contiguous vector [n] of weights on that GPU."""
-    if t.dim() != 1 or t.shape[0] != n:
-        raise SmatError(SMAT_ERR_INVALID, f"{what} has shape {tuple(t.shape)}, expected ({n},)")
-    if t.get_device() != device:
-        raise SmatError(SMAT_ERR_INVALID, f"{what} must be on the same GPU as the call's first matrix")
-    if n > 1 and t.stride(0) != 1:
-        raise SmatError(SMAT_ERR_INVALID, f"{what} must be contiguous")
-    return dtype_code(t), t.data_ptr()
 
 
 def _weights(code: int, n: int, device: int, *named):
     """(their dtype code, pointers) of the vectors [n] that are given, which share a dtype; `code` where there are none."""
-    first, ptrs = None, []
+    dtype, ptrs = None, []
     for t, what in named:
         if t is None:
             ptrs.append(None)
             continue
-        c, ptr = _weight(t, n, device, what)
-        if first is None:
-            first = c
-        elif c != first:
-            raise SmatError(SMAT_ERR_DTYPE, f"{what} has dtype {t.dtype}, another one than the weights before it")
-        ptrs.append(ptr)
-    return (code if first is None else first), ptrs
+        if t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
+            _refuse_vector(t, n, device, what)
+        if t.dtype is not dtype:
+            if dtype is not None:
+                raise SmatError(SMAT_ERR_DTYPE, f"{what} has dtype {t.dtype}, another one than the weights before it")
+            code, dtype = dtype_code(t), t.dtype
+        ptrs.append(t.data_ptr())
+    return code, ptrs
 
 
 # ------------------------------------------------------------------ norms
