@@ -432,17 +432,16 @@ __global__ __launch_bounds__(256) void k_embed_join(RowArgs r) {
   if (c + 1 >= r.chunks) return;
   const int32_t eight = (int32_t)(t - c * r.tiles) * 64 + ((int)threadIdx.x & 63);
   const int64_t begin = c * r.chunk, end = begin + r.chunk;
-  const uint32_t key = r.keys[end - 1];
-  if (key == (uint32_t)a.rows || r.keys[end] != key) return;
-  if (begin > 0 && r.keys[begin] == key && r.keys[begin - 1] == key) return;  // an earlier chunk's
-  // the last chunk that holds a token of the run
-  int64_t low = c + 1, high = r.chunks - 1;
-  while (low < high) {
-    const int64_t middle = (low + high + 1) / 2;
-    if (r.keys[middle * r.chunk] == key)
-      low = middle;
-    else
-      high = middle - 1;
+  // the keys on both sides of the chunk's ends, loaded together
+  const uint32_t key = r.keys[end - 1], after = r.keys[end], first = r.keys[begin], before = r.keys[begin > 0 ? begin - 1 : 0];
+  if (key == (uint32_t)a.rows || after != key) return;
+  if (begin > 0 && first == key && before == key) return;  // an earlier chunk's
+  // the last chunk that holds a token of the run: the lanes look at 64 chunks at a time
+  int64_t low = c + 1, high = r.chunks;
+  for (int64_t each; low + 1 < high; high = low + each < high ? low + each : high) {
+    each = (high - low + 63) / 64;
+    const int64_t probe = low + ((int)threadIdx.x & 63) * each;
+    low += (__popcll(__ballot(probe < high && r.keys[probe < high ? probe * r.chunk : 0] == key)) - 1) * each;
   }
   if (eight >= r.across) return;
   const int64_t step = (int64_t)r.across * 16;
