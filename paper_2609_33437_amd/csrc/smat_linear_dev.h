@@ -488,20 +488,17 @@ __device__ __forceinline__ void side_values(const Raw8<T>& raw, const void* row,
 }
 
 // ---------------------------------------------------------------- statistics of logits
-// exp(v - top) as the sums take it.  In bf16 the product with log2 e is one fused operation, which rounds top log2 e: an error
-// of an fp32 rounding of top in the row's log sum.
+// exp(v - top) as the sums take it: by the hardware's exp2 in bf16.  The difference is taken first: one fused operation with top
+// log2 e rounded would be off by its rounding, which passes exp2's range where logits are 2^31.
 template <typename T>
 struct StatExp {
-  float top, shift;
-  __device__ __forceinline__ explicit StatExp(float t) {
-    top = t == -__builtin_inff() ? 0.f : t;  // only -inf: a sum of zeros
-    shift = -top * 1.44269504088896340736f;
-  }
+  float top;
+  __device__ __forceinline__ explicit StatExp(float t) : top(t == -__builtin_inff() ? 0.f : t) {}  // only -inf: a sum of zeros
   __device__ __forceinline__ float operator()(float v) const {
     if constexpr (El<T>::kBytes == 4)
       return expf(v - top);
     else
-      return __builtin_amdgcn_exp2f(__builtin_fmaf(v, 1.44269504088896340736f, shift));
+      return __builtin_amdgcn_exp2f((v - top) * 1.44269504088896340736f);
   }
 };
 // (top, sum) of two sets of values: sum = sum exp(v - top), and exp(v - 0) where there is only -inf.

@@ -264,6 +264,35 @@ def test_padded_rows_without_a_number(dtype, m, n, k):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 3, 64, 600])
+@pytest.mark.parametrize("power", [0, 20, 31, 33, 60, 110])
+def test_logits_of_any_size(dtype, m, power):
+    """Logits of multiples of 2^(power - 8) up to 2^power, whose differences no exponential can tell from infinite ones from
+    power 20 on: losses and gradients are then exact."""
+    n, k = 300, 32
+    x, w = torch.zeros(m, k, device=DEV, dtype=DT[dtype]), torch.zeros(n, k, device=DEV, dtype=DT[dtype])
+    x[:, 3] = 2.0 ** power
+    w[:, 3] = (torch.arange(n, device=DEV) % 255 + 1) / 256
+    t = torch.arange(m, device=DEV) * 7 % 255
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    smat.smat_linear_xent(x, w, t, loss, lse)
+    z = x.double() @ w.double().t().contiguous()
+    want = torch.logsumexp(z, 1)
+    if power < 20:
+        assert float((lse - want).abs().max()) < 1e-4
+        return
+    assert torch.equal(lse.double(), want) and torch.equal(loss.double(), want - z.gather(1, t[:, None])[:, 0])
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    smat.smat_linear_xent_grad(x, w, t, lse, dx=dx, dw=dw)
+    dz = torch.zeros(m, n, device=DEV, dtype=torch.float64)
+    dz[:, 254] = 1.0
+    dz[torch.arange(m), t] -= 1.0
+    assert torch.equal(dx.double(), dz @ w.double())
+    want = dz.t().contiguous() @ x.double()      # multiples of 2^power, up to 600 of them
+    assert torch.equal(dw.double(), want.to(dw.dtype).double())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m", [3, 64, 600])
 def test_logits_without_a_number(dtype, m):
     """Logits of -inf have no probability; +inf and NaN spoil their rows and no others; huge logits do not overflow."""
