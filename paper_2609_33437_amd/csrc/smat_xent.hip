@@ -48,10 +48,11 @@ __global__ __launch_bounds__(kRowThreads) void k_xent_rows(XentArgs a, const flo
   if (threadIdx.x != 0) return;
 #pragma unroll
   for (int k = 1; k < kRowThreads / 64; ++k) join_stats(top, sum, tops[k], sums[k]);
-  const float lse = logf(sum) + top;
+  const float rest = logf(sum);
   const int64_t t = a.targets[i];
-  a.lse[i] = lse;
-  a.loss[i] = t == a.ignore ? 0.f : t < 0 || t >= a.n ? __builtin_nanf("") : lse - target_z[i];
+  a.lse[i] = rest + top;
+  // from the largest value on, not from lse, whose rounding may be larger than a small loss
+  a.loss[i] = t == a.ignore ? 0.f : t < 0 || t >= a.n ? __builtin_nanf("") : rest + (top - target_z[i]);
 }
 
 // Sum of the losses, rows that count and their mean, in one block and a fixed order, in fp64.

@@ -264,6 +264,25 @@ def test_padded_rows_without_a_number(dtype, m, n, k):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [2, 200])
+def test_small_losses_beside_large_logits(dtype, m):
+    """A target 8 above 255 equal logits of 1016 has a loss of log(1 + 255 exp(-8)), which the row's log sum, rounded by up to
+    2^-14, would hide."""
+    n, k = 256, 32
+    x, w = torch.zeros(m, k, device=DEV, dtype=DT[dtype]), torch.zeros(n, k, device=DEV, dtype=DT[dtype])
+    x[:, 0] = 8.0
+    w[:, 0] = 127.0
+    w[3, 0] = 128.0
+    t = torch.full((m,), 3, device=DEV)
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    smat.smat_linear_xent(x, w, t, loss, lse)
+    want = float(np.log1p(255 * np.exp(-8.0)))
+    # the terms beside the 1 sum to 0.09, each within 16 U; a thread adds up to 32 values to the 1, then at most 16 sums of others,
+    # each within U of 1.09; and the logarithm: below 52 U = 3.1e-6
+    assert float((loss.double() - want).abs().max()) < 4e-6
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m", [1, 3, 64, 600])
 @pytest.mark.parametrize("power", [0, 20, 31, 33, 60, 110])
 def test_logits_of_any_size(dtype, m, power):
