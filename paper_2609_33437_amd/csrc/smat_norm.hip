@@ -5,7 +5,7 @@
 //   dx = r (g - xh mean(g xh) - mean(g)) with g = dy w (rms: without mean(g)), dw = sum_rows dy xh, db = sum_rows dy
 //
 // Bound by HBM: the forward pass reads and writes a row once, the backward reads two and writes one: 16384 x 4096 bf16 takes
-// 44 us, 6.1 TB/s, and 76 us, 5.3 TB/s, with 5 us more to join the blocks' sums.  A row is held in
+// 44 us, 6.1 TB/s, and 79 us, 5.1 TB/s, with 5 us more to join the blocks' sums.  A row is held in
 // registers between its sums and its use, by 16 to 1024 threads with one or two eights of columns each, so the variance is
 // the sum of squared differences from the mean, not a difference of sums.  Statistics and sums are fp32.
 #include "smat_decoder.h"
@@ -452,11 +452,11 @@ int32_t norm_grad_blocks(int64_t m, int64_t n) {
   // 4.8 us so and 6.1 apart, of 16384 10.7 and 11.8; three 5.8 and 6.1, 13.3 and 11.8. A call with 8 x 64 takes 9.0 us, host
   // bound, and 13.2 with two launches.
   if (n <= kMaxHeld && blocks > 0 && blocks <= 2) return 1;
-  // One block a compute unit; two where each still has several turns, and rows are narrow enough for both blocks' registers.
-  // Replayed, with 256 and 512 blocks: 600 x 4096 13.5 and 17.5 us, 1024 x 2048 10.5 and 12.2, 2000 x 4096 18.2 and 19.1, 3000 x
-  // 12288 60 and 75, 12115 x 5544 82 and 87; 8192 x 512 11.8 and 11.1, 4096 x 2048 18.4 and 16.4, 10000 x 768 18.5 and 16.4,
-  // 16384 x 4096 80 and 81.
-  const int64_t most = n <= 4096 && blocks >= 2048 ? 512 : 256;
+  // One block a compute unit; two where rows are narrow and each block still has several turns.  Replayed on rows that are not in a
+  // cache, with the join, 256 and 512 blocks: 600 x 4096 14.3 and 18.1 us, 1024 x 2048 11.3 and 13.0, 3000 x 12288 72 and 83,
+  // 12115 x 5544 90 and 96, 16384 x 4096 87 and 89; 8192 x 512 14.4 and 13.2, 4096 x 2048 21.5 and 18.5, 10000 x 768 20.5 and
+  // 18.9.
+  const int64_t most = n <= 2048 && blocks >= 2048 ? 512 : 256;
   return (int32_t)(blocks < most ? blocks : most);
 }
 
