@@ -104,7 +104,8 @@ struct LinPlan {
   double us;         // estimated
 };
 // Element types by smat_dtype code: 0 = fp32, 1 = bf16.
-LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi);
+// With `like`, a plan of as many rows and as long sums, each row's sums are formed in that plan's order, to the same bits.
+LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan* like = nullptr);
 // Columns that one pair of a row's stats covers in a part of a plan.
 int64_t stat_columns(const LinPart& part);
 hipError_t launch_linear(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,

@@ -1337,6 +1337,37 @@ double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& p
   return least;
 }
 
+// The tiles of least time for the parts of another plan that sum in its order: the same number of groups and ranges share
+// r's stages.  kNever where a part has none.
+double choose_like(const LinPlan& like, const FormCost* costs, int count, const Sizes& z, LinPlan& plan) {
+  double sum = 0.0;
+  for (int p = 0; p < like.parts; ++p) {
+    const LinPart& q = like.part[p];
+    Sizes part = z;
+    part.i = q.rows;
+    double least = kNever;
+    if (q.form == kRows) {
+      least = kRowsStart + z.rows / kRowsRate[q.rows > 4 ? 3 : q.rows > 2 ? 2 : q.rows - 1];
+      plan.part[p] = q;
+    } else {
+      int32_t groups = 0;
+      for (const FormCost& f : kDirectCosts[0])
+        if (f.form == q.form) groups = f.groups;
+      for (int c = 0; c < count; ++c) {
+        const double us = costs[c].groups == groups ? time_of(costs[c], part, q.splits) : kNever;
+        if (us < least) {
+          least = us;
+          plan.part[p] = {q.rows, costs[c].form, q.splits};
+        }
+      }
+    }
+    if (least >= kNever) return kNever;
+    sum += least + (p ? 2.0 : 0.0);
+  }
+  plan.parts = like.parts;
+  return sum;
+}
+
 // An operand as it lies in memory: `rows` runs of `run` elements.
 struct Operand {
   const void* p;
@@ -1368,7 +1399,7 @@ int64_t stat_columns(const LinPart& part) {
   }
 }
 
-LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
+LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan* like) {
   const int bytes = dtype == 1 ? 2 : 4;
   const int64_t deep = 128 / bytes;
   LinPlan best{};
@@ -1392,13 +1423,16 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       moved += 2.0 * (double)o[k].rows * (double)o[k].run * bytes;
     }
   const int transposed = (p_transposed(epi) ? 1 : 0) + (q_transposed(epi) ? 1 : 0);  // operands
-  const double direct = dtype == 1 ? choose_parts(kDirectCosts[transposed], 6, z, best) : choose_parts(kFp32Costs, 3, z, best);
+  const auto choose_tiles = [&](const FormCost* costs, int count, LinPlan& plan) {
+    return like ? choose_like(*like, costs, count, z, plan) : choose_parts(costs, count, z, plan);
+  };
+  const double direct = dtype == 1 ? choose_tiles(kDirectCosts[transposed], 6, best) : choose_tiles(kFp32Costs, 3, best);
   double least = direct;
   best.direct = 1;
   if (off) {
     // copies on 16-byte rows first, or stages by way of registers: a launch and the bytes against slower stages
     LinPlan staged{};
-    const double through = dtype == 1 ? choose_parts(kStagedCosts[transposed], 2, z, staged) : choose_parts(kFp32StagedCosts, 2, z, staged);
+    const double through = dtype == 1 ? choose_tiles(kStagedCosts[transposed], 2, staged) : choose_tiles(kFp32StagedCosts, 2, staged);
     least = direct + 6.0 + moved / 5.0e6;
     if (wide || through <= least) {
       best = staged;
@@ -1407,8 +1441,9 @@ LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi) {
       best.pack = off;
     }
   }
+  if (least >= kNever && like) return linear_plan(a, dtype, epi);
   // few rows: the kernel that takes operands of any alignment without a copy
-  if ((epi == kEpiLayer || epi == kEpiXent || epi == kEpiXentGrad) && a.i <= kMaxRows && few_fit) {
+  if (!like && (epi == kEpiLayer || epi == kEpiXent || epi == kEpiXentGrad) && a.i <= kMaxRows && few_fit) {
     const double rate = kRowsRate[a.i > 4 ? 3 : a.i > 2 ? 2 : a.i - 1];
     if (kRowsStart + z.bytes / rate <= least) {
       least = kRowsStart + z.bytes / rate;

@@ -291,7 +291,7 @@ bool on_16_bytes(const void* p, int64_t ld, int64_t run, int64_t bytes) {
 constexpr int64_t kLowRows = 128;
 
 // The products' plans and the workspace where x and W are copied as `pack` says; their estimated microseconds.
-double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
+double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p, const LinPlan* like) {
   const int64_t bytes = dtype == 1 ? 2 : 4;
   char* base = reinterpret_cast<char*>(uintptr_t(1) << 20);  // a workspace's address, for its alignment
   double us = 0.0;
@@ -300,7 +300,7 @@ double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p) {
   for (int last = 0; last < 2; ++last) {
     const Piece q = piece_args(a, dtype, p, last ? p.pieces - 1 : 0, base);
     p.logits[last] = p.dx[last] = p.dw[last] = LinPlan{};
-    if (a.m > 0) p.logits[last] = linear_plan(q.logits, dtype, kEpiXentGrad);
+    if (a.m > 0) p.logits[last] = linear_plan(q.logits, dtype, kEpiXentGrad, like);
     if (a.m > 0 && a.k > 0 && a.dx) p.dx[last] = linear_plan(q.dx, dtype, kEpiSum);
     if (a.k > 0 && a.dw) p.dw[last] = linear_plan(q.dw, dtype, kEpiScaled);
     double piece = 0.0;
@@ -349,12 +349,18 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   XentGradArgs both = a;
   if (!a.dx) both.dx = a.dw;
   if (!a.dw) both.dw = a.dx;
-  double us = plan_products(both, dtype, p);
+  // In fp32 the logits' sums take the order of the losses' call.  What a logit lost there to rounding is in lse too, so exp(z - lse)
+  // of a probable class is exact to lse's rounding; by sums in another order it is off by both logits' (157 x 43584 x 2829:
+  // dW by 3.3e-6 of its norm, by 1.1e-6 so).  In bf16 the rounding of dz is larger.
+  LinPlan losses{};
+  if (dtype != 1 && a.m > 0) losses = xent_plan(XentArgs{a.x, a.w, a.ldx, a.ldw, a.m, a.n, a.k}, dtype).logits;
+  const LinPlan* like = losses.parts ? &losses : nullptr;
+  double us = plan_products(both, dtype, p, like);
   // rows of W off 16 bytes serve two products: a copy of each piece for both, where that is estimated to be faster
   if (a.m > 0 && a.k > 0 && !on_16_bytes(a.w, a.ldw, a.k, bytes)) {
     XentGradPlan q = p;
     q.pack = 1;
-    const double copied = plan_products(both, dtype, q);
+    const double copied = plan_products(both, dtype, q, like);
     if (copied < us) {
       us = copied;
       p = q;
@@ -365,7 +371,7 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   // less.  (2048 x 128256 x 4096, half of the rows without: losses and gradients 4.75 ms, 6.15 ms with
   // products over all rows.)
   p.some = a.k > 0 && !p.low && us > 50.0 * (10.0 + (double)a.m / 1000.0);
-  plan_products(a, dtype, p);
+  plan_products(a, dtype, p, like);
   return p;
 }
 

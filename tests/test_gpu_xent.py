@@ -263,6 +263,24 @@ def test_padded_rows_without_a_number(dtype, m, n, k):
     assert not loss[none].any() and not dx[none].any() and dx[~none].isnan().all()
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 900, 1001), (5, 2000, 1001), (8, 40000, 515), (40, 700, 515), (129, 9000, 130), (157, 43584, 2829),
+                                   (300, 50, 4001), (515, 3001, 769), (600, 20000, 1024), (2100, 1000, 333)])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_fp32_logits_are_the_same_in_both_calls(m, n, k, pad):
+    """Where a target has the whole probability an fp32 gradient is exactly zero: its logit is computed again to the same bits."""
+    gen = torch.Generator(DEV).manual_seed(3)
+    x, w = strided(m, k, "f32", pad), strided(n, k, "f32", pad, pad)
+    w.copy_(torch.randn(n, k, generator=gen, device=DEV))
+    t = torch.randint(0, n, (m,), generator=gen, device=DEV)
+    x.copy_(w[t] * (600.0 / k))          # logits of about 600, others within 600 / sqrt(k) times 6
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    smat.smat_linear_xent(x, w, t, loss, lse)
+    assert not loss.any()
+    dx, dw = torch.full((m, k), float("nan"), device=DEV), torch.full((n, k), float("nan"), device=DEV)
+    smat.smat_linear_xent_grad(x, w, t, lse, dx=dx, dw=dw)
+    assert not dx.any() and not dw.any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m", [2, 200])
 def test_small_losses_beside_large_logits(dtype, m):
