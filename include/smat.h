@@ -743,7 +743,7 @@ smat_status smat_embed_grad(const smat_embed_grad_args* args, void* workspace, s
 
 /* Arguments of smat_linear_xent: the cross entropy of the logits z = x W^T against targets, without storing z.
  *   lse[i] = log sum_j exp z[i][j], loss[i] = lse[i] - z[i][targets[i]]
- * A target of ignore_index marks a row without one: its loss is 0.  Another target outside [0, n) gives a loss of NaN. */
+ * lse_low[i] is what rounding lse[i] to fp32 left of it (0 where lse[i] is not finite).  A target of ignore_index marks a row without one: its loss is 0.  Another target outside [0, n) gives a loss of NaN. */
 typedef struct smat_linear_xent_args {
   int32_t dtype, reserved; /* smat_dtype of x and w; reserved must be 0 */
   int64_t m, n, k;         /* rows, classes (> 0), width */
@@ -757,6 +757,7 @@ typedef struct smat_linear_xent_args {
   float* lse;              /* [m] */
   float* totals;           /* [3], or NULL: the sum of the losses, the number of rows with a target, and their quotient
                               (NaN where there is none) */
+  float* lse_low;          /* [m], or NULL */
 } smat_linear_xent_args;
 
 /* smat_linear_xent -- an output layer with its loss, from single tokens (m = 1) up.  Errors: SMAT_ERR_INVALID,
@@ -768,6 +769,8 @@ smat_status smat_linear_xent(const smat_linear_xent_args* args, void* workspace,
 /* Arguments of smat_linear_xent_grad: the gradients of s * sum_i row_scale[i] loss[i],
  *   dz[i][j] = (exp(z[i][j] - lse[i]) - [j = targets[i]]) row_scale[i]      0 in rows without a target
  *   dx = s dz W,  dW = s dz^T x,  s = scale[0] / totals[1]
+ * The log sum is lse + lse_low.  With lse alone every probability of a row is off by lse's rounding, 2^-24 |lse| of itself, and
+ * the dz of a target whose probability is within that of 1 is lost; with both such rows keep theirs.
  * Rows without a target take no part, whatever x, lse and row_scale hold in them, and their rows of dx are zeros.  The
  * vocabulary is taken in pieces: z is computed again and dz, rounded to dtype, held for one piece (in the workspace), so
  * nothing of the size m * n is stored.  s multiplies the fp32 sums; it is 0 where totals[1] is. */
@@ -788,6 +791,7 @@ typedef struct smat_linear_xent_grad_args {
   int64_t lddx;
   void* dw;                /* [n, k], or NULL */
   int64_t lddw;
+  const float* lse_low;    /* [m], as smat_linear_xent wrote it, or NULL: zeros */
 } smat_linear_xent_grad_args;
 
 /* smat_linear_xent_grad -- the gradients of an output layer from its loss.  Errors: SMAT_ERR_INVALID, SMAT_ERR_DTYPE,

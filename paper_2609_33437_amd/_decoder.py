@@ -122,7 +122,7 @@ def smat_embed_grad(dy, ids, dtable, scale: float = 1.0, padding_idx=None, accum
 
 
 # ------------------------------------------------------------------ output layer
-def _xent(a, x, w, targets, lse, totals):
+def _xent(a, x, w, targets, lse, totals, lse_low):
     torch = _torch()
     m, k = x.shape
     n = w.shape[0] if w.dim() == 2 else -1
@@ -134,25 +134,29 @@ def _xent(a, x, w, targets, lse, totals):
     a.lse = _typed(lse, m, torch.float32, device, "lse")
     if totals is not None:
         a.totals = _typed(totals, 3, torch.float32, device, "totals")
+    if lse_low is not None:
+        a.lse_low = _typed(lse_low, m, torch.float32, device, "lse_low")
     return m, n, k, device
 
 
-def smat_linear_xent(x, w, targets, loss, lse, totals=None, ignore_index: int = -100, workspace=None, stream=None) -> None:
+def smat_linear_xent(x, w, targets, loss, lse, totals=None, ignore_index: int = -100, workspace=None, stream=None,
+                     lse_low=None) -> None:
     """loss[i] = lse[i] - z[i, targets[i]] with z = x w^T and lse[i] = log sum_j exp z[i, j], without storing z; totals (fp32
-    [3]) = the losses' sum, the number of rows with a target, and their mean."""
+    [3]) = the losses' sum, the number of rows with a target, and their mean.  lse_low (fp32 [m]) = what rounding lse left."""
     a = smat_linear_xent_args(dtype=_first(x, "x"), ignore_index=int(ignore_index))
-    m, _, _, device = _xent(a, x, w, targets, lse, totals)
+    m, _, _, device = _xent(a, x, w, targets, lse, totals, lse_low)
     a.loss = _typed(loss, m, _torch().float32, device, "loss")
     L = lib()
     _call(L.smat_linear_xent, L.smat_linear_xent_workspace_bytes, a, workspace, device, stream)
 
 
 def smat_linear_xent_grad(x, w, targets, lse, dx=None, dw=None, row_scale=None, scale=None, totals=None,
-                          ignore_index: int = -100, workspace=None, stream=None) -> None:
+                          ignore_index: int = -100, workspace=None, stream=None, lse_low=None) -> None:
     """The gradients of scale / totals[1] * sum_i row_scale[i] loss[i] (row_scale fp32 [m], scale fp32 [1] on the GPU; without
-    them and totals 1), from the lse that smat_linear_xent wrote."""
+    them and totals 1), from the lse and lse_low that smat_linear_xent wrote.  Without lse_low rows whose target has nearly the
+    whole probability have gradients of lse's rounding."""
     a = smat_linear_xent_grad_args(dtype=_first(x, "x"), ignore_index=int(ignore_index))
-    m, n, k, device = _xent(a, x, w, targets, lse, totals)
+    m, n, k, device = _xent(a, x, w, targets, lse, totals, lse_low)
     f32 = _torch().float32
     if row_scale is not None:
         a.row_scale = _typed(row_scale, m, f32, device, "row_scale")

@@ -138,14 +138,15 @@ class smat_embed_grad_args(ctypes.Structure):
 class smat_linear_xent_args(ctypes.Structure):
     _fields_ = [("dtype", c_int32), ("reserved", c_int32), ("m", c_int64), ("n", c_int64), ("k", c_int64),
                 ("x", c_void_p), ("ldx", c_int64), ("w", c_void_p), ("ldw", c_int64), ("targets", c_void_p),
-                ("ignore_index", c_int64), ("loss", c_void_p), ("lse", c_void_p), ("totals", c_void_p)]
+                ("ignore_index", c_int64), ("loss", c_void_p), ("lse", c_void_p), ("totals", c_void_p), ("lse_low", c_void_p)]
 
 
 class smat_linear_xent_grad_args(ctypes.Structure):
     _fields_ = [("dtype", c_int32), ("reserved", c_int32), ("m", c_int64), ("n", c_int64), ("k", c_int64),
                 ("x", c_void_p), ("ldx", c_int64), ("w", c_void_p), ("ldw", c_int64), ("targets", c_void_p),
                 ("ignore_index", c_int64), ("lse", c_void_p), ("row_scale", c_void_p), ("scale", c_void_p),
-                ("totals", c_void_p), ("dx", c_void_p), ("lddx", c_int64), ("dw", c_void_p), ("lddw", c_int64)]
+                ("totals", c_void_p), ("dx", c_void_p), ("lddx", c_int64), ("dw", c_void_p), ("lddw", c_int64),
+                ("lse_low", c_void_p)]
 
 
 class SmatError(RuntimeError):

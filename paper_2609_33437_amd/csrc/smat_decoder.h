@@ -87,6 +87,7 @@ struct XentArgs {
   int64_t ignore;
   float* loss;
   float* lse;
+  float* lse_low;  // or NULL
   float* totals;  // sum of the losses, rows that count, their mean; or NULL
 };
 struct XentPlan {
@@ -103,6 +104,7 @@ struct XentGradArgs {
   const int64_t* targets;
   int64_t ignore;
   const float* lse;
+  const float* lse_low;  // or NULL
   const float* row_scale;
   const float* scale;
   const float* totals;

@@ -136,11 +136,13 @@ smat_status xent_call(const smat_linear_xent_args* g, XentCall* c, const char* w
   arrays.vector("loss", g->loss, g->m, 4, true);
   arrays.vector("lse", g->lse, g->m, 4, true);
   if (g->totals) arrays.vector("totals", g->totals, 3, 4, true);
+  if (g->lse_low) arrays.vector("lse_low", g->lse_low, g->m, 4, true);
   arrays.add(matrix("x", g->x, g->m, g->k, g->ldx, g->dtype));
   arrays.add(matrix("w", g->w, g->n, g->k, g->ldw, g->dtype));
   arrays.vector("targets", g->targets, g->m, 8);
   if (smat_status st = arrays.check(where)) return st;
-  c->a = XentArgs{g->x, g->w, g->ldx, g->ldw, g->m, g->n, g->k, g->targets, g->ignore_index, g->loss, g->lse, g->totals};
+  c->a = XentArgs{g->x, g->w, g->ldx, g->ldw, g->m, g->n, g->k, g->targets, g->ignore_index, g->loss, g->lse, g->lse_low,
+                  g->totals};
   c->plan = xent_plan(c->a, g->dtype);
   return SMAT_OK;
 }
@@ -164,12 +166,13 @@ smat_status xent_grad_call(const smat_linear_xent_grad_args* g, XentGradCall* c,
   arrays.add(matrix("w", g->w, g->n, g->k, g->ldw, g->dtype));
   arrays.vector("targets", g->targets, g->m, 8);
   arrays.vector("lse", g->lse, g->m, 4);
+  if (g->lse_low) arrays.vector("lse_low", g->lse_low, g->m, 4);
   if (g->row_scale) arrays.vector("row_scale", g->row_scale, g->m, 4);
   if (g->scale) arrays.vector("scale", g->scale, 1, 4);
   if (g->totals) arrays.vector("totals", g->totals, 3, 4);
   if (smat_status st = arrays.check(where)) return st;
-  c->a = XentGradArgs{g->x, g->w, g->ldx, g->ldw, g->m, g->n, g->k, g->targets, g->ignore_index, g->lse, g->row_scale, g->scale,
-                      g->totals, g->dx, g->lddx, g->dw, g->lddw};
+  c->a = XentGradArgs{g->x, g->w, g->ldx, g->ldw, g->m, g->n, g->k, g->targets, g->ignore_index, g->lse, g->lse_low, g->row_scale,
+                      g->scale, g->totals, g->dx, g->lddx, g->dw, g->lddw};
   c->plan = xent_grad_plan(c->a, g->dtype);
   return SMAT_OK;
 }

@@ -61,13 +61,14 @@ struct LinArgs {
   int64_t ldup;
   int32_t act;
   // cross entropy of logits v, columns col0 .. col0 + j of `classes` ones: the largest value and the sum of exponentials of
-  // each tile's columns of a row, and the target's logit; or out = (exp(v - lse) - [column is the target]) row_scale
+  // each tile's columns of a row, and the target's logit; or out = (exp(v - lse - lse_low) - [column is the target]) row_scale
   const int64_t* targets;
   int64_t ignore, classes, col0;
   float* stats;  // [i][stat_ld][2]
   int64_t stat_ld;
   float* target_z;
   const float* lse;
+  const float* lse_low;    // NULL: 0
   const float* row_scale;  // NULL: 1
   void* out_low;  // what rounding out to bf16 left, in bf16; or NULL
   // out = s (v + sum_in), zeros in rows without a target (targets not NULL), or sum_out = v + sum_in (NULL: 0), with s = scale[0] / totals[1] (NULL: 1)

@@ -1510,6 +1510,7 @@ LinArgs rows_of(LinArgs a, int64_t from, int64_t rows, int bytes, bool pt) {
   a.targets = static_cast<const int64_t*>(skip_bytes(a.targets, from * 8));
   a.target_z = static_cast<float*>(skip_bytes(a.target_z, from * 4));
   a.lse = static_cast<const float*>(skip_bytes(a.lse, from * 4));
+  a.lse_low = static_cast<const float*>(skip_bytes(a.lse_low, from * 4));
   a.row_scale = static_cast<const float*>(skip_bytes(a.row_scale, from * 4));
   a.sum_in = static_cast<const float*>(skip_bytes(a.sum_in, from * a.ldsum * 4));
   a.sum_out = static_cast<float*>(skip_bytes(a.sum_out, from * a.ldsum * 4));

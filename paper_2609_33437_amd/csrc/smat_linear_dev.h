@@ -346,7 +346,7 @@ struct Side<T, kEpiXent> {
 template <typename T>
 struct Side<T, kEpiXentGrad> {
   int64_t target;
-  float lse, scale;
+  float lse, low, scale;
 };
 template <typename T>
 struct Side<T, kEpiSum> {
@@ -457,6 +457,7 @@ __device__ __forceinline__ void side_load(const LinArgs& a, int64_t i, int64_t j
     if (WHOLE || i < a.i) {
       s.target = a.targets[i];
       s.lse = a.lse[i];
+      s.low = a.lse_low ? a.lse_low[i] : 0.f;
       s.scale = a.row_scale ? a.row_scale[i] : 1.f;
     }
   }
@@ -501,6 +502,14 @@ struct StatExp {
       return __builtin_amdgcn_exp2f((v - top) * 1.44269504088896340736f);
   }
 };
+// exp(v - lse - low), low being what lse's rounding left: up to 13 where logits are so large, and most often far below 1.
+template <typename T>
+__device__ __forceinline__ float grad_exp(float v, float lse, float low) {
+  if constexpr (El<T>::kBytes == 4)
+    return expf((v - lse) - low);
+  else
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(v - lse, 1.44269504088896340736f, low * -1.44269504088896340736f));
+}
 // (top, sum) of two sets of values: sum = sum exp(v - top), and exp(v - 0) where there is only -inf.
 __device__ __forceinline__ void join_stats(float& top, float& sum, float other_top, float other_sum) {
   const float t = fmaxf(top, other_top), from = t == -__builtin_inff() ? 0.f : t;
@@ -581,11 +590,17 @@ __device__ __forceinline__ void epilogue8(const LinArgs& a, int64_t i, int64_t j
       for (int e = 0; e < 8; ++e) v[e] = 0.f;
     } else {
       const int at = target_place(a, s.target, j0);
+      float hit = 0.f;
+      if (at >= 0) {  // one eight of a row: expm1 keeps what p - 1 would lose where p is nearly 1
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = act_exp<T>(v[e] - s.lse) * scale;
-      if (at >= 0) {  // one eight of a row
+        for (int e = 0; e < 8; ++e) hit = e == at ? v[e] : hit;
+        hit = expm1f((hit - s.lse) - s.low) * scale;
+      }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] -= e == at ? scale : 0.f;
+      for (int e = 0; e < 8; ++e) v[e] = grad_exp<T>(v[e], s.lse, s.low) * scale;
+      if (at >= 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e == at ? hit : v[e];
       }
     }
     if (!WHOLE) {

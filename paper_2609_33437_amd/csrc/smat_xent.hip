@@ -3,6 +3,10 @@
 //   lse_i = log sum_j exp z_ij,  loss_i = lse_i - z_i,t_i
 //   dz_ij = (exp(z_ij - lse_i) - [j = t_i]) g_i,  dx = s dz W,  dW = s dz^T x
 //
+// lse is the largest logit plus a log between 0 and log n, and where logits are in the hundreds its rounding to fp32 exceeds
+// 1 - p of a target that has nearly the whole probability.  So it is held as two fp32 numbers, and p - 1 is an expm1 of
+// their difference from the logit: such a row's dz keeps its digits down to 1 - p of 2^-24, and sums to 0.
+//
 // The forward product's epilogue leaves the largest value and the sum of exponentials of each tile's columns of a row, which
 // k_xent_rows joins.  The gradient goes through the vocabulary in pieces: a piece's logits again, turned into dz (in the
 // call's dtype) by their epilogue, then dz W added to dx in fp32 and dz^T x, which is the piece's part of dW.  So beside
@@ -50,7 +54,12 @@ __global__ __launch_bounds__(kRowThreads) void k_xent_rows(XentArgs a, const flo
   for (int k = 1; k < kRowThreads / 64; ++k) join_stats(top, sum, tops[k], sums[k]);
   const float rest = logf(sum);
   const int64_t t = a.targets[i];
-  a.lse[i] = rest + top;
+  const float lse = rest + top;
+  a.lse[i] = lse;
+  if (a.lse_low) {  // what the sum's rounding left, exactly
+    const float part = lse - top;
+    a.lse_low[i] = __builtin_isfinite(lse) ? (top - (lse - part)) + (rest - part) : 0.f;
+  }
   // from the largest value on, not from lse, whose rounding may be larger than a small loss
   a.loss[i] = t == a.ignore ? 0.f : t < 0 || t >= a.n ? __builtin_nanf("") : rest + (top - target_z[i]);
 }
@@ -146,6 +155,7 @@ namespace {
 struct SomeRows {
   int64_t* targets;
   float* lse;
+  float* lse_low;
   float* row_scale;
   int32_t* from;
   int32_t* place;
@@ -155,13 +165,14 @@ SomeRows some_rows(char* at, int64_t m) {
   SomeRows r{};
   r.targets = reinterpret_cast<int64_t*>(at);
   r.lse = reinterpret_cast<float*>(r.targets + m);
-  r.row_scale = r.lse + m;
+  r.lse_low = r.lse + m;
+  r.row_scale = r.lse_low + m;
   r.from = reinterpret_cast<int32_t*>(r.row_scale + m);
   r.place = r.from + m;
   r.count = r.place + m;
   return r;
 }
-constexpr int64_t some_rows_bytes(int64_t m) { return m * 24 + 4; }
+constexpr int64_t some_rows_bytes(int64_t m) { return m * 28 + 4; }
 
 __global__ __launch_bounds__(1024) void k_xent_some(XentGradArgs a, SomeRows r) {
   __shared__ int32_t waves[2][16];
@@ -186,6 +197,7 @@ __global__ __launch_bounds__(1024) void k_xent_some(XentGradArgs a, SomeRows r) 
       r.from[at] = (int32_t)i;
       r.targets[at] = t;
       r.lse[at] = a.lse[i];
+      if (a.lse_low) r.lse_low[at] = a.lse_low[i];
       if (a.row_scale) r.row_scale[at] = a.row_scale[i];
     }
   }
@@ -249,6 +261,7 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
   q.logits.classes = a.n;
   q.logits.col0 = from;
   q.logits.lse = a.lse;
+  q.logits.lse_low = a.lse_low;
   q.logits.row_scale = a.row_scale;
   q.dx.prod[0] = LinProduct{dz, w, plan.width, ldw, width, true};
   if (low) q.dx.prod[1] = LinProduct{low, w, plan.width, ldw, width, true};
@@ -266,6 +279,7 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
     const SomeRows r = some_rows(ws + plan.rows, a.m);
     q.logits.targets = r.targets;
     q.logits.lse = r.lse;
+    if (a.lse_low) q.logits.lse_low = r.lse_low;
     if (a.row_scale) q.logits.row_scale = r.row_scale;
     q.dx.out_rows = r.from;
     q.logits.count = q.dx.count = q.dw.count = r.count;

@@ -314,7 +314,7 @@ class _LinearXent(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, w, targets, ignore_index, reduction):
-        loss, lse, totals = _losses(x, w, targets, ignore_index, reduction)
+        loss, lse, totals = _losses(x, w, targets, ignore_index, reduction, True)
         ctx.ignore_index, ctx.reduction = ignore_index, reduction
         ctx.save_for_backward(x, w, targets, lse, totals)
         return loss if reduction == 0 else totals[2 * reduction - 2].clone()
@@ -328,17 +328,17 @@ class _LinearXent(torch.autograd.Function):
         dw = torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None
         grad = grad.contiguous()
         rows = ctx.reduction == 0
-        smat_linear_xent_grad(x, w, targets, lse, dx=dx, dw=dw, row_scale=grad if rows else None, scale=None if rows else grad,
-                              totals=totals if ctx.reduction == 2 else None, ignore_index=ctx.ignore_index)
+        smat_linear_xent_grad(x, w, targets, lse[0], dx=dx, dw=dw, row_scale=grad if rows else None, scale=None if rows else grad,
+                              totals=totals if ctx.reduction == 2 else None, ignore_index=ctx.ignore_index, lse_low=lse[1])
         return dx, dw, None, None, None
 
 
-def _losses(x, w, targets, ignore_index: int, reduction: int):
-    """(loss of each row, lse, totals or None)."""
+def _losses(x, w, targets, ignore_index: int, reduction: int, saved: bool):
+    """(loss of each row, lse and for gradients what its rounding left, totals or None)."""
     empty = dict(dtype=torch.float32, device=x.device)
-    loss, lse = torch.empty(x.shape[0], **empty), torch.empty(x.shape[0], **empty)
+    loss, lse = torch.empty(x.shape[0], **empty), torch.empty(2 if saved else 1, x.shape[0], **empty)
     totals = torch.empty(3, **empty) if reduction else None
-    smat_linear_xent(x, w, targets, loss, lse, totals=totals, ignore_index=ignore_index)
+    smat_linear_xent(x, w, targets, loss, lse[0], totals=totals, ignore_index=ignore_index, lse_low=lse[1] if saved else None)
     return loss, lse, totals
 
 
@@ -473,7 +473,7 @@ def linear_cross_entropy(x, weight, targets, ignore_index: int = -100, reduction
     if _saves(x, weight):
         loss = _LinearXent.apply(x, weight, flat, int(ignore_index), how)
     else:
-        loss, _, totals = _losses(x, weight, flat, int(ignore_index), how)
+        loss, _, totals = _losses(x, weight, flat, int(ignore_index), how, False)
         if how:
             loss = totals[2 * how - 2]
     return loss.view(targets.shape) if how == 0 else loss

@@ -1,0 +1,88 @@
+"""Gradients of the output layer's loss where a row's target has nearly the whole probability, against the definition: the
+term p - 1 of the target is then far smaller than the rounding of the row's log sum or of its logits.
+
+The first test's logits are exact: 1016 for 255 classes and 1016 + margin for the target, so q = 1 - p = 255 exp(-margin) /
+(1 + 255 exp(-margin)).  With U = 2^-24, the row's sum of exponentials is 1 and at most 0.09 beside it, joined by at most 48
+additions, each within U, of exponentials within 2^-20 of themselves: within 50 U + 2^-20 q, and its logarithm likewise, which is the
+loss.  The log sum reaches the gradient as two numbers, within U of the smaller one, itself below 2^-14; so dz of the target, -q by
+expm1, and the other classes' together, q, are each off by at most e = 56 U + 2^-18 q.  In bf16 with more than 128 rows each
+dz is rounded, by at most 2^-8 of itself, and by 2^-16 with fewer; the products are fp32 sums of N terms, within (N + 16) 2^-23 of their
+magnitudes, and the outputs are rounded once."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_33437_amd import layers
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+U = 2.0 ** -24
+
+
+def confident(m, margin, dtype):
+    """x [m, 32], W [256, 32], target 3: its logit stands `margin` above 255 equal ones of 1016."""
+    x, w = torch.zeros(m, 32, device=DEV, dtype=DT[dtype]), torch.zeros(256, 32, device=DEV, dtype=DT[dtype])
+    x[:, 0], x[:, 1] = 8.0, 1.0
+    w[:, 0] = 127.0
+    w[3, 1] = margin
+    return x, w, torch.full((m,), 3, device=DEV)
+
+
+def check_confident(m, margin, dtype, dx, dw):
+    beside = 255 * np.exp(-float(margin))
+    q = beside / (1 + beside)
+    each = 0.0 if dtype == "f32" else 2.0 ** -16 if m <= 128 else 2.0 ** -8
+    out = U if dtype == "f32" else 2.0 ** -8
+    e = 56 * U + 2.0 ** -18 * q + each * q
+    dx, dw = dx.double(), dw.double()
+    # column 0 of dx: 127 times the sum of dz, which is 0
+    sums = (256 + 16) * 2.0 ** -23
+    assert float(dx[:, 0].abs().max()) <= (127 * (2 * e) + sums * 127 * 2 * (q + e)) * (1 + out)
+    # column 1: margin times dz of the target
+    err = margin * (e + sums * (q + e))
+    assert float((dx[:, 1] + margin * q).abs().max()) <= err + (margin * q + err) * out
+    assert not dx[:, 2:].any()
+    sums = (m + 16) * 2.0 ** -23
+    for column, by in ((0, 8.0), (1, 1.0)):
+        err = by * m * (e + sums * (q + e))
+        assert abs(float(dw[3, column]) + by * m * q) <= err + (by * m * q + err) * out
+        others = torch.cat([dw[:3, column], dw[4:, column]])
+        err /= 255
+        assert float((others - by * m * q / 255).abs().max()) <= err + (by * m * q / 255 + err) * out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 2, 64, 200, 600])
+@pytest.mark.parametrize("margin", [8, 12, 16])
+def test_confident_rows(dtype, m, margin):
+    x, w, t = confident(m, margin, dtype)
+    own = x.requires_grad_(), w.requires_grad_()
+    layers.linear_cross_entropy(*own, t, reduction="sum").backward()
+    check_confident(m, margin, dtype, own[0].grad, own[1].grad)
+    summed = own[0].grad, own[1].grad
+    own[0].grad = own[1].grad = None
+    layers.linear_cross_entropy(*own, t, reduction="none").sum().backward()
+    assert torch.equal(own[0].grad, summed[0]) and torch.equal(own[1].grad, summed[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 5, 200])
+def test_equal_logits_of_any_size(dtype, m):
+    """Two classes with the same logit, whatever its size, have half of the probability each: exp(-log 2) and expm1(-log 2) in
+    fp32 are within 2^-20 of that, and the products below have one term or, in columns of W, m equal ones."""
+    for power in (0, 12, 24, 31, 60):
+        x, w = torch.zeros(m, 16, device=DEV, dtype=DT[dtype]), torch.zeros(40, 16, device=DEV, dtype=DT[dtype])
+        x[:, 0], x[:, 1] = 2.0 ** power, 1.0
+        w[:, 0] = -1.0 if power > 8 else -256.0
+        w[5, 0] = w[9, 0] = 1.0
+        w[5, 1], w[9, 1] = 0.0, 0.0
+        w[5, 2], w[9, 3] = 1.0, 1.0
+        x.requires_grad_()
+        w.requires_grad_()
+        layers.linear_cross_entropy(x, w, torch.full((m,), 5, device=DEV), reduction="sum").backward()
+        tol = 2.0 ** -20 + (2.0 ** -8 * 2 if dtype == "bf16" else 0.0)
+        assert float((x.grad[:, 2].double() + 0.5).abs().max()) <= 0.5 * tol, power
+        assert float((x.grad[:, 3].double() - 0.5).abs().max()) <= 0.5 * tol, power
+        err = 0.5 * m * (tol + (m + 16) * 2.0 ** -23)
+        assert abs(float(w.grad[5, 1]) + 0.5 * m) <= err and abs(float(w.grad[9, 1]) - 0.5 * m) <= err, power
