@@ -1280,8 +1280,9 @@ double time_of(const FormCost& f, const Sizes& z, int64_t splits) {
   return sum;
 }
 
-// The least-time tile and number of ranges of r by those costs.  Ranges beyond one block a place only cost.
-double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part) {
+// The least-time tile and number of ranges of r by those costs, or with `only` so many ranges.  Ranges beyond one block a
+// place only cost.
+double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part, int64_t only = 0) {
   double least = kNever;
   part = {z.i, 0, 1};
   for (int c = 0; c < count; ++c) {
@@ -1290,7 +1291,8 @@ double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part) {
     int64_t most = slots / tiles + 1;
     if (most > kMostSplits) most = kMostSplits;
     if (most > z.stages / (2 * f.groups)) most = z.stages / (2 * f.groups);
-    for (int64_t splits = 1; splits == 1 || splits <= most; ++splits) {
+    if (only) most = only;
+    for (int64_t splits = only ? only : 1; splits == 1 || splits <= most; ++splits) {
       const double us = time_of(f, z, splits);
       if (us < least) {
         least = us;
@@ -1304,11 +1306,11 @@ double choose(const FormCost* costs, int count, const Sizes& z, LinPart& part) {
 // The same in one launch or two: rounds of blocks that fill every compute unit, then the rows that are left with the
 // tile that suits them, where that beats a last round of few blocks.  (4096 x 8960 x 1536 with a gated epilogue: three
 // rounds of 256 x 256 tiles, the last of 48, take 193 us, two rounds and the rest 179 us.)
-double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& plan) {
+double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& plan, int64_t only = 0) {
   constexpr double kWorthIt = 15.0, kLaunch = 2.0;
-  double least = choose(costs, count, z, plan.part[0]);
+  double least = choose(costs, count, z, plan.part[0], only);
   plan.parts = 1;
-  if (least < kWorthIt) return least;
+  if (least < kWorthIt || only > 1) return least;
   for (int c = 0; c < count; ++c) {
     const FormCost& f = costs[c];
     const int64_t across = div_up(z.j, f.j), slots = (int64_t)kComputeUnits * f.resident;
@@ -1318,7 +1320,7 @@ double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& p
     first.i = rows;
     rest.i = z.i - rows;
     LinPart other;
-    double after = choose(costs, count, rest, other);
+    double after = choose(costs, count, rest, other, only);
     if (z.rows > 0.0 && rest.i <= kMaxRows) {
       const double few = kRowsStart + z.rows / kRowsRate[rest.i > 4 ? 3 : rest.i > 2 ? 2 : rest.i - 1];
       if (few < after) {
@@ -1337,9 +1339,27 @@ double choose_parts(const FormCost* costs, int count, const Sizes& z, LinPlan& p
   return least;
 }
 
-// The tiles of least time for the parts of another plan that sum in its order: the same number of groups and ranges share
-// r's stages.  kNever where a part has none.
+// Groups of a tile, 0 for the kernel for few rows.
+int32_t groups_of(int32_t form) {
+  for (const FormCost& f : kDirectCosts[0])
+    if (f.form == form) return f.groups;
+  return 0;
+}
+bool same_order(const LinPart& a, const LinPart& b) { return groups_of(a.form) == groups_of(b.form) && a.splits == b.splits; }
+
+// The tiles of least time that sum in another plan's order: the same number of groups and ranges share r's stages, whatever
+// the tile.  Where its parts sum in different orders each keeps its rows.  kNever where there are none.
 double choose_like(const LinPlan& like, const FormCost* costs, int count, const Sizes& z, LinPlan& plan) {
+  const int32_t all = groups_of(like.part[0].form);
+  if (all > 0 && (like.parts == 1 || same_order(like.part[0], like.part[1]))) {
+    FormCost same[6];
+    int some = 0;
+    for (int c = 0; c < count; ++c)
+      if (costs[c].groups == all) same[some++] = costs[c];
+    Sizes tiles = z;
+    tiles.rows = 0.0;
+    return choose_parts(same, some, tiles, plan, like.part[0].splits);
+  }
   double sum = 0.0;
   for (int p = 0; p < like.parts; ++p) {
     const LinPart& q = like.part[p];
@@ -1350,9 +1370,7 @@ double choose_like(const LinPlan& like, const FormCost* costs, int count, const 
       least = kRowsStart + z.rows / kRowsRate[q.rows > 4 ? 3 : q.rows > 2 ? 2 : q.rows - 1];
       plan.part[p] = q;
     } else {
-      int32_t groups = 0;
-      for (const FormCost& f : kDirectCosts[0])
-        if (f.form == q.form) groups = f.groups;
+      const int32_t groups = groups_of(q.form);
       for (int c = 0; c < count; ++c) {
         const double us = costs[c].groups == groups ? time_of(costs[c], part, q.splits) : kNever;
         if (us < least) {

@@ -363,11 +363,12 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   XentGradArgs both = a;
   if (!a.dx) both.dx = a.dw;
   if (!a.dw) both.dw = a.dx;
-  // In fp32 the logits' sums take the order of the losses' call.  What a logit lost there to rounding is in lse too, so exp(z - lse)
-  // of a probable class is exact to lse's rounding; by sums in another order it is off by both logits' (157 x 43584 x 2829:
-  // dW by 3.3e-6 of its norm, by 1.1e-6 so).  In bf16 the rounding of dz is larger.
+  // The logits' sums take the order of the losses' call.  What a logit lost there to rounding is in the log sum too, so
+  // exp(z - lse) of a probable class is exact; by sums in another order it is off by both logits' (fp32 157 x 43584 x 2829: dW by
+  // 3.3e-6 of its norm, by 1.1e-6 so; bf16 2100 x 60000 x 2048 with targets of logit 600 and probability 1: dx, which is 0, up to
+  // 1.7e-3 in the 52 rows left over for another tile).
   LinPlan losses{};
-  if (dtype != 1 && a.m > 0) losses = xent_plan(XentArgs{a.x, a.w, a.ldx, a.ldw, a.m, a.n, a.k}, dtype).logits;
+  if (a.m > 0) losses = xent_plan(XentArgs{a.x, a.w, a.ldx, a.ldw, a.m, a.n, a.k}, dtype).logits;
   const LinPlan* like = losses.parts ? &losses : nullptr;
   double us = plan_products(both, dtype, p, like);
   // rows of W off 16 bytes serve two products: a copy of each piece for both, where that is estimated to be faster

@@ -12,6 +12,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2609_33437_amd as smat
 from paper_2609_33437_amd import layers
 
 pytestmark = pytest.mark.gpu
@@ -86,3 +87,31 @@ def test_equal_logits_of_any_size(dtype, m):
         assert float((x.grad[:, 3].double() - 0.5).abs().max()) <= 0.5 * tol, power
         err = 0.5 * m * (tol + (m + 16) * 2.0 ** -23)
         assert abs(float(w.grad[5, 1]) + 0.5 * m) <= err and abs(float(w.grad[9, 1]) - 0.5 * m) <= err, power
+
+
+# tiles alone, with rows left over for other tiles or for the kernel for few rows, ranges of k
+SAME = [("bf16", 1, 900, 1001), ("bf16", 5, 2000, 1001), ("bf16", 8, 40000, 512), ("bf16", 40, 700, 2048), ("bf16", 129, 9000, 130),
+        ("bf16", 157, 43584, 2829), ("bf16", 300, 50, 4001), ("bf16", 515, 32003, 769), ("bf16", 515, 32003, 2048),
+        ("bf16", 1283, 128256, 1024), ("bf16", 2100, 60000, 2048), ("bf16", 3001, 50257, 768), ("bf16", 700, 1000, 4096),
+        ("f32", 515, 32003, 769), ("f32", 157, 43584, 2829), ("f32", 1030, 20001, 770), ("f32", 259, 30000, 1024)]
+
+
+def check_same_logits(dtype, m, n, k, ignored=0.0):
+    """Where a target has the whole probability a gradient is exactly zero, if its logit is computed again to the same bits."""
+    gen = torch.Generator(DEV).manual_seed(3)
+    w = torch.randn(n, k, generator=gen, device=DEV).to(DT[dtype])
+    t = torch.randint(0, n, (m,), generator=gen, device=DEV)
+    x = (w[t].float() * (600.0 / k)).to(DT[dtype])          # logits of about 600, others within 600 / sqrt(k) times 6
+    t[torch.rand(m, generator=gen, device=DEV) < ignored] = -100
+    loss, lse, low = (torch.empty(m, device=DEV) for _ in range(3))
+    smat.smat_linear_xent(x, w, t, loss, lse, lse_low=low)
+    assert not loss.any() and not low.any()
+    dx, dw = torch.full_like(x, float("nan")), torch.full_like(w, float("nan"))
+    smat.smat_linear_xent_grad(x, w, t, lse, dx=dx, dw=dw, lse_low=low)
+    rows = dx.any(1)
+    assert not rows.any() and not dw.any(), f"{int(rows.sum())} rows, dx up to {float(dx.abs().max())} beside W of {float(w.abs().max())}"
+
+
+@pytest.mark.parametrize("dtype,m,n,k", SAME)
+def test_logits_are_the_same_in_both_calls(dtype, m, n, k):
+    check_same_logits(dtype, m, n, k)
