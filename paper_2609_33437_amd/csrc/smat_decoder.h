@@ -119,6 +119,7 @@ struct XentGradPlan {
   int32_t pack;  // each piece of W is copied to 16-byte rows for its products; x always is
   int32_t low;   // what rounding dz to bf16 leaves is kept too, behind dz, and multiplied
   int32_t some;  // the products take the rows with a target only, in order; x is copied so
+  int64_t first;  // with `some`: the logits' first part has so many rows, which stay its own; 0: any row may be in either part
   LinPlan logits[2], dx[2], dw[2];  // of a whole piece and of the last one
   size_t dz, sum, x, w, rows, workspace;  // behind the products' own
 };

@@ -82,6 +82,9 @@ struct LinArgs {
   const int32_t* count;
   const int32_t* out_rows;
   int64_t row_from;
+  // of kEpiXentGrad in two parts that sum in different orders: how many of `count` are the first part's, or NULL: as many as it
+  // has rows.  The second part's follow them.
+  const int32_t* first_count;
   // of kEpiSum: rows of a tile and the ranges of r that may be made, for fewer rows than planned; the block's own range
   int32_t tile_rows, most_splits, range;
   // sums of `splits` ranges of r, joined by a second kernel: [splits][i][j rounded up to 8] fp32
@@ -107,6 +110,8 @@ struct LinPlan {
 // Element types by smat_dtype code: 0 = fp32, 1 = bf16.
 // With `like`, a plan of as many rows and as long sums, each row's sums are formed in that plan's order, to the same bits.
 LinPlan linear_plan(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan* like = nullptr);
+// Whether a plan's parts sum in the same order.
+bool one_order(const LinPlan& plan);
 // Columns that one pair of a row's stats covers in a part of a plan.
 int64_t stat_columns(const LinPart& part);
 hipError_t launch_linear(const LinArgs& a, int dtype, LinEpilogue epi, const LinPlan& plan, void* workspace,

@@ -528,7 +528,7 @@ __global__ __launch_bounds__(kFastThreads, 2) void k_linear_fast(LinArgs a) {
   extern __shared__ char smem[];  // [stage parity][P half 0, P half 1, Q half 0, Q half 1]
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
   uint32_t ti, tj;
-  if (without_rows<EPI>(a)) return;
+  if (without_rows<T, EPI>(a)) return;
   if (!tile_place<EPI>(a, kFastB, kFastB, ti, tj)) return;
   const int64_t i0 = (int64_t)ti * kFastB, j0 = (int64_t)tj * kFastB;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave / 4 * 64, wj = wave % 4 * 32;
@@ -672,7 +672,7 @@ __global__ __launch_bounds__(S::kThreads, S::kSimdWaves) void k_linear_group(Lin
   extern __shared__ char smem[];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), group = wave / kWaves, w = wave % kWaves;
   uint32_t ti, tj;
-  if (without_rows<EPI>(a)) return;
+  if (without_rows<T, EPI>(a)) return;
   if (!tile_place<EPI>(a, S::kI, S::kJ, ti, tj)) return;
   const int64_t i0 = (int64_t)ti * S::kI, j0 = (int64_t)tj * S::kJ;
   const int wi = w / S::WJ * S::TI, wj = w % S::WJ * S::TJ;
@@ -916,7 +916,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
   constexpr int kChunk = 16 / El<T>::kBytes, kGroups = kRowsWaves * kRowsEach / JB, kValues = kRowsEach * M;
   constexpr int kStep = 64 * kChunk, kAhead = M <= 2 ? 4 : 2;
   __shared__ float sums[kGroups][M][JB + 4];
-  if (without_rows<EPI>(a)) return;
+  if (without_rows<T, EPI>(a)) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   const int group = wave % kGroups, jrow = wave / kGroups * kRowsEach;
   const int64_t j0 = (int64_t)blockIdx.x * JB, r = a.prod[0].r;
@@ -1014,7 +1014,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_linear_rows(LinArgs a) {
 // 4096 x 2048 take 14 us, 6.2 TB/s.
 template <typename T, int EPI>
 __global__ __launch_bounds__(256) void k_linear_join(LinArgs a) {
-  if (without_rows<EPI>(a)) return;
+  if (without_rows<T, EPI>(a)) return;
   const int64_t eights = ((a.j + kCkptBlock - 1) / kCkptBlock) * 4, ld = (a.j + 7) & ~(int64_t)7;
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t i = t / eights, j = (t - i * eights) * 8;
@@ -1351,7 +1351,7 @@ bool same_order(const LinPart& a, const LinPart& b) { return groups_of(a.form) =
 // the tile.  Where its parts sum in different orders each keeps its rows.  kNever where there are none.
 double choose_like(const LinPlan& like, const FormCost* costs, int count, const Sizes& z, LinPlan& plan) {
   const int32_t all = groups_of(like.part[0].form);
-  if (all > 0 && (like.parts == 1 || same_order(like.part[0], like.part[1]))) {
+  if (all > 0 && one_order(like)) {
     FormCost same[6];
     int some = 0;
     for (int c = 0; c < count; ++c)
@@ -1404,6 +1404,8 @@ void operands(const LinArgs& a, LinEpilogue epi, int bytes, Operand (&o)[4]) {
 }
 int64_t packed_ld(int64_t run, int bytes) { return div_up(run * bytes, 16) * 16 / bytes; }
 }  // namespace
+
+bool one_order(const LinPlan& plan) { return plan.parts < 2 || same_order(plan.part[0], plan.part[1]); }
 
 int64_t stat_columns(const LinPart& part) {
   if (part.splits > 1) return kCkptBlock;  // as the join writes them

@@ -378,8 +378,20 @@ __device__ __forceinline__ uint32_t range_of(const LinArgs& a) {
   return EPI == kEpiSum ? (uint32_t)a.range : blockIdx.y;
 }
 
+// Rows of the logits' gradient further up, of all that a part reads and writes by row.
+template <typename T>
+__device__ __forceinline__ void move_rows(LinArgs& a, int64_t by) {
+  using Mem = typename El<T>::Mem;
+  a.prod[0].p = static_cast<const Mem*>(a.prod[0].p) + by * a.prod[0].ldp;
+  a.out = static_cast<Mem*>(a.out) + by * a.ldout;
+  a.targets += by;
+  a.lse += by;
+  if (a.lse_low) a.lse_low += by;
+  if (a.row_scale) a.row_scale += by;
+}
+
 // Products of which only some rows are there (LinArgs::count): sets their number, and says whether there are none.
-template <int EPI>
+template <typename T, int EPI>
 __device__ __forceinline__ bool without_rows(LinArgs& a) {
   if constexpr (EPI == kEpiXentGrad || EPI == kEpiSum || EPI == kEpiScaled) {
     if (a.count) {
@@ -388,7 +400,19 @@ __device__ __forceinline__ bool without_rows(LinArgs& a) {
         if (rows < a.prod[0].r) a.prod[0].r = rows;
       } else {
         const int64_t planned = a.i;
-        if (rows - a.row_from < a.i) a.i = rows - a.row_from;
+        int64_t from = a.row_from, end = rows;
+        if constexpr (EPI == kEpiXentGrad) {
+          if (a.first_count) {
+            const int64_t first = *a.first_count;
+            if (from == 0) {
+              end = first;
+            } else {
+              move_rows<T>(a, first - from);
+              from = first;
+            }
+          }
+        }
+        if (end - from < a.i) a.i = end - from;
         if (a.i <= 0) return true;
         if constexpr (EPI == kEpiSum) {
           if (a.splits > 1) a.splits = more_splits(a, planned);

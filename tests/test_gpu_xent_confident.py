@@ -14,6 +14,7 @@ import torch
 
 import paper_2609_33437_amd as smat
 from paper_2609_33437_amd import layers
+from test_gpu_xent import check_gradients, logits
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -115,3 +116,26 @@ def check_same_logits(dtype, m, n, k, ignored=0.0):
 @pytest.mark.parametrize("dtype,m,n,k", SAME)
 def test_logits_are_the_same_in_both_calls(dtype, m, n, k):
     check_same_logits(dtype, m, n, k)
+
+
+@pytest.mark.parametrize("dtype,m,n,k", [s for s in SAME if s[1] > 128] + [("f32", 771, 32003, 769), ("f32", 1027, 50304, 300)])
+@pytest.mark.parametrize("ignored", [0.1, 0.5, 0.99])
+def test_logits_are_the_same_without_some_rows(dtype, m, n, k, ignored):
+    """Rows without a target are left out of large products; the others stay with those that sum in their order."""
+    check_same_logits(dtype, m, n, k, ignored)
+
+
+@pytest.mark.parametrize("where", ["first", "last", "all_but_last", "one"])
+def test_a_part_without_rows(where):
+    """512 rows by tiles and 3 by the kernel for few rows, of which one part has no target."""
+    m, n, k = 515, 32003, 769
+    gen = torch.Generator(DEV).manual_seed(9)
+    x, w = torch.randn(m, k, generator=gen, device=DEV), torch.randn(n, k, generator=gen, device=DEV) * 0.1
+    t = torch.randint(0, n, (m,), generator=gen, device=DEV)
+    keep = torch.zeros(m, dtype=torch.bool, device=DEV)
+    keep[{"first": slice(0, 512), "last": slice(512, 515), "all_but_last": slice(0, 514), "one": slice(513, 514)}[where]] = True
+    t[~keep] = -100
+    weights = torch.rand(m, generator=gen, device=DEV) + 0.5
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    smat.smat_linear_xent(x, w, t, loss, lse)
+    check_gradients(x, w, t, "f32", *logits(x, w), lse, row_scale=weights)
