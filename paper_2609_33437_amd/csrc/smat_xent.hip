@@ -387,7 +387,7 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   // and blocks without any end at once.  A launch finds them; it is spent where it is estimated at a fiftieth of the call or
   // less.  (2048 x 128256 x 4096, half of the rows without: losses and gradients 4.75 ms, 6.15 ms with
   // products over all rows.)
-  p.some = a.k > 0 && !p.low && us > 50.0 * (10.0 + (double)a.m / 1000.0);
+  p.some = a.m > 0 && a.k > 0 && !p.low && us > 50.0 * (10.0 + (double)a.m / 1000.0);
   plan_products(a, dtype, p, like);
   // A row left out moves the ones behind it up, but not into a part that sums in another order than theirs (fp32 515 x 32003 x 769
   // with a tenth of the rows without a target: 765 us; 742 where the 464 rows leave none to the second part, whose rows then

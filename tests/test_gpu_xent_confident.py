@@ -139,3 +139,15 @@ def test_a_part_without_rows(where):
     loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
     smat.smat_linear_xent(x, w, t, loss, lse)
     check_gradients(x, w, t, "f32", *logits(x, w), lse, row_scale=weights)
+
+
+@pytest.mark.parametrize("dtype,n,k", [("f32", 151936, 4096), ("bf16", 40000, 1024)])
+def test_an_empty_batch_before_a_large_head(dtype, n, k):
+    """No rows, and a head whose products would be long: a gradient of zeros."""
+    x, w, t = torch.empty(0, k, device=DEV, dtype=DT[dtype]), torch.ones(n, k, device=DEV, dtype=DT[dtype]), torch.empty(0, dtype=torch.int64, device=DEV)
+    lse, dw = torch.empty(0, device=DEV), torch.full_like(w, 7.0)
+    smat.smat_linear_xent_grad(x, w, t, lse, dx=torch.empty_like(x), dw=dw)
+    assert not dw.any()
+    dw.fill_(7.0)
+    smat.smat_linear_xent_grad(x, w, t, lse, dw=dw, workspace=torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV))
+    assert not dw.any()
