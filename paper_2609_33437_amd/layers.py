@@ -12,7 +12,8 @@ byte, against d + 2 f or d + 3 f of two bytes.
 Gradients are those of the checkpointed values: they differ from exact ones by what 8 bits lose of the
 saved activations (about one per cent of a weight gradient's norm), never in the forward pass.  They have no
 derivatives of their own, and there are none in forward mode: asking for either raises.  Without gradients (a merged
-model answering) nothing is saved, and a few tokens take the product's form for few rows.
+model answering) nothing is saved, and a few tokens take the product's form for few rows.  torch.jit.trace keeps a call as
+one node; make_fx and torch.export, which would lose it, are refused.
 
 What stands between a decoder's linear layers is here too: the token embedding, layer and RMS norms, and the output layer
 with its cross entropy, whose logits are never stored (smat_embed, smat_norm, smat_linear_xent).  Norms compute in fp32
@@ -95,10 +96,39 @@ def _elsewhere(x: torch.Tensor) -> bool:
     return x.is_cuda and x.get_device() != torch._C._cuda_getDevice()
 
 
+_modes, _included = torch._C._len_torch_dispatch_stack, torch._C._dispatch_tls_is_dispatch_key_included
+_pre_dispatch, _jit_trace = torch._C.DispatchKey.PreDispatch, torch._C._get_tracing_state
+
+
+def _refuse_graph_tracers() -> None:
+    """Raises while make_fx or torch.export records the operators that torch dispatches: it would see an output's allocation and
+    not the call that writes it, inside an autograd function too."""
+    if _modes() or _included(_pre_dispatch):
+        from torch.fx.experimental.proxy_tensor import get_proxy_mode
+
+        if get_proxy_mode() is not None:
+            raise SmatError(SMAT_ERR_INVALID, "the layers cannot be recorded by make_fx or torch.export")
+
+
+def _derivative(backward):
+    """A backward pass that has no derivatives of its own and is not recorded by graph tracers."""
+
+    @once_differentiable
+    def checked(ctx, *grads):
+        _refuse_graph_tracers()
+        return backward(ctx, *grads)
+
+    return checked
+
+
 def _saves(*tensors) -> bool:
-    """Whether autograd records the call.  Where it does not, tangents, which torch carries through frozen
-    weights and no_grad too, are refused (the recorded functions raise on them themselves)."""
+    """Whether the call goes through its autograd function: autograd records it, or torch.jit.trace does, which keeps the
+    function as one node.  Where it does not, tangents, which torch carries through frozen weights and no_grad too, are
+    refused (the recorded functions raise on them themselves)."""
+    _refuse_graph_tracers()
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        return True
+    if _jit_trace() is not None:
         return True
     if getattr(forward_ad, "_current_level", 0) >= 0 and any(      # -1: no tangents are about
             t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
@@ -151,7 +181,7 @@ class _Linear(torch.autograd.Function):
         return out
 
     @staticmethod
-    @once_differentiable
+    @_derivative
     def backward(ctx, dy):
         w, *saved = ctx.saved_tensors
         need_x, need_w, need_b, need_r = ctx.needs_input_grad
@@ -185,7 +215,7 @@ class _Mlp(torch.autograd.Function):
         return out
 
     @staticmethod
-    @once_differentiable
+    @_derivative
     def backward(ctx, dy):
         w1, w2, *saved = ctx.saved_tensors
         kept = _kept(ctx, saved)
@@ -233,7 +263,7 @@ class _GatedMlp(torch.autograd.Function):
         return out
 
     @staticmethod
-    @once_differentiable
+    @_derivative
     def backward(ctx, dy):
         wg, wu, wd, *saved = ctx.saved_tensors
         kept = _kept(ctx, saved)
@@ -276,7 +306,7 @@ class _Norm(torch.autograd.Function):
         return y
 
     @staticmethod
-    @once_differentiable
+    @_derivative
     def backward(ctx, dy):
         x, w, mean, rstd = ctx.saved_tensors
         need_x, need_w, need_b, _, _ = ctx.needs_input_grad
@@ -301,7 +331,7 @@ class _Embedding(torch.autograd.Function):
         return out
 
     @staticmethod
-    @once_differentiable
+    @_derivative
     def backward(ctx, dy):
         ids, = ctx.saved_tensors
         dtable = torch.empty(ctx.shape, dtype=ctx.dtype, device=dy.device)
@@ -320,7 +350,7 @@ class _LinearXent(torch.autograd.Function):
         return loss if reduction == 0 else totals[2 * reduction - 2].clone()
 
     @staticmethod
-    @once_differentiable
+    @_derivative
     def backward(ctx, grad):
         x, w, targets, lse, totals = ctx.saved_tensors
         need_x, need_w = ctx.needs_input_grad[:2]
@@ -447,8 +477,9 @@ def embedding(ids, weight, scale: float = 1.0, padding_idx: Optional[int] = None
     if padding_idx is not None and not 0 <= padding_idx < weight.shape[0]:
         raise SmatError(SMAT_ERR_INVALID, f"padding_idx {padding_idx} is outside the table")
     dtype = torch.get_autocast_dtype("cuda") if torch.is_autocast_enabled("cuda") else weight.dtype
-    weight, shape, flat = _weight(weight), ids.shape, _ids(ids, weight, "ids")
-    if _saves(weight):
+    weight = _weight(weight)
+    saved, shape, flat = _saves(weight), ids.shape, _ids(ids, weight, "ids")
+    if saved:
         out = _Embedding.apply(weight, flat, float(scale), padding_idx, dtype)
     else:
         out = torch.empty(flat.shape[0], weight.shape[1], dtype=dtype, device=weight.device)
@@ -469,8 +500,9 @@ def linear_cross_entropy(x, weight, targets, ignore_index: int = -100, reduction
     x, weight = _cast(x, weight)
     if x.shape[:-1] != targets.shape:
         raise SmatError(SMAT_ERR_INVALID, f"targets have shape {tuple(targets.shape)}, the rows of x {tuple(x.shape[:-1])}")
-    x, weight, flat, how = _rows(x), _weight(weight), _ids(targets, x, "targets"), ("none", "sum", "mean").index(reduction)
-    if _saves(x, weight):
+    x, weight, how = _rows(x), _weight(weight), ("none", "sum", "mean").index(reduction)
+    saved, flat = _saves(x, weight), _ids(targets, x, "targets")
+    if saved:
         loss = _LinearXent.apply(x, weight, flat, int(ignore_index), how)
     else:
         loss, _, totals = _losses(x, weight, flat, int(ignore_index), how, False)
