@@ -1397,7 +1397,7 @@ void operands(const LinArgs& a, LinEpilogue epi, int bytes, Operand (&o)[4]) {
   const bool pt = p_transposed(epi), qt = q_transposed(epi);
   for (int s = 0; s < 2; ++s) {
     const LinProduct& pr = a.prod[s];
-    const int64_t ends = pr.p_clean ? 0 : pr.r;  // Q's rows past r read as zeros, so finite values past P's do no harm
+    const int64_t ends = a.p_clean ? 0 : pr.r;  // Q's rows past r read as zeros, so finite values past P's do no harm
     o[2 * s] = {pr.p, pr.ldp, pt ? pr.r : a.i, pt ? a.i : pr.r, pr.r == 0 || operand_fits(pr.p, pr.ldp, ends, pt, bytes), pt};
     o[2 * s + 1] = {pr.q, pr.ldq, qt ? pr.r : a.j, qt ? a.j : pr.r, pr.r == 0 || operand_fits(pr.q, pr.ldq, pr.r, qt, bytes), qt};
   }

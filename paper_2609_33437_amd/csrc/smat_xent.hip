@@ -264,8 +264,9 @@ Piece piece_args(const XentGradArgs& a, int dtype, const XentGradPlan& plan, int
   q.logits.lse = a.lse;
   q.logits.lse_low = a.lse_low;
   q.logits.row_scale = a.row_scale;
-  q.dx.prod[0] = LinProduct{dz, w, plan.width, ldw, width, true};
-  if (low) q.dx.prod[1] = LinProduct{low, w, plan.width, ldw, width, true};
+  q.dx.prod[0] = LinProduct{dz, w, plan.width, ldw, width};
+  if (low) q.dx.prod[1] = LinProduct{low, w, plan.width, ldw, width};
+  q.dx.p_clean = 1;
   q.dx.i = a.m;
   q.dx.j = a.k;
   q.dx.out = a.dx;
