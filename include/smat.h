@@ -651,8 +651,9 @@ smat_status smat_linear_wgrad(const smat_linear_wgrad_args* args, void* workspac
 
 /* ---------------------------------------------------------------- norms, token embedding, output layer with its loss
  * What a decoder has beside attention and the linear layers above.  Conventions as there: row-major matrices with a row
- * stride, at any element's alignment; fp32 arithmetic, each output rounded once; outputs overlap neither inputs nor
- * each other nor the workspace; the calls can be captured into a graph, and their results are the same bits in every run. */
+ * stride, at any element's alignment; fp32 arithmetic, each output rounded once (the output layer's gradients also round the
+ * logits' gradient dz to their dtype, see there); outputs overlap neither inputs nor each other nor the workspace; the calls
+ * can be captured into a graph, and their results are the same bits in every run. */
 
 typedef enum smat_norm_kind {
   SMAT_NORM_LAYER = 0, /* y = (x - mean) rstd w + b, mean = mean x, rstd = 1 / sqrt(mean (x - mean)^2 + eps) */
@@ -741,9 +742,12 @@ typedef struct smat_embed_grad_args {
 smat_status smat_embed_grad_workspace_bytes(const smat_embed_grad_args* args, size_t* bytes);
 smat_status smat_embed_grad(const smat_embed_grad_args* args, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* Arguments of smat_linear_xent: the cross entropy of the logits z = x W^T against targets, without storing z.
+/* Arguments of smat_linear_xent: the cross entropy of the logits z = x W^T against targets, without storing z whole.
  *   lse[i] = log sum_j exp z[i][j], loss[i] = lse[i] - z[i][targets[i]]
- * lse_low[i] is what rounding lse[i] to fp32 left of it (0 where lse[i] is not finite).  A target of ignore_index marks a row without one: its loss is 0.  Another target outside [0, n) gives a loss of NaN. */
+ * lse_low[i] is what rounding lse[i] to fp32 left of it (0 where lse[i] is not finite).  A target of ignore_index marks a row
+ * without one: its loss is 0.  Another target outside [0, n) gives a loss of NaN.  The workspace holds two fp32 numbers for each 32
+ * to 256 logits of a row, copies of x and W where their rows are off 16 bytes and copying pays, and where tiles of z are too few
+ * to fill the GPU, fp32 sums of z over ranges of k, which are below 135 MB. */
 typedef struct smat_linear_xent_args {
   int32_t dtype, reserved; /* smat_dtype of x and w; reserved must be 0 */
   int64_t m, n, k;         /* rows, classes (> 0), width */
@@ -771,9 +775,14 @@ smat_status smat_linear_xent(const smat_linear_xent_args* args, void* workspace,
  *   dx = s dz W,  dW = s dz^T x,  s = scale[0] / totals[1]
  * The log sum is lse + lse_low.  With lse alone every probability of a row is off by lse's rounding, 2^-24 |lse| of itself, and
  * the dz of a target whose probability is within that of 1 is lost; with both such rows keep theirs.
- * Rows without a target take no part, whatever x, lse and row_scale hold in them, and their rows of dx are zeros.  The
- * vocabulary is taken in pieces: z is computed again and dz, rounded to dtype, held for one piece (in the workspace), so
- * nothing of the size m * n is stored.  s multiplies the fp32 sums; it is 0 where totals[1] is. */
+ * Rows without a target take no part, whatever x, lse, lse_low and row_scale hold in them, and their rows of dx are zeros.  s
+ * multiplies the fp32 sums; it is 0 where totals[1] is.
+ * The vocabulary is taken in pieces: z is computed again and dz, rounded to dtype, held for one piece.  In bf16 with up to 128 rows
+ * what that rounding left is held and multiplied too; with more, dx and dw carry it, up to 2^-8 of each dz, beside their own
+ * rounding.  A piece has all classes where m * n values of dtype are 128 MB or less, else as many as make its dz about 128 MB, and
+ * 1024 at least, so dz is larger beyond 65,536 rows of bf16 or 32,768 of fp32.  The workspace holds a piece's dz, a copy of x
+ * [m, k], with several pieces the fp32 sums of dx [m, k], where W's rows are off 16 bytes and copying pays a piece of W, 28 bytes
+ * a row, and sums over ranges as smat_linear_xent's. */
 typedef struct smat_linear_xent_grad_args {
   int32_t dtype, reserved; /* smat_dtype of x, w, dx and dw; reserved must be 0 */
   int64_t m, n, k;

@@ -141,7 +141,7 @@ def _xent(a, x, w, targets, lse, totals, lse_low):
 
 def smat_linear_xent(x, w, targets, loss, lse, totals=None, ignore_index: int = -100, workspace=None, stream=None,
                      lse_low=None) -> None:
-    """loss[i] = lse[i] - z[i, targets[i]] with z = x w^T and lse[i] = log sum_j exp z[i, j], without storing z; totals (fp32
+    """loss[i] = lse[i] - z[i, targets[i]] with z = x w^T and lse[i] = log sum_j exp z[i, j], without storing z whole; totals (fp32
     [3]) = the losses' sum, the number of rows with a target, and their mean.  lse_low (fp32 [m]) = what rounding lse left."""
     a = smat_linear_xent_args(dtype=_first(x, "x"), ignore_index=int(ignore_index))
     m, _, _, device = _xent(a, x, w, targets, lse, totals, lse_low)

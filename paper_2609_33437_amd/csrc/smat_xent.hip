@@ -10,8 +10,8 @@
 // The forward product's epilogue leaves the largest value and the sum of exponentials of each tile's columns of a row, which
 // k_xent_rows joins.  The gradient goes through the vocabulary in pieces: a piece's logits again, turned into dz (in the
 // call's dtype) by their epilogue, then dz W added to dx in fp32 and dz^T x, which is the piece's part of dW.  So beside
-// its outputs a call holds one piece, whatever the vocabulary, for a fourth product beside the three that
-// cannot be left out.  s is applied to the fp32 sums of both products, so a mean over many rows costs dz no precision.
+// its outputs a call holds one piece of dz, a copy of x and, with several pieces, fp32 sums of dx, whatever the vocabulary, for a
+// fourth product beside the three that cannot be left out.  s is applied to the fp32 sums of both products, so a mean over many rows costs dz no precision.
 #include "smat_decoder.h"
 #include "smat_linear_dev.h"
 
@@ -323,8 +323,10 @@ double plan_products(const XentGradArgs& a, int dtype, XentGradPlan& p, const Li
     double piece = 0.0;
     for (const LinPlan* l : {&p.logits[last], &p.dx[last], &p.dw[last]}) {
       if (l->workspace > product) product = l->workspace;
-      // stages by way of registers take 1.5 times their estimate in bf16 where rows of W are far from whole cache lines (160 x
-      // 62106 x 2982: 190 us)
+      // bf16 stages by way of registers take up to 1.5 times their estimate, which decides between them and a copy of W.  Calls
+      // copied and by way of registers, where the factor makes the choice: 33 x 62106 x 1537 361 and 456 us, 160 x 62106 x 4097
+      // 850 and 896, 300 x 10007 x 2982 138 and 146, 160 x 32003 x 1537 209 and 207, 9 x 62106 x 769 195 and 178, 100 x 62106 x 2982
+      // 633 and 545: over 15 sizes the copies spare up to 26 % and cost up to 14 %
       piece += l->us * (dtype == 1 && l->parts && !l->direct ? 1.5 : 1.0);
     }
     if (p.pack) piece += pack_us((double)q.logits.j * (double)a.k * (double)bytes);
@@ -351,10 +353,13 @@ XentGradPlan xent_grad_plan(const XentGradArgs& a, int dtype) {
   XentGradPlan p{};
   const int64_t bytes = dtype == 1 ? 2 : 4;
   if (!a.dx && !a.dw) return p;
-  // With few rows a rounding of dz is not averaged out in dx and dW, and W's and dW's bytes bound the products: both halves of
-  // dz are multiplied.
+  // With both halves of dz multiplied, dx and dW are as exact as their own rounding; with one, theirs and dz's add up.  Up to
+  // kLowRows rows, where W's and dW's bytes bound the products, the second half costs a quarter or a third (32000 x 1024: 32 rows 77 us
+  // and 62, errors of dx and dW against float64 1.66e-3 and 1.43e-3 of their norms, 2.07e-3 and 1.90e-3; 128 rows 99 us and 75,
+  // 1.66e-3 and 1.38e-3, 2.01e-3 and 1.74e-3), with more up to a half (512 rows 205 us and 140, 1.66e-3 and 1.47e-3, 1.97e-3 and
+  // 1.81e-3).
   p.low = dtype == 1 && a.m <= kLowRows;
-  // a piece's dz of up to 128 MB stays in the Infinity Cache between the three products that write and read it
+  // a piece's dz of about 128 MB stays in the Infinity Cache between the three products that write and read it
   // (4096 x 128256 x 2048: 6.61 ms with losses, in pieces of 64 MB 6.81 ms, of 512 MB 6.53 ms, in one of 1.05 GB 6.50 ms)
   constexpr int64_t kPieceBytes = 128ll << 20, kLeast = 1024;
   int64_t most = a.m > 0 ? kPieceBytes / (a.m * bytes) / 256 * 256 : a.n;
