@@ -151,3 +151,32 @@ def test_an_empty_batch_before_a_large_head(dtype, n, k):
     dw.fill_(7.0)
     smat.smat_linear_xent_grad(x, w, t, lse, dw=dw, workspace=torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV))
     assert not dw.any()
+
+
+def test_captured_with_rows_left_out():
+    """One graph of losses and gradients, replayed for batches that leave out other rows, whole parts of them too."""
+    m, n, k = 515, 32003, 769
+    gen = torch.Generator(DEV).manual_seed(4)
+    x, w = torch.randn(m, k, generator=gen, device=DEV), torch.randn(n, k, generator=gen, device=DEV) * 0.1
+    t = torch.randint(0, n, (m,), generator=gen, device=DEV)
+
+    def step():
+        loss, lse, low, tot = (torch.empty(s, device=DEV) for s in (m, m, m, 3))
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        smat.smat_linear_xent(x, w, t, loss, lse, totals=tot, lse_low=low)
+        smat.smat_linear_xent_grad(x, w, t, lse, dx=dx, dw=dw, totals=tot, lse_low=low)
+        return loss, lse, low, tot, dx, dw
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = step()
+    for left_out in (slice(0, 0), slice(0, 512), slice(512, 515), slice(100, 514), slice(0, 515), slice(3, 4)):
+        t.copy_(torch.randint(0, n, (m,), generator=gen, device=DEV))
+        t[left_out] = -100
+        g.replay()
+        torch.cuda.synchronize()
+        got = [h.clone() for h in held]
+        for a, b in zip(got, step()):
+            assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num()), left_out
