@@ -16,7 +16,7 @@ model answering) nothing is saved, and a few tokens take the product's form for 
 one node; make_fx and torch.export, which would lose it, are refused.
 
 What stands between a decoder's linear layers is here too: the token embedding, layer and RMS norms, and the output layer
-with its cross entropy, whose logits are never stored (smat_embed, smat_norm, smat_linear_xent).  Norms compute in fp32
+with its cross entropy, whose logits are not kept (smat_embed, smat_norm, smat_linear_xent).  Norms compute in fp32
 and return their input's dtype, whatever autocast says, and their weights may be fp32 beside bf16 activations; an
 embedding under autocast returns its dtype.  The loss is fp32.
 
@@ -488,7 +488,7 @@ def embedding(ids, weight, scale: float = 1.0, padding_idx: Optional[int] = None
 
 
 def linear_cross_entropy(x, weight, targets, ignore_index: int = -100, reduction: str = "mean") -> torch.Tensor:
-    """The cross entropy of the logits x weight^T for x [.., k] against int64 targets [..], in fp32, without storing the logits.
+    """The cross entropy of the logits x weight^T for x [.., k] against int64 targets [..], in fp32, without keeping the logits.
     Rows whose target is ignore_index have no loss and no gradient; another target outside the vocabulary gives NaN.
     reduction: "mean" over the rows with a target (NaN where there is none, with gradients of 0), "sum", or "none" for each
     row's loss in targets' shape."""
